@@ -244,8 +244,13 @@ def _verify_state(c, g, rng):
         near = target[:, :K].contiguous()
         near += torch.randn(S, K, V, generator=g, device="cuda").mul_(0.5)
         s["draft"] = near
+        # the drafts are draws from the small model's truncated distribution
         noise = torch.rand(S, K, V, generator=g, device="cuda").clamp_(1e-30).log_().neg_().log_()
-        s["tokens"] = (near / max(c["T"], 1e-3) - noise).argmax(-1).to(torch.int32)
+        noise = near / max(c["T"], 1e-3) - noise
+        if c["min_p"] > 0:
+            low = near.amax(-1, keepdim=True) + c["T"] * math.log(c["min_p"])
+            noise = torch.where(near >= low, noise, -math.inf)
+        s["tokens"] = noise.argmax(-1).to(torch.int32)
     else:
         s["tokens"] = target[:, :K].argmax(-1).to(torch.int32)
     return s
