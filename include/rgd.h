@@ -388,6 +388,129 @@ int32_t rgd_kernel_probe_step(rgd_model* m, const float* logits, int32_t R, cons
                               int32_t* probe_tokens, int32_t* probe_len, int32_t* event,
                               rgd_stream stream);
 
+/* ---- paged sequences: a cache whose sequences differ in length, share pages
+ * and are forked, rolled back and compacted on the device ----
+ *
+ * A plain description of caller-owned device buffers (no handle; the fields are
+ * read during the call).  Sequence s holds positions [0, lens[s]); position t
+ * lies in slot t % page_size of page pages[s][t / page_size].  Several
+ * sequences may hold the same page; refs[p] counts the table entries that hold
+ * page p, 0 for a free one.  A cache starts with lens and refs 0.  The entry
+ * points below keep these arrays in line, take them in stream order and leave
+ * the host out of it, so a step of them can be captured into a graph.
+ * Entries of a table behind a sequence's pages say nothing.  A length outside
+ * [0, max_pages * page_size] counts as the nearest one inside; positions whose
+ * table entry is outside [0, n_pages) are neither written nor attended to. */
+typedef struct rgd_paged_cache {
+  int32_t n_layers;
+  int32_t n_pages;    /* at most 2^20 */
+  int32_t n_kv_heads; /* Hkv */
+  int32_t page_size;  /* positions per page: a multiple of 16, at most 4096 */
+  int32_t head_dim;   /* D: 32, 64 or 128 */
+  int32_t dtype;      /* rgd_dtype of K and V */
+  int32_t max_seqs;   /* S, at most 65536 */
+  int32_t max_pages;  /* table entries per sequence */
+  void* pool_k;       /* dev [n_layers][n_pages][Hkv][page_size][D], as in rgd_kv_create */
+  void* pool_v;       /* dev [n_layers][n_pages][Hkv][D][page_size] */
+  int32_t* pages;     /* dev [S][max_pages] */
+  int32_t* lens;      /* dev [S] */
+  int32_t* refs;      /* dev [n_pages] */
+  int32_t* status;    /* dev [1]: set to 1 by an rgd_paged_reserve that found no room */
+} rgd_paged_cache;
+
+/* Bytes of caller-provided device workspace (256-byte aligned) that
+ * rgd_paged_select, rgd_paged_reserve and rgd_paged_compact need; 0 for a
+ * description they refuse.  Calls that share a workspace must not overlap. */
+uint64_t rgd_paged_workspace_bytes(const rgd_paged_cache* cache);
+
+/* Forks, reorders, rolls back and frees, all sequences at once: sequence s
+ * becomes the first min(keep[s], len) positions of what sequence parent[s] was
+ * before the call.  No K or V is copied: the pages are shared.  parent dev
+ * int32 [S] (NULL, or an entry outside [0, S): s itself), keep dev int32 [S]
+ * (NULL or negative: every position; 0 frees the sequence).  refs follows;
+ * table entries that a sequence no longer has become -1.  workspace may be
+ * NULL when parent is.  Asynchronous. */
+int32_t rgd_paged_select(const rgd_paged_cache* cache, const int32_t* parent, const int32_t* keep, void* workspace,
+                         rgd_stream stream);
+
+/* Makes room for grow[s] more positions (dev int32 [S]; negative counts as 0)
+ * behind each sequence and adds them to lens.  New pages are the lowest free
+ * ones, in the order of the sequences.  A sequence that grows and whose last
+ * page is partly filled and held by another table entry too gets a copy of that
+ * page (every layer) in its place, so the new positions are its own.  If the
+ * pool has too few free pages or a table too few entries, status[0] is set to 1
+ * and nothing else is changed.  Asynchronous. */
+int32_t rgd_paged_reserve(const rgd_paged_cache* cache, const int32_t* grow, void* workspace, rgd_stream stream);
+
+/* Moves pages so that the pages held by any sequence (refs > 0) are the pages
+ * [0, n): those at or above n go, in order, to the free ones below it, in every
+ * layer; tables and refs follow.  live dev int32 [1] receives n.  Asynchronous. */
+int32_t rgd_paged_compact(const rgd_paged_cache* cache, int32_t* live, void* workspace, rgd_stream stream);
+
+/* Writes the K and V of each sequence's last n_new[s] positions (dev int32 [S],
+ * counts outside [0, n] as the nearest inside; NULL: n of each) of one layer:
+ * token i of sequence s goes to position lens[s] - n_new[s] + i (rgd_paged_reserve
+ * has made it, so that no other sequence holds its page; positions before 0 are
+ * left out).  k, v dev in the cache's type:
+ * row s * n + i at k + (s * n + i) * ldk elements, [Hkv][D] each; keys already
+ * rotated.  ldk, ldv >= Hkv * D; k, v and their row strides 16-byte aligned.
+ * Asynchronous. */
+int32_t rgd_paged_append(const rgd_paged_cache* cache, int32_t layer, const void* k, const void* v, int64_t ldk,
+                         int64_t ldv, int32_t n, const int32_t* n_new, rgd_stream stream);
+
+/* Bytes of device workspace (256-byte aligned) for rgd_paged_attention with up
+ * to n new tokens per sequence and n_heads query heads; 0 for arguments it
+ * refuses. */
+uint64_t rgd_paged_attention_workspace_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads);
+
+/* Causal attention of each sequence's last n_new[s] positions (as for
+ * rgd_paged_append, whose K and V are in the cache) over the whole sequence, one
+ * layer: token i sees positions [0, lens[s] - n_new[s] + i].  q dev in the
+ * cache's type, row s * n + i at q + (s * n + i) * ldq elements, [n_heads][D]
+ * (16-byte aligned rows); query head h reads KV head h / (n_heads / Hkv), scores
+ * are scaled by 1/sqrt(D).  out dev [S * n][n_heads * D] in the cache's type
+ * (16-byte aligned, not overlapping q), lse dev fp32 [S * n][n_heads] or NULL:
+ * the log of the sum of exponentiated scores, for joining with attention over
+ * other positions.  A token that sees nothing gets 0 and -inf; rows at or behind
+ * n_new[s] are left as they were.  Slots behind a length and free pages may hold
+ * anything.  1 <= n <= 1024, n_heads <= 1024.  Meant for few tokens: every 64
+ * query vectors (tokens x query heads per KV head) of a sequence read its K and
+ * V once.  Asynchronous. */
+int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,
+                            const int32_t* n_new, int32_t n_heads, void* workspace, void* out, float* lse,
+                            rgd_stream stream);
+
+/* ---- verification of drafted tokens ---- */
+
+/* Bytes of device workspace (256-byte aligned) for rgd_verify_drafts; 0 for
+ * sizes it refuses. */
+uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
+
+/* Checks up to K drafted tokens of each of S sequences against the target's
+ * distribution, so that the tokens kept are distributed as if they had been
+ * sampled from the target one by one.  target dev fp32 [S][K+1][V]: row i holds
+ * the logits after the first i drafts.  draft dev fp32 [S][K][V]: the logits
+ * draft_tokens (dev int32 [S][K]) were sampled from with the same T and min_p,
+ * or NULL: the drafts carry no distribution (a greedy probe, a lookup), each
+ * counts as certain.  n_draft dev int32 [S] or NULL (K of each; counts outside
+ * [0, K] as the nearest inside).  u dev fp32 [S][K+1]: uniform in [0, 1).
+ * With p_i the distribution of rgd_sample_continuations on target row i
+ * (temperature T, then min-p; T == 0: the first maximum has everything) and q_i
+ * that of draft row i (one-hot at the draft without draft logits or at T == 0):
+ * draft x_i is accepted while u[i] q_i(x_i) < p_i(x_i).  At the first refusal the next
+ * token is drawn from max(p_i - q_i, 0), after n_draft acceptances from p_i, by
+ * u[K]: the smallest id whose running weight exceeds u[K] times the total.
+ * out dev int32 [S][K+1]: the accepted drafts, the drawn token, then -1;
+ * n_accepted dev int32 [S].  A draft outside [0, V) is refused.  NaN logits
+ * count as -inf.  A target row whose maximum is not finite has no distribution:
+ * its draft is refused and -1 stands for the drawn token; such a draft row has
+ * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, T >= 0, min_p in
+ * [0, 1].  Sums are taken in fp64, so that the draw is the exact one unless u[K]
+ * meets the border of two tokens by 1e-11 of the total.  Asynchronous. */
+int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t* draft_tokens,
+                          const int32_t* n_draft, int32_t S, int32_t K, int32_t V, float T, float min_p,
+                          const float* u, void* workspace, int32_t* out, int32_t* n_accepted, rgd_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -13,7 +13,9 @@ import os
 __all__ = [
     "RGDError", "lib", "ModelConfig", "Model", "KV", "Table", "prefill_kv", "probe", "probe_fixed", "gate",
     "sample_continuations", "sample_continuations_pless", "check_status", "kernel_attention", "kernel_lm_head", "kernel_argmax",
-    "kernel_sample", "kernel_sample_noalloc", "kernel_sample_pless", "sampler_workspace_bytes", "timing_enable", "timing_read", "TIMERS", "EVENT_INCOMPAT", "EVENT_STOP", "EVENT_MAXLEN",
+    "kernel_sample", "kernel_sample_noalloc", "kernel_sample_pless", "sampler_workspace_bytes", "timing_enable", "timing_read", "TIMERS", "PagedCache", "paged_workspace_bytes", "paged_select",
+    "paged_reserve", "paged_compact", "paged_append", "paged_attention_workspace_bytes", "paged_attention",
+    "verify_workspace_bytes", "verify_drafts", "EVENT_INCOMPAT", "EVENT_STOP", "EVENT_MAXLEN",
     "DTYPE_F32", "DTYPE_BF16",
 ]
 
@@ -24,6 +26,8 @@ EXPORTS = (
     "rgd_prefill_kv", "rgd_prefill_kv_scored", "rgd_probe", "rgd_probe_fixed", "rgd_probe_soft", "rgd_probe_adaptive", "rgd_gate", "rgd_sample_continuations", "rgd_sample_continuations_pless", "rgd_check_status",
     "rgd_kernel_attention", "rgd_kernel_lm_head", "rgd_sampler_workspace_bytes",
     "rgd_kernel_argmax", "rgd_kernel_sample", "rgd_kernel_sample_noalloc", "rgd_kernel_sample_pless", "rgd_kernel_probe_step", "rgd_timing_enable", "rgd_timing_read",
+    "rgd_paged_workspace_bytes", "rgd_paged_select", "rgd_paged_reserve", "rgd_paged_compact", "rgd_paged_append",
+    "rgd_paged_attention_workspace_bytes", "rgd_paged_attention", "rgd_verify_workspace_bytes", "rgd_verify_drafts",
 )
 
 DTYPE_F32, DTYPE_BF16 = 0, 1
@@ -45,6 +49,7 @@ if not os.path.exists(LIB_PATH):
 lib = C.CDLL(LIB_PATH)
 
 VP, I32, U32, F32, U64 = C.c_void_p, C.c_int32, C.c_uint32, C.c_float, C.c_uint64
+I64 = C.c_int64
 I32P = C.POINTER(C.c_int32)
 
 
@@ -62,6 +67,12 @@ class LayerWeights(C.Structure):
 class Weights(C.Structure):
     _fields_ = [("embed", VP), ("final_norm", VP), ("lm_head", VP),
                 ("layers", C.POINTER(LayerWeights))]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [(n, I32) for n in ("n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "dtype", "max_seqs",
+                                   "max_pages")] + \
+               [(n, VP) for n in ("pool_k", "pool_v", "pages", "lens", "refs", "status")]
 
 
 def _sig(name, res, *args):
@@ -99,6 +110,16 @@ _sig("rgd_kernel_argmax", I32, VP, I32, I32, VP, VP, VP)
 _sig("rgd_kernel_sample", I32, VP, I32, I32, F32, F32, VP, U32, U32, I32, VP, VP, VP)
 _sig("rgd_kernel_sample_noalloc", I32, VP, I32, I32, F32, F32, VP, U32, U32, I32, VP, VP)
 _sig("rgd_kernel_sample_pless", I32, VP, I32, I32, F32, VP, U32, U32, I32, VP, VP, VP)
+_CACHE = C.POINTER(PagedCacheDesc)
+_sig("rgd_paged_workspace_bytes", U64, _CACHE)
+_sig("rgd_paged_select", I32, _CACHE, VP, VP, VP, VP)
+_sig("rgd_paged_reserve", I32, _CACHE, VP, VP, VP)
+_sig("rgd_paged_compact", I32, _CACHE, VP, VP, VP)
+_sig("rgd_paged_append", I32, _CACHE, I32, VP, VP, I64, I64, I32, VP, VP)
+_sig("rgd_paged_attention_workspace_bytes", U64, _CACHE, I32, I32)
+_sig("rgd_paged_attention", I32, _CACHE, I32, VP, I64, I32, VP, I32, VP, VP, VP, VP)
+_sig("rgd_verify_workspace_bytes", U64, I32, I32, I32)
+_sig("rgd_verify_drafts", I32, VP, VP, VP, VP, I32, I32, I32, F32, F32, VP, VP, VP, VP, VP)
 _sig("rgd_timing_enable", I32, VP, I32)
 _sig("rgd_timing_read", I32, VP, C.POINTER(C.c_double), C.POINTER(C.c_int64))
 
@@ -352,3 +373,176 @@ def kernel_sample_pless(z, T, seeds, ctr, stream0, draws, workspace, out):
     R, V = z.shape
     _check(lib.rgd_kernel_sample_pless(_ptr(z), R, V, T, _ptr(seeds), ctr, stream0, draws,
                                        _ptr(workspace), _ptr(out), _stream()))
+
+
+# ------------------------------------------------------------ paged sequences --
+def _refuse(msg):
+    raise RGDError(1, msg)
+
+
+def _on(device, **tensors):
+    """Refuses tensors that are not contiguous tensors of their type and shape on `device`.
+    name=(tensor, dtype name, shape or None, optional)."""
+    for name, (t, dtype, shape, optional) in tensors.items():
+        if t is None:
+            if not optional:
+                _refuse(f"{name} is None")
+            continue
+        if t.device != device or str(t.dtype) != "torch." + dtype:
+            _refuse(f"{name} must be a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            _refuse(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+        if not t.is_contiguous():
+            _refuse(f"{name} must be contiguous")
+
+
+def _workspace(device, ws, need):
+    _on(device, workspace=(ws, "uint8", None, False))
+    if ws.numel() < need:
+        _refuse(f"workspace holds {ws.numel()} of {need} bytes")
+
+
+def _rows(device, name, t, dtype, shape):
+    """The row stride of a tensor [rows][heads][D] whose rows may lie apart (a slice of a fused projection)."""
+    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        _refuse(f"{name} must be a {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2]):
+        _refuse(f"{name}: the heads of a row must be contiguous")
+    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+
+
+class _On:
+    """The device of the operands made current for one call, with its current stream."""
+
+    def __init__(self, device):
+        import torch
+        self.device, self.guard = device, torch.cuda.device(device)
+
+    def __enter__(self):
+        import torch
+        self.guard.__enter__()
+        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+
+    def __exit__(self, *e):
+        return self.guard.__exit__(*e)
+
+
+class PagedCache:
+    """Paged sequences over caller-owned device tensors (kept alive here):
+    pool_k [L][pages][Hkv][page_size][D], pool_v [L][pages][Hkv][D][page_size]
+    (bf16 or fp32), and int32 pages [S][max_pages], lens [S], refs [pages],
+    status [1].  The operators below change the tensors in place."""
+
+    def __init__(self, pool_k, pool_v, pages, lens, refs, status):
+        dtypes = {"torch.bfloat16": DTYPE_BF16, "torch.float32": DTYPE_F32}
+        if pool_k.dim() != 5 or str(pool_k.dtype) not in dtypes or not pool_k.is_cuda:
+            _refuse("pool_k must be a 5-dimensional bf16 or fp32 tensor on a GPU")
+        L, P, H, ps, D = pool_k.shape
+        if pages.dim() != 2:
+            _refuse("pages must have two dimensions")
+        S, width = pages.shape
+        name = str(pool_k.dtype)[len("torch."):]
+        self.device = pool_k.device
+        _on(self.device, pool_k=(pool_k, name, None, False), pool_v=(pool_v, name, (L, P, H, D, ps), False),
+            pages=(pages, "int32", None, False), lens=(lens, "int32", (S,), False),
+            refs=(refs, "int32", (P,), False), status=(status, "int32", (1,), False))
+        self.pool_k, self.pool_v, self.pages, self.lens, self.refs, self.status = pool_k, pool_v, pages, lens, refs, status
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, P, H, ps, D
+        self.max_seqs, self.max_pages = S, width
+        self.desc = PagedCacheDesc(L, P, H, ps, D, dtypes["torch." + name], S, width, pool_k.data_ptr(),
+                                   pool_v.data_ptr(), pages.data_ptr(), lens.data_ptr(), refs.data_ptr(),
+                                   status.data_ptr())
+
+
+def _bytes(n):
+    if n == 0:
+        raise RGDError(1, lib.rgd_last_error().decode())
+    return int(n)
+
+
+def paged_workspace_bytes(cache):
+    return _bytes(lib.rgd_paged_workspace_bytes(C.byref(cache.desc)))
+
+
+def paged_select(cache, parent, keep, workspace):
+    """Sequence s becomes the first keep[s] positions (None or negative: all) of
+    sequence parent[s] (None or outside the cache: itself), all at once."""
+    S = cache.max_seqs
+    _on(cache.device, parent=(parent, "int32", (S,), True), keep=(keep, "int32", (S,), True))
+    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
+    with _On(cache.device) as s:
+        _check(lib.rgd_paged_select(C.byref(cache.desc), _ptr(parent), _ptr(keep), _ptr(workspace), s))
+
+
+def paged_reserve(cache, grow, workspace):
+    """Makes room for grow[s] more positions of each sequence and adds them to lens;
+    cache.status becomes 1, and nothing else changes, where there is none."""
+    _on(cache.device, grow=(grow, "int32", (cache.max_seqs,), False))
+    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
+    with _On(cache.device) as s:
+        _check(lib.rgd_paged_reserve(C.byref(cache.desc), _ptr(grow), _ptr(workspace), s))
+
+
+def paged_compact(cache, live, workspace):
+    """Moves the live pages to [0, live[0])."""
+    _on(cache.device, live=(live, "int32", (1,), False))
+    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
+    with _On(cache.device) as s:
+        _check(lib.rgd_paged_compact(C.byref(cache.desc), _ptr(live), _ptr(workspace), s))
+
+
+def paged_append(cache, layer, k, v, n, n_new=None):
+    """K and V rows [S * n][Hkv][D] (rows may lie apart) of each sequence's last n_new[s]
+    (None: n) positions into the pages of one layer."""
+    S, shape = cache.max_seqs, (cache.max_seqs * n, cache.n_kv_heads, cache.head_dim)
+    _on(cache.device, n_new=(n_new, "int32", (S,), True))
+    ldk = _rows(cache.device, "k", k, cache.pool_k.dtype, shape)
+    ldv = _rows(cache.device, "v", v, cache.pool_k.dtype, shape)
+    with _On(cache.device) as s:
+        _check(lib.rgd_paged_append(C.byref(cache.desc), layer, _ptr(k), _ptr(v), ldk, ldv, n, _ptr(n_new), s))
+
+
+def paged_attention_workspace_bytes(cache, n, n_heads):
+    return _bytes(lib.rgd_paged_attention_workspace_bytes(C.byref(cache.desc), n, n_heads))
+
+
+def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
+    """Causal attention of each sequence's last n_new[s] (None: n) positions, q
+    [S * n][heads][D] (rows may lie apart), into out [S * n][heads * D] and lse [S * n][heads]."""
+    S, D = cache.max_seqs, cache.head_dim
+    if q.dim() != 3:
+        _refuse("q must have three dimensions")
+    heads = q.shape[1]
+    ldq = _rows(cache.device, "q", q, cache.pool_k.dtype, (S * n, heads, D))
+    _on(cache.device, n_new=(n_new, "int32", (S,), True),
+        out=(out, str(cache.pool_k.dtype)[len("torch."):], (S * n, heads * D), False),
+        lse=(lse, "float32", (S * n, heads), True))
+    _workspace(cache.device, workspace, paged_attention_workspace_bytes(cache, n, heads))
+    with _On(cache.device) as s:
+        _check(lib.rgd_paged_attention(C.byref(cache.desc), layer, _ptr(q), ldq, n, _ptr(n_new), heads,
+                                       _ptr(workspace), _ptr(out), _ptr(lse), s))
+
+
+# ------------------------------------------------------- verification of drafts --
+def verify_workspace_bytes(S, K, V):
+    n = lib.rgd_verify_workspace_bytes(S, K, V)
+    if n == 0:
+        _refuse("S, K or V out of range")
+    return int(n)
+
+
+def verify_drafts(target, draft, draft_tokens, n_draft, T, min_p, u, workspace, out, n_accepted):
+    """Accepts a prefix of each sequence's drafts and draws the token after it, from target
+    logits [S][K+1][V], the drafts' logits [S][K][V] (None: certain drafts) and uniforms u [S][K+1]."""
+    if target.dim() != 3 or not target.is_cuda:
+        _refuse("target must be a 3-dimensional tensor on a GPU")
+    S, K, V = target.shape[0], target.shape[1] - 1, target.shape[2]
+    dev = target.device
+    _on(dev, target=(target, "float32", None, False), draft=(draft, "float32", (S, K, V), True),
+        draft_tokens=(draft_tokens, "int32", (S, K), False), n_draft=(n_draft, "int32", (S,), True),
+        u=(u, "float32", (S, K + 1), False), out=(out, "int32", (S, K + 1), False),
+        n_accepted=(n_accepted, "int32", (S,), False))
+    _workspace(dev, workspace, verify_workspace_bytes(S, K, V))
+    with _On(dev) as s:
+        _check(lib.rgd_verify_drafts(_ptr(target), _ptr(draft), _ptr(draft_tokens), _ptr(n_draft), S, K, V, T, min_p,
+                                     _ptr(u), _ptr(workspace), _ptr(out), _ptr(n_accepted), s))

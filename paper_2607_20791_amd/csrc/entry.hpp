@@ -8,6 +8,8 @@ namespace rgd {
 
 // Sets the thread's last-error message and returns code.
 int32_t set_error(int32_t code, const char* msg);
+// Empties it (at the start of an entry point).
+void clear_error();
 
 // min-p (pless false) or p-less draws on z [R][V] with a caller-provided
 // device workspace of rgd_sampler_workspace_bytes(R, V) bytes, 256-byte

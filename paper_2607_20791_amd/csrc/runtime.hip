@@ -1706,6 +1706,8 @@ namespace rgd {
 
 int32_t set_error(int32_t code, const char* msg) { return fail(code, "%s", msg); }
 
+void clear_error() { g_err.clear(); }
+
 int32_t kernel_sample(const float* z, int32_t R, int32_t V, float T, float min_p, bool pless,
                       const uint64_t* seeds, uint32_t ctr, uint32_t stream0, int32_t draws, void* workspace,
                       int32_t* out, rgd_stream stream) {

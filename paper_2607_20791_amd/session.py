@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import DTYPE_BF16, DTYPE_F32, KV, Model, ModelConfig
+from . import DTYPE_BF16, DTYPE_F32, KV, Model, ModelConfig, PagedCache
 
 
 def _torch():
@@ -59,6 +59,17 @@ def alloc_kv(model: Model, w, max_prompts: int, max_prefix: int, n_pages: int,
     qk = torch.zeros(pool_k, dtype=dt, device="cuda")
     qv = torch.zeros(pool_v, dtype=dt, device="cuda")
     return KV(model, max_prompts, max_prefix, n_pages, page_size, pk, pv, qk, qv)
+
+
+def alloc_paged(n_layers: int, n_pages: int, n_kv_heads: int, head_dim: int, max_seqs: int, max_pages: int,
+                page_size: int = 16, bf16: bool = True) -> PagedCache:
+    """An empty paged cache on the current GPU: max_seqs sequences of up to max_pages pages out of n_pages."""
+    torch = _torch()
+    dt = torch.bfloat16 if bf16 else torch.float32
+    k = torch.zeros(n_layers, n_pages, n_kv_heads, page_size, head_dim, dtype=dt, device="cuda")
+    v = torch.zeros(n_layers, n_pages, n_kv_heads, head_dim, page_size, dtype=dt, device="cuda")
+    i32 = lambda fill, *s: torch.full(s, fill, dtype=torch.int32, device="cuda")  # noqa: E731
+    return PagedCache(k, v, i32(-1, max_seqs, max_pages), i32(0, max_seqs), i32(0, n_pages), i32(0, 1))
 
 
 def v_stride(max_prefix: int) -> int:

@@ -1,0 +1,96 @@
+"""Refusals of the paged-sequence and draft-verification entry points: before any
+HIP call, so they run without a GPU (no pointer here is ever followed)."""
+import ctypes as C
+
+import pytest
+
+INVALID = 1
+
+
+@pytest.fixture(scope="module")
+def rgd():
+    import paper_2607_20791_amd as m
+    return m
+
+
+GOOD = dict(n_layers=2, n_pages=8, n_kv_heads=2, page_size=16, head_dim=64, dtype=1, max_seqs=3, max_pages=4,
+            pool_k=0x1000, pool_v=0x2000, pages=0x3000, lens=0x3100, refs=0x3200, status=0x3300)
+WS = C.c_void_p(0x10000)
+P = C.c_void_p(0x40000)
+OUT = C.c_void_p(0x80000)
+
+
+def _desc(rgd, **kw):
+    return C.byref(rgd.PagedCacheDesc(**{**GOOD, **kw}))
+
+
+BAD = [dict(n_layers=0), dict(n_pages=0), dict(n_pages=(1 << 20) + 1), dict(n_kv_heads=0), dict(page_size=8),
+       dict(page_size=24), dict(page_size=8192), dict(head_dim=48), dict(head_dim=256), dict(dtype=2), dict(max_seqs=0),
+       dict(max_seqs=65537), dict(max_pages=0), dict(max_pages=1 << 27), dict(pool_k=None), dict(pool_v=None),
+       dict(pool_k=0x1008), dict(pages=None), dict(lens=None), dict(refs=None), dict(status=None)]
+
+
+@pytest.mark.parametrize("kw", BAD, ids=lambda k: "-".join(f"{a}={b}" for a, b in k.items()))
+def test_bad_descriptions_are_refused_everywhere(rgd, kw):
+    lib, d = rgd.lib, _desc(rgd, **kw)
+    assert lib.rgd_paged_workspace_bytes(d) == 0 and lib.rgd_last_error()
+    assert lib.rgd_paged_attention_workspace_bytes(d, 1, 2) == 0
+    assert lib.rgd_paged_select(d, P, P, WS, None) == INVALID and lib.rgd_last_error()
+    assert lib.rgd_paged_reserve(d, P, WS, None) == INVALID
+    assert lib.rgd_paged_compact(d, P, WS, None) == INVALID
+    assert lib.rgd_paged_append(d, 0, P, P, 128, 128, 1, None, None) == INVALID
+    assert lib.rgd_paged_attention(d, 0, P, 128, 1, None, 2, WS, OUT, None, None) == INVALID
+
+
+def test_null_descriptions_and_arguments(rgd):
+    lib, d = rgd.lib, _desc(rgd)
+    off = C.c_void_p(0x10010)
+    assert lib.rgd_paged_workspace_bytes(None) == 0
+    assert lib.rgd_paged_workspace_bytes(d) > 0 and lib.rgd_last_error() == b""
+    for rc in (lib.rgd_paged_select(None, P, P, WS, None), lib.rgd_paged_select(d, P, None, None, None),
+               lib.rgd_paged_select(d, P, None, off, None), lib.rgd_paged_reserve(d, None, WS, None),
+               lib.rgd_paged_reserve(d, P, None, None), lib.rgd_paged_reserve(d, P, off, None),
+               lib.rgd_paged_compact(d, None, WS, None), lib.rgd_paged_compact(d, P, off, None)):
+        assert rc == INVALID and lib.rgd_last_error()
+
+
+def test_append_arguments(rgd):
+    lib, d = rgd.lib, _desc(rgd)
+
+    def call(layer=0, k=P, v=P, ldk=128, ldv=128, n=1):
+        return lib.rgd_paged_append(d, layer, k, v, ldk, ldv, n, None, None)
+
+    for kw in (dict(layer=2), dict(layer=-1), dict(k=None), dict(v=None), dict(ldk=127), dict(ldv=120), dict(ldk=132),
+               dict(k=C.c_void_p(0x40008)), dict(n=0), dict(n=1 << 24)):
+        assert call(**kw) == INVALID, kw
+
+
+def test_attention_arguments(rgd):
+    lib, d = rgd.lib, _desc(rgd)
+    assert lib.rgd_paged_attention_workspace_bytes(d, 1, 4) > 0
+    for n, h in ((0, 4), (1025, 4), (1, 0), (1, 3), (1, 1026)):
+        assert lib.rgd_paged_attention_workspace_bytes(d, n, h) == 0
+
+    def call(layer=0, q=P, ldq=256, n=1, heads=4, ws=WS, out=OUT):
+        return lib.rgd_paged_attention(d, layer, q, ldq, n, None, heads, ws, out, None, None)
+
+    for kw in (dict(layer=2), dict(q=None), dict(ldq=255), dict(ldq=260), dict(q=C.c_void_p(0x40002)), dict(n=0),
+               dict(heads=3), dict(ws=None), dict(ws=C.c_void_p(0x10080)), dict(out=None),
+               dict(out=C.c_void_p(0x80008)), dict(out=P), dict(out=C.c_void_p(0x40000 + 512))):
+        assert call(**kw) == INVALID, kw
+
+
+def test_verify_arguments(rgd):
+    lib = rgd.lib
+    for s, k, v in ((0, 4, 100), (65537, 4, 100), (1, 0, 100), (1, 256, 100), (1, 4, 1), (1, 4, (1 << 20) + 1)):
+        assert lib.rgd_verify_workspace_bytes(s, k, v) == 0
+    assert lib.rgd_verify_workspace_bytes(2, 4, 101) > 0
+
+    def call(target=P, tokens=P, S=2, K=4, V=101, T=1.0, min_p=0.1, u=P, ws=WS, out=OUT, count=OUT):
+        return lib.rgd_verify_drafts(target, None, tokens, None, S, K, V, T, min_p, u, ws, out, count, None)
+
+    nan = float("nan")
+    for kw in (dict(target=None), dict(tokens=None), dict(u=None), dict(ws=None), dict(out=None), dict(count=None),
+               dict(S=0), dict(K=0), dict(V=1), dict(T=-1.0), dict(T=nan), dict(T=float("inf")), dict(min_p=1.5),
+               dict(min_p=-0.1), dict(min_p=nan), dict(ws=C.c_void_p(0x10001))):
+        assert call(**kw) == INVALID and lib.rgd_last_error(), kw
