@@ -380,51 +380,48 @@ def _refuse(msg):
     raise RGDError(1, msg)
 
 
-def _on(device, **tensors):
-    """Refuses tensors that are not contiguous tensors of their type and shape on `device`.
-    name=(tensor, dtype name, shape or None, optional)."""
-    for name, (t, dtype, shape, optional) in tensors.items():
-        if t is None:
-            if not optional:
-                _refuse(f"{name} is None")
-            continue
-        if t.device != device or str(t.dtype) != "torch." + dtype:
-            _refuse(f"{name} must be a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
-        if shape is not None and tuple(t.shape) != tuple(shape):
-            _refuse(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
-        if not t.is_contiguous():
-            _refuse(f"{name} must be contiguous")
+def _tensor(device, name, t, dtype, shape):
+    """The address of a contiguous tensor of this type, shape (None: any) and device; anything else is refused."""
+    if t is None:
+        _refuse(f"{name} is None")
+    if t.dtype != dtype or t.device != device:
+        _refuse(f"{name} must be a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    if shape is not None and t.shape != shape:
+        _refuse(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if not t.is_contiguous():
+        _refuse(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _optional(device, name, t, dtype, shape):
+    return None if t is None else _tensor(device, name, t, dtype, shape)
 
 
 def _workspace(device, ws, need):
-    _on(device, workspace=(ws, "uint8", None, False))
+    p = _tensor(device, "workspace", ws, torch.uint8, None)
     if ws.numel() < need:
         _refuse(f"workspace holds {ws.numel()} of {need} bytes")
+    return p
 
 
 def _rows(device, name, t, dtype, shape):
-    """The row stride of a tensor [rows][heads][D] whose rows may lie apart (a slice of a fused projection)."""
-    if t.device != device or t.dtype != dtype or tuple(t.shape) != tuple(shape):
+    """Address and row stride of a tensor [rows][heads][D] whose rows may lie apart (a slice of a fused projection)."""
+    if t.dtype != dtype or t.device != device or t.shape != shape:
         _refuse(f"{name} must be a {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    if t.stride(2) != 1 or (shape[1] > 1 and t.stride(1) != shape[2]):
+    row, head, one = t.stride()
+    if (shape[2] > 1 and one != 1) or (shape[1] > 1 and head != shape[2]):
         _refuse(f"{name}: the heads of a row must be contiguous")
-    return t.stride(0) if shape[0] > 1 else shape[1] * shape[2]
+    return t.data_ptr(), row if shape[0] > 1 else shape[1] * shape[2]
 
 
-class _On:
-    """The device of the operands made current for one call, with its current stream."""
-
-    def __init__(self, device):
-        import torch
-        self.device, self.guard = device, torch.cuda.device(device)
-
-    def __enter__(self):
-        import torch
-        self.guard.__enter__()
-        return C.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
-
-    def __exit__(self, *e):
-        return self.guard.__exit__(*e)
+def _launch(device, fn, *args):
+    """fn(*args, stream) on the operands' device and its current stream."""
+    i = device.index
+    if torch.cuda.current_device() == i:
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+        return
+    with torch.cuda.device(i):
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
 
 
 class PagedCache:
@@ -434,24 +431,24 @@ class PagedCache:
     status [1].  The operators below change the tensors in place."""
 
     def __init__(self, pool_k, pool_v, pages, lens, refs, status):
-        dtypes = {"torch.bfloat16": DTYPE_BF16, "torch.float32": DTYPE_F32}
-        if pool_k.dim() != 5 or str(pool_k.dtype) not in dtypes or not pool_k.is_cuda:
+        types = {torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+        if pool_k.dim() != 5 or pool_k.dtype not in types or not pool_k.is_cuda:
             _refuse("pool_k must be a 5-dimensional bf16 or fp32 tensor on a GPU")
         L, P, H, ps, D = pool_k.shape
         if pages.dim() != 2:
             _refuse("pages must have two dimensions")
         S, width = pages.shape
-        name = str(pool_k.dtype)[len("torch."):]
-        self.device = pool_k.device
-        _on(self.device, pool_k=(pool_k, name, None, False), pool_v=(pool_v, name, (L, P, H, D, ps), False),
-            pages=(pages, "int32", None, False), lens=(lens, "int32", (S,), False),
-            refs=(refs, "int32", (P,), False), status=(status, "int32", (1,), False))
+        dev, i32 = pool_k.device, torch.int32
+        self.desc = PagedCacheDesc(L, P, H, ps, D, types[pool_k.dtype], S, width,
+                                   _tensor(dev, "pool_k", pool_k, pool_k.dtype, None),
+                                   _tensor(dev, "pool_v", pool_v, pool_k.dtype, (L, P, H, D, ps)),
+                                   _tensor(dev, "pages", pages, i32, None), _tensor(dev, "lens", lens, i32, (S,)),
+                                   _tensor(dev, "refs", refs, i32, (P,)), _tensor(dev, "status", status, i32, (1,)))
+        self.ref = C.byref(self.desc)
+        self.device, self.dtype = dev, pool_k.dtype
         self.pool_k, self.pool_v, self.pages, self.lens, self.refs, self.status = pool_k, pool_v, pages, lens, refs, status
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, P, H, ps, D
         self.max_seqs, self.max_pages = S, width
-        self.desc = PagedCacheDesc(L, P, H, ps, D, dtypes["torch." + name], S, width, pool_k.data_ptr(),
-                                   pool_v.data_ptr(), pages.data_ptr(), lens.data_ptr(), refs.data_ptr(),
-                                   status.data_ptr())
 
 
 def _bytes(n):
@@ -461,66 +458,60 @@ def _bytes(n):
 
 
 def paged_workspace_bytes(cache):
-    return _bytes(lib.rgd_paged_workspace_bytes(C.byref(cache.desc)))
+    return _bytes(lib.rgd_paged_workspace_bytes(cache.ref))
 
 
 def paged_select(cache, parent, keep, workspace):
     """Sequence s becomes the first keep[s] positions (None or negative: all) of
     sequence parent[s] (None or outside the cache: itself), all at once."""
-    S = cache.max_seqs
-    _on(cache.device, parent=(parent, "int32", (S,), True), keep=(keep, "int32", (S,), True))
-    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
-    with _On(cache.device) as s:
-        _check(lib.rgd_paged_select(C.byref(cache.desc), _ptr(parent), _ptr(keep), _ptr(workspace), s))
+    dev, shape = cache.device, (cache.max_seqs,)
+    _launch(dev, lib.rgd_paged_select, cache.ref, _optional(dev, "parent", parent, torch.int32, shape),
+            _optional(dev, "keep", keep, torch.int32, shape), _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
 
 def paged_reserve(cache, grow, workspace):
     """Makes room for grow[s] more positions of each sequence and adds them to lens;
     cache.status becomes 1, and nothing else changes, where there is none."""
-    _on(cache.device, grow=(grow, "int32", (cache.max_seqs,), False))
-    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
-    with _On(cache.device) as s:
-        _check(lib.rgd_paged_reserve(C.byref(cache.desc), _ptr(grow), _ptr(workspace), s))
+    dev = cache.device
+    _launch(dev, lib.rgd_paged_reserve, cache.ref, _tensor(dev, "grow", grow, torch.int32, (cache.max_seqs,)),
+            _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
 
 def paged_compact(cache, live, workspace):
     """Moves the live pages to [0, live[0])."""
-    _on(cache.device, live=(live, "int32", (1,), False))
-    _workspace(cache.device, workspace, paged_workspace_bytes(cache))
-    with _On(cache.device) as s:
-        _check(lib.rgd_paged_compact(C.byref(cache.desc), _ptr(live), _ptr(workspace), s))
+    dev = cache.device
+    _launch(dev, lib.rgd_paged_compact, cache.ref, _tensor(dev, "live", live, torch.int32, (1,)),
+            _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
 
 def paged_append(cache, layer, k, v, n, n_new=None):
     """K and V rows [S * n][Hkv][D] (rows may lie apart) of each sequence's last n_new[s]
     (None: n) positions into the pages of one layer."""
-    S, shape = cache.max_seqs, (cache.max_seqs * n, cache.n_kv_heads, cache.head_dim)
-    _on(cache.device, n_new=(n_new, "int32", (S,), True))
-    ldk = _rows(cache.device, "k", k, cache.pool_k.dtype, shape)
-    ldv = _rows(cache.device, "v", v, cache.pool_k.dtype, shape)
-    with _On(cache.device) as s:
-        _check(lib.rgd_paged_append(C.byref(cache.desc), layer, _ptr(k), _ptr(v), ldk, ldv, n, _ptr(n_new), s))
+    dev, S = cache.device, cache.max_seqs
+    shape = (S * n, cache.n_kv_heads, cache.head_dim)
+    pk, ldk = _rows(dev, "k", k, cache.dtype, shape)
+    pv, ldv = _rows(dev, "v", v, cache.dtype, shape)
+    _launch(dev, lib.rgd_paged_append, cache.ref, layer, pk, pv, ldk, ldv, n,
+            _optional(dev, "n_new", n_new, torch.int32, (S,)))
 
 
 def paged_attention_workspace_bytes(cache, n, n_heads):
-    return _bytes(lib.rgd_paged_attention_workspace_bytes(C.byref(cache.desc), n, n_heads))
+    return _bytes(lib.rgd_paged_attention_workspace_bytes(cache.ref, n, n_heads))
 
 
 def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
     """Causal attention of each sequence's last n_new[s] (None: n) positions, q
     [S * n][heads][D] (rows may lie apart), into out [S * n][heads * D] and lse [S * n][heads]."""
-    S, D = cache.max_seqs, cache.head_dim
+    dev, S, D = cache.device, cache.max_seqs, cache.head_dim
     if q.dim() != 3:
         _refuse("q must have three dimensions")
     heads = q.shape[1]
-    ldq = _rows(cache.device, "q", q, cache.pool_k.dtype, (S * n, heads, D))
-    _on(cache.device, n_new=(n_new, "int32", (S,), True),
-        out=(out, str(cache.pool_k.dtype)[len("torch."):], (S * n, heads * D), False),
-        lse=(lse, "float32", (S * n, heads), True))
-    _workspace(cache.device, workspace, paged_attention_workspace_bytes(cache, n, heads))
-    with _On(cache.device) as s:
-        _check(lib.rgd_paged_attention(C.byref(cache.desc), layer, _ptr(q), ldq, n, _ptr(n_new), heads,
-                                       _ptr(workspace), _ptr(out), _ptr(lse), s))
+    pq, ldq = _rows(dev, "q", q, cache.dtype, (S * n, heads, D))
+    _launch(dev, lib.rgd_paged_attention, cache.ref, layer, pq, ldq, n,
+            _optional(dev, "n_new", n_new, torch.int32, (S,)), heads,
+            _workspace(dev, workspace, paged_attention_workspace_bytes(cache, n, heads)),
+            _tensor(dev, "out", out, cache.dtype, (S * n, heads * D)),
+            _optional(dev, "lse", lse, torch.float32, (S * n, heads)))
 
 
 # ------------------------------------------------------- verification of drafts --
@@ -536,13 +527,10 @@ def verify_drafts(target, draft, draft_tokens, n_draft, T, min_p, u, workspace, 
     logits [S][K+1][V], the drafts' logits [S][K][V] (None: certain drafts) and uniforms u [S][K+1]."""
     if target.dim() != 3 or not target.is_cuda:
         _refuse("target must be a 3-dimensional tensor on a GPU")
-    S, K, V = target.shape[0], target.shape[1] - 1, target.shape[2]
-    dev = target.device
-    _on(dev, target=(target, "float32", None, False), draft=(draft, "float32", (S, K, V), True),
-        draft_tokens=(draft_tokens, "int32", (S, K), False), n_draft=(n_draft, "int32", (S,), True),
-        u=(u, "float32", (S, K + 1), False), out=(out, "int32", (S, K + 1), False),
-        n_accepted=(n_accepted, "int32", (S,), False))
-    _workspace(dev, workspace, verify_workspace_bytes(S, K, V))
-    with _On(dev) as s:
-        _check(lib.rgd_verify_drafts(_ptr(target), _ptr(draft), _ptr(draft_tokens), _ptr(n_draft), S, K, V, T, min_p,
-                                     _ptr(u), _ptr(workspace), _ptr(out), _ptr(n_accepted), s))
+    S, K1, V = target.shape
+    K, dev, f32, i32 = K1 - 1, target.device, torch.float32, torch.int32
+    _launch(dev, lib.rgd_verify_drafts, _tensor(dev, "target", target, f32, None),
+            _optional(dev, "draft", draft, f32, (S, K, V)), _tensor(dev, "draft_tokens", draft_tokens, i32, (S, K)),
+            _optional(dev, "n_draft", n_draft, i32, (S,)), S, K, V, T, min_p, _tensor(dev, "u", u, f32, (S, K1)),
+            _workspace(dev, workspace, verify_workspace_bytes(S, K, V)), _tensor(dev, "out", out, i32, (S, K1)),
+            _tensor(dev, "n_accepted", n_accepted, i32, (S,)))
