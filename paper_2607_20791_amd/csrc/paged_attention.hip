@@ -7,13 +7,14 @@
 // go through MFMA, 16 query vectors to a tile, because the tile's unused
 // columns cost less than the reads they wait for.
 //
-// A wave is the unit of work, without LDS or barriers.  The positions of all
-// (sequence, KV head, query tile) items lie one behind the other in steps of
-// 32, and every wave takes an equal run of steps, over the borders of items: short and
-// long sequences fill the chip alike, whatever their order.  The waves work the
-// runs out of the lengths on the device.  An item inside one run is finished by
-// its wave; the pieces of one that is cut go to the workspace and a second kernel
-// joins them by their maxima and sums, in order.
+// The positions of all (sequence, KV head, query tile) items lie one behind the
+// other in steps of 32, and every workgroup takes an equal run of steps, over the
+// borders of items: short and long sequences fill the chip alike, whatever their
+// order.  The workgroups work the runs out of the lengths on the device.  Inside a
+// run the four waves take an item's steps in turn, each with a maximum and sum of its
+// own, and meet in LDS at the item's end.  An item inside one run is finished there;
+// the pieces of one that is cut go to the workspace and a second kernel joins them
+// by their maxima and sums, in order.
 //
 // Scores are computed transposed, S^T = K Q^T.  bf16: the K rows of a step are
 // gathered so that a lane ends up with eight consecutive positions of one query
@@ -33,9 +34,11 @@ namespace rgd {
 
 namespace {
 
-constexpr int kStep = 32;       // positions per step of the plan
-constexpr int kMinSteps = 4;    // a wave's run is no shorter
-constexpr int kMaxWaves = 2048; // 8 per CU
+constexpr int kStep = 32;      // positions per step of the plan
+constexpr int kMinSteps = 4;   // a run is no shorter: one step a wave
+constexpr int kItemCost = 8;   // what an item costs besides its steps, in steps
+constexpr int kMaxRuns = 512;  // two workgroups per CU
+constexpr int kWaves = 4;      // per workgroup
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;       // the running maximum moves when a score passes it by this (log2 units)
@@ -62,57 +65,80 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
   return q;
 }
 
-// Steps are counted in doubles (whole numbers far below 2^53).
-RGD_DEV double wave_scan(double v) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double t = __shfl_up(v, o, 64);
-    if (lane >= o) v += t;
-  }
-  return v;
+// Sum over the lanes up to this one (64-bit: long tables times many sequences).
+template <int CTRL, int ROWS>
+RGD_DEV long long scan_step(long long v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return v + (((long long)hi << 32) | (unsigned)lo);
+}
+RGD_DEV long long wave_scan(long long v) {
+  v = scan_step<0x111, 0xf>(v);  // row_shr:1
+  v = scan_step<0x112, 0xf>(v);
+  v = scan_step<0x114, 0xf>(v);
+  v = scan_step<0x118, 0xf>(v);
+  v = scan_step<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+  return scan_step<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+}
+RGD_DEV long long lane_value(long long v, int lane) {
+  const int lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+  return ((long long)hi << 32) | (unsigned)lo;
 }
 
 template <int COLS>
-RGD_DEV double units_of(const PagedAttnArgs& a, int s) {
-  if (s >= a.c.S) return 0.0;
+RGD_DEV long long steps_of(const PagedAttnArgs& a, int s) {
+  if (s >= a.c.S) return 0;
   const Seq q = seq_of<COLS>(a, s);
-  return (double)q.steps * (double)q.items;
+  return (long long)(q.steps + kItemCost) * q.items;
 }
 
-// The steps of all sequences and of those before sequence `upto`.
+// Floor of x / y for 0 <= x < 2^52, 0 < y (exact: the quotients here are below
+// 2^31, so a fraction is at least 2^-31 of the divisor away from a whole number).
+RGD_DEV long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
+
+// The runs.  Workspace: [0] steps per run, then the steps before each sequence
+// [S], for the joining kernel; behind them the pieces.
+struct Runs {
+  long long total, length;
+};
+constexpr int kHead = 1;
+__host__ __device__ inline size_t plan_floats(int S) { return ((size_t)(kHead + S) * 2 + 63) / 64 * 64; }
+
+// Finds the run of workgroup r (of `runs`): the sequence it starts in and the
+// steps before that one.  False: there is none.
 template <int COLS>
-RGD_DEV double count_units(const PagedAttnArgs& a, int upto, double& before) {
+RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& s, long long& before) {
   const int lane = threadIdx.x & 63;
-  double total = 0.0;
-  before = 0.0;
-  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
-    const double u = units_of<COLS>(a, s0 + lane), incl = wave_scan(u);
-    if (upto >= s0 && upto < s0 + 64) before = total + __shfl(incl - u, upto - s0, 64);
-    total += __shfl(incl, 63, 64);
+  long long u = steps_of<COLS>(a, lane), incl = wave_scan(u);
+  plan.total = lane_value(incl, 63);
+  for (int s0 = 64; s0 < a.c.S; s0 += 64) plan.total += lane_value(wave_scan(steps_of<COLS>(a, s0 + lane)), 63);
+  plan.length = max((long long)kMinSteps, quotient(plan.total + runs - 1, runs));
+  const long long start = r * plan.length;
+  if (r == 0 && threadIdx.x < 64) {
+    long long* head = (long long*)a.ws;
+    if (lane == 0) head[0] = plan.length;
+    long long base = 0;
+    for (int s0 = 0; s0 < a.c.S; s0 += 64) {
+      const long long v = s0 ? steps_of<COLS>(a, s0 + lane) : u, in = s0 ? wave_scan(v) : incl;
+      if (s0 + lane < a.c.S) head[kHead + s0 + lane] = base + in - v;
+      base += lane_value(in, 63);
+    }
   }
-  return total;
-}
-
-// Steps per wave.
-RGD_DEV double run_length(double total, int waves) { return fmax((double)kMinSteps, ceil(total / (double)waves)); }
-
-// The sequence that holds step `at` and the steps before it.
-template <int COLS>
-RGD_DEV int find_seq(const PagedAttnArgs& a, double at, double& before) {
-  const int lane = threadIdx.x & 63;
-  double base = 0.0;
-  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
-    const double u = units_of<COLS>(a, s0 + lane), incl = wave_scan(u);
-    const unsigned long long hit = __ballot(base + incl > at);
+  if (start >= plan.total) return false;
+  long long base = 0;
+  for (int s0 = 0;;) {
+    const unsigned long long hit = __ballot(base + incl > start);
     if (hit) {
       const int l = __builtin_ctzll(hit);
-      before = base + __shfl(incl - u, l, 64);
-      return s0 + l;
+      before = base + lane_value(incl - u, l);
+      s = s0 + l;
+      return true;
     }
-    base += __shfl(incl, 63, 64);
+    base += lane_value(incl, 63);
+    s0 += 64;
+    u = steps_of<COLS>(a, s0 + lane);
+    incl = wave_scan(u);
   }
-  return -1;
 }
 
 RGD_DEV f32x4 mfma_bf16(const u32x4& x, const u32x4& y, f32x4 c) {
@@ -143,36 +169,74 @@ RGD_DEV bool any_nonfinite(u32x4 v) {
   return bad;
 }
 
-// Walks a sequence's table 16 positions at a time, two times 64 entries in registers.
+// Looks up a sequence's table by 16-position blocks in rising order, two times 64
+// entries in registers.
 struct TableWalk {
   const int* row;
   int width, bpp;  // 16-position blocks per page
-  int j, sub, jb, cur, nxt, lane;
+  unsigned long long inv;
+  int jb, cur, nxt, lane;
+  RGD_DEV int page_index(int block) const { return (int)(((unsigned long long)block * inv) >> 36); }
   RGD_DEV void start(const PagedView& c, int s, int block) {
     row = c.pages + (size_t)s * c.width;
     width = c.width;
     bpp = c.ps >> 4;
+    inv = ((1ull << 36) + bpp - 1) / bpp;  // blocks are below 2^26, bpp at most 2^8: exact
     lane = threadIdx.x & 63;
-    j = block / bpp;
-    sub = block - j * bpp;
-    jb = j;
+    jb = page_index(block);
     cur = row[min(jb + lane, width - 1)];
     nxt = row[min(jb + 64 + lane, width - 1)];
   }
-  // the page of the next block (any value behind the table) and the block's place in it
-  RGD_DEV int next(int& place) {
-    if (j - jb >= 64) {
+  // the page of a block (behind the table: any value) and the block's place in it
+  RGD_DEV int find(int block, int& place) {
+    const int j = page_index(block);
+    place = block - j * bpp;
+    while (j - jb >= 64) {
       cur = nxt;
       jb += 64;
       nxt = row[min(jb + 64 + lane, width - 1)];
     }
-    const int p = __builtin_amdgcn_readlane(cur, j - jb);
-    place = sub;
-    if (++sub == bpp) {
-      sub = 0;
-      ++j;
+    return __builtin_amdgcn_readlane(cur, j - jb);
+  }
+};
+
+// One item of a run: steps [t0, t1) of query tile qb of KV head g of sequence s.
+struct Item {
+  Seq sq;
+  int s, g, qb, t0, t1;
+  bool valid;
+  RGD_DEV int end() const { return min(t1 * kStep, max(sq.len, 1)); }
+  RGD_DEV int begin(int wave, int per) const { return t0 * kStep + wave * per; }
+};
+
+RGD_DEV Seq uniform(const Seq& q) { return Seq{uniform(q.len), uniform(q.m), uniform(q.steps), uniform(q.items)}; }
+
+// The items of a run, one after the other.
+template <int COLS>
+struct Walk {
+  Seq sq;
+  int s, item, u0, left;
+  RGD_DEV Item next(const PagedAttnArgs& a) {
+    Item it{};
+    if (left <= 0) return it;
+    if (item == sq.items) {  // steps are left, so a sequence with new tokens follows
+      item = 0;
+      do sq = uniform(seq_of<COLS>(a, ++s));
+      while (sq.items == 0);
     }
-    return p;
+    // an item's first kItemCost units of the plan are its fixed cost, in front of its steps
+    const int u1 = min(sq.steps + kItemCost, u0 + left), tiles = sq.items / a.c.Hkv;
+    it.sq = sq;
+    it.s = s;
+    it.g = item / tiles;
+    it.qb = item - it.g * tiles;
+    it.t0 = max(0, u0 - kItemCost);
+    it.t1 = u1 - kItemCost;
+    it.valid = it.t1 > it.t0;  // else the next run has the item's first step
+    left -= u1 - u0;
+    u0 = 0;
+    ++item;
+    return it;
   }
 };
 
@@ -195,12 +259,12 @@ struct Piece {
   int ok;                       // bit b: block b is a page of the pool
   int lane, row, grp;
 
-  RGD_DEV void load_k(const PagedAttnArgs& a, int g) {
+  RGD_DEV void load_k(const PagedAttnArgs& a, int g, int p0) {
     ok = 0;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       int place;
-      int p = walk.next(place);
+      int p = walk.find((p0 >> 4) + b, place);
       if (page_ok(a.c, p)) ok |= 1 << b;
       else p = 0;
       const size_t head = ((size_t)p * a.c.Hkv + g) * a.c.ps * D;
@@ -263,101 +327,141 @@ struct Piece {
     }
   }
 
-  // Steps [t0, t1) of one item.
-  RGD_DEV void run(const PagedAttnArgs& a, const Seq& sq, int s, int g, int qb, int t0, int t1) {
-    lane = threadIdx.x & 63;
-    row = lane & 15;
-    grp = lane >> 4;
-    const int G = a.Hq / a.c.Hkv, cols = sq.m * G;
-    walk.start(a.c, s, t0 * 2);
-    // the tile's queries; columns behind the last one repeat it
-    int lim[NT], least = 0x7FFFFFFF;
+  // Weights of tile t's scores (log2 units) against its running maximum, which moves
+  // with them; hi + lo: the weights in two bf16.
+  RGD_DEV void weights(int t, const float (&x)[E], float (&p)[E], u32x4& hi, u32x4& lo) {
+    float top = x[0];
+#pragma unroll
+    for (int j = 1; j < E; ++j) top = fmaxf(top, x[j]);
+    if (__any(top > m[t] + kLazy)) {
+      top = fmaxf(top, __shfl_xor(top, 16, 64));
+      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float nm = fmaxf(m[t], top), down = exp2_raw(m[t] - nm);
+      m[t] = nm;
+      l[t] *= down;
+#pragma unroll
+      for (int d = 0; d < VL; ++d) o[t][d] *= down;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      p[j] = exp2_raw(x[j] - m[t]);
+      sum += p[j];
+    }
+    l[t] += sum;
+    if constexpr (BF) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        hi[j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
+        lo[j] = pack_bf16x2(p[2 * j] - __uint_as_float(hi[j] << 16),
+                            p[2 * j + 1] - __uint_as_float(hi[j] & 0xFFFF0000u));
+      }
+    }
+  }
+
+  static constexpr int PER = 16 * NB, STRIDE = kWaves * PER;  // a round's positions, the way to the wave's next round
+
+  RGD_DEV void load_q(const PagedAttnArgs& a, const Item& it) {
+    const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const int col = min(qb * COLS + t * 16 + row, cols - 1), i = col / G;
-      lim[t] = sq.len - sq.m + i + 1;
-      const T* src = (const T*)a.q + ((size_t)s * a.n + i) * a.ldq + (size_t)(g * G + col - i * G) * D;
+      const int col = min(it.qb * COLS + t * 16 + row, cols - 1), i = col / G;  // columns behind the last one repeat it
+      const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
       for (int c = 0; c < KL; ++c) q[t][c] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
+    }
+  }
+
+  RGD_DEV void start(const PagedAttnArgs& a, const Item& it, const TableWalk& w, int wave) {
+    const int p0 = it.begin(wave, PER);
+    if (!it.valid || p0 >= it.end()) return;
+    walk = w;
+    load_q(a, it);
+    load_k(a, it.g, p0);
+    load_v(a);
+  }
+
+  // The wave's share of an item's steps, whose queries and first K and V are on their
+  // way; leaves those of the next item on theirs (walk_next: its table's first entries).
+  RGD_DEV void run(const PagedAttnArgs& a, const Item& it, const Item& next, const TableWalk& walk_next, int wave) {
+    const Seq& sq = it.sq;
+    const int G = a.Hq / a.c.Hkv, cols = sq.m * G, qb = it.qb, g = it.g;
+    int lim[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      lim[t] = sq.len - sq.m + min(qb * COLS + t * 16 + row, cols - 1) / G + 1;
       m[t] = kNoRef;
       l[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < VL; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int first = (qb * COLS) / G;  // the tile's first token: all its columns see that much
-    least = sq.len - sq.m + first + 1;
+    const int least = sq.len - sq.m + (qb * COLS) / G + 1;  // all of the tile's tokens see that much
     const float scale = kLog2e / sqrtf((float)D);
-    constexpr int PER = 16 * NB;
-    const int p1 = min(t1 * kStep, max(sq.len, 1));
-    int p0 = t0 * kStep;
-    load_k(a, g);
-    load_v(a);
-    for (; p0 < p1; p0 += PER) {
+    const int p1 = it.end();
+    int p0 = it.begin(wave, PER);
+    if (p0 >= p1) {
+      start(a, next, walk_next, wave);
+      return;
+    }
+    constexpr int ALL = (1 << NB) - 1;
+    while (p0 < p1) {
+      while (ok == ALL && p0 + PER <= least && p0 + STRIDE < p1) {  // every column sees it all, and another round follows
+        f32x4 s4[NT][NB];
+        scores(s4);
+        load_k(a, g, p0 + STRIDE);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          float x[E], p[E];
+#pragma unroll
+          for (int j = 0; j < E; ++j) x[j] = s4[t][j / 4][j % 4] * scale;
+          u32x4 hi, lo;
+          weights(t, x, p, hi, lo);
+#pragma unroll
+          for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p, hi, lo, o[t][d]);
+        }
+        load_v(a);
+        p0 += STRIDE;
+      }
       const int here = ok;
       f32x4 s4[NT][NB];
       scores(s4);
-      const bool more = p0 + PER < p1;
-      if (more) load_k(a, g);
-      const bool whole = p0 + PER <= least && here == (1 << NB) - 1;
+      const bool more = p0 + STRIDE < p1;
+      const int first = next.begin(wave, PER);
+      const bool on = !more && next.valid && first < next.end();
+      if (more) {
+        load_k(a, g, p0 + STRIDE);
+      } else if (on) {
+        walk = walk_next;
+        load_q(a, next);
+        load_k(a, next.g, first);
+      }
       const int pos = p0 + grp * E;  // of this lane's first score
       const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
-      bool mixed = false;  // a position that some of the tile's tokens see and others do not is not finite
-      if (!whole) {
-        const int held = there ? sq.len - pos : 0;
-        bool odd = false;
+      bool odd = false;
+      const int held = there ? sq.len - pos : 0;
 #pragma unroll
-        for (int d = 0; d < VL; ++d) {
-          v[d] = keep_first<T>(v[d], held);
-          odd = odd || any_nonfinite<T>(v[d]);
-        }
-        mixed = __any(odd);
+      for (int d = 0; d < VL; ++d) {
+        v[d] = keep_first<T>(v[d], held);
+        odd = odd || any_nonfinite<T>(v[d]);
       }
+      // 0 times a value that is not finite is not 0: where some tokens see such a
+      // value and others do not, each token's columns take the product with what it sees
+      const bool mixed = __any(odd);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
-        float x[E];
+        const int seen = there ? lim[t] - pos : 0;
+        float x[E], p[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) x[j] = s4[t][j / 4][j % 4] * scale;
-        if (!whole) {
-          const int seen = there ? lim[t] - pos : 0;
-#pragma unroll
-          for (int j = 0; j < E; ++j) x[j] = j < seen ? x[j] : -INFINITY;
-        }
-        float top = x[0];
-#pragma unroll
-        for (int j = 1; j < E; ++j) top = fmaxf(top, x[j]);
-        if (__any(top > m[t] + kLazy)) {
-          top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float nm = fmaxf(m[t], top), down = exp2_raw(m[t] - nm);
-          m[t] = nm;
-          l[t] *= down;
-#pragma unroll
-          for (int d = 0; d < VL; ++d) o[t][d] *= down;
-        }
-        float p[E];
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < E; ++j) {
-          p[j] = exp2_raw(x[j] - m[t]);
-          sum += p[j];
-        }
-        l[t] += sum;
-        u32x4 hi{}, lo{};
-        if constexpr (BF) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            hi[j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
-            lo[j] = pack_bf16x2(p[2 * j] - __uint_as_float(hi[j] << 16),
-                                p[2 * j + 1] - __uint_as_float(hi[j] & 0xFFFF0000u));
-          }
-        }
+        for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] * scale : -INFINITY;
+        u32x4 hi, lo;
+        weights(t, x, p, hi, lo);
         if (!mixed) {
 #pragma unroll
           for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p, hi, lo, o[t][d]);
         } else {
-          // 0 times such a value is not 0: each token's columns take the product with what it sees
-          const int c0 = qb * COLS + t * 16, c1 = min(c0 + 16, cols) - 1;
-          for (int i = min(c0, cols - 1) / G; i <= max(c1, 0) / G; ++i) {
+          const int c0 = min(qb * COLS + t * 16, cols - 1), c1 = min(qb * COLS + t * 16 + 15, cols - 1);
+#pragma unroll 1
+          for (int i = c0 / G; i <= c1 / G; ++i) {
             const int see = sq.len - sq.m + i + 1;
             const int n = there ? see - pos : 0;
 #pragma unroll
@@ -368,7 +472,8 @@ struct Piece {
           }
         }
       }
-      if (more) load_v(a);
+      if (more || on) load_v(a);
+      p0 += STRIDE;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -386,7 +491,7 @@ RGD_DEV void store_row4(T* p, f32x4 v) {
   else *(f32x4*)p = v;
 }
 
-// Pieces: slot 2 w + 1 holds the start of the item that wave w's run ends in, slot 2 w the
+// Pieces: slot 2 r + 1 holds the start of the item that run r ends in, slot 2 r the
 // part of an item that an earlier run began.  Per slot [COLS][D] weighted sums,
 // then [COLS] (maximum, sum).
 template <int D, int NT>
@@ -395,81 +500,94 @@ constexpr size_t slot_floats() {
 }
 
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int waves) {
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
   using P = Piece<T, D, NT>;
-  constexpr int COLS = P::COLS;
-  const int w = uniform(blockIdx.x * 4 + (threadIdx.x >> 6));
-  if (w >= waves) return;
+  constexpr int COLS = P::COLS, LD = D + 4;
+  __shared__ float part[kWaves][COLS][LD];
+  __shared__ float2 ml[kWaves][COLS];
+  const int r = blockIdx.x, wave = uniform(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
-  double unused;
-  const double total = count_units<COLS>(a, -1, unused);
-  const double run = run_length(total, waves), start = (double)w * run;
-  if (start >= total) return;
-  double before = 0.0;
-  int s = uniform(find_seq<COLS>(a, start, before));
-  long long left = (long long)fmin(run, total - start);
-  Seq sq = seq_of<COLS>(a, s);
-  sq = Seq{uniform(sq.len), uniform(sq.m), uniform(sq.steps), uniform(sq.items)};
-  const double inside = start - before;
-  int item = uniform((int)(inside / (double)sq.steps));
-  int t0 = uniform((int)(inside - (double)item * (double)sq.steps));
+  Runs plan;
+  int s;
+  long long before;
+  if (!find_run<COLS>(a, r, runs, plan, s, before)) return;
+  const long long start = r * plan.length;
+  Walk<COLS> walk;
+  walk.s = uniform(s);
+  walk.left = uniform((int)min(plan.length, plan.total - start));
+  walk.sq = uniform(seq_of<COLS>(a, walk.s));
+  walk.item = uniform((int)quotient(start - before, walk.sq.steps + kItemCost));
+  walk.u0 = uniform((int)(start - before - (long long)walk.item * (walk.sq.steps + kItemCost)));
   const int G = a.Hq / a.c.Hkv;
-  while (left > 0) {
-    const int t1 = (int)min((long long)sq.steps, t0 + left), tiles = sq.items / a.c.Hkv;
-    const int g = item / tiles, qb = item - g * tiles;
-    P x;
-    x.run(a, sq, s, g, qb, t0, t1);
+  P x;
+  x.lane = lane;
+  x.row = row;
+  x.grp = grp;
+  Item it = walk.next(a);
+  TableWalk table;
+  table.start(a.c, it.s, it.begin(wave, P::PER) >> 4);
+  x.start(a, it, table, wave);
+  while (it.valid) {
+    const Item next = walk.next(a);
+    if (next.valid) table.start(a.c, next.s, next.begin(wave, P::PER) >> 4);
+    x.run(a, it, next, table, wave);
+    const Seq& sq = it.sq;
+    const int g = it.g, qb = it.qb, t0 = it.t0, t1 = it.t1, cols = min(COLS, sq.m * G - qb * COLS);
+    s = it.s;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+      if (t * 16 + row < cols) {
+#pragma unroll
+        for (int d = 0; d < P::VL; ++d) *(f32x4*)&part[wave][t * 16 + row][d * 16 + grp * 4] = x.o[t][d];
+        if (grp == 0) ml[wave][t * 16 + row] = float2{x.m[t], x.l[t]};
+      }
+    __syncthreads();
     const bool done = t0 == 0 && t1 == sq.steps;
+    float* slot = a.ws + plan_floats(a.c.S) + (size_t)(2 * r + (t0 == 0)) * slot_floats<D, NT>();
+    for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
+      const int c = i / (D / 4), d = i % (D / 4) * 4, col = qb * COLS + c;
+      float top = ml[0][c].x, sum = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int col = qb * COLS + t * 16 + row;
-      if (col >= sq.m * G) continue;
+      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[w][c].x);
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float f = exp2_raw(ml[w][c].x - top);
+        sum += f * ml[w][c].y;
+        o += f * *(const f32x4*)&part[w][c][d];
+      }
       if (done) {
-        const size_t r = (size_t)s * a.n + col / G;
+        const size_t row_out = (size_t)s * a.n + col / G;
         const int h = g * G + col % G;
-        const float inv = x.l[t] == 0.f ? 0.f : 1.f / x.l[t];
-        T* out = (T*)a.out + (r * a.Hq + h) * D + grp * 4;
-#pragma unroll
-        for (int d = 0; d < P::VL; ++d) store_row4(out + d * 16, x.o[t][d] * inv);
-        if (a.lse && grp == 0) a.lse[r * a.Hq + h] = lse_of(x.m[t], x.l[t]);
+        store_row4((T*)a.out + (row_out * a.Hq + h) * D + d, o * (sum == 0.f ? 0.f : 1.f / sum));
+        if (a.lse && d == 0) a.lse[row_out * a.Hq + h] = lse_of(top, sum);
       } else {
-        float* slot = a.ws + (size_t)(2 * w + (t0 == 0)) * slot_floats<D, NT>();
-        const int c = t * 16 + row;
-#pragma unroll
-        for (int d = 0; d < P::VL; ++d) *(f32x4*)(slot + c * D + d * 16 + grp * 4) = x.o[t][d];
-        if (grp == 0) *(float2*)(slot + COLS * D + 2 * c) = float2{x.m[t], x.l[t]};
+        *(f32x4*)(slot + c * D + d) = o;
+        if (d == 0) *(float2*)(slot + COLS * D + 2 * c) = float2{top, sum};
       }
     }
-    left -= t1 - t0;
-    t0 = 0;
-    if (left > 0 && ++item == sq.items) {
-      item = 0;
-      do {
-        ++s;
-        sq = seq_of<COLS>(a, s);  // steps are left, so a sequence with new tokens follows
-        sq = Seq{uniform(sq.len), uniform(sq.m), uniform(sq.steps), uniform(sq.items)};
-      } while (sq.items == 0);
-    }
+    it = next;
+    __syncthreads();
   }
 }
 
 // The outputs of the items that several runs share: one workgroup per (row,
 // query head); each group of D threads sums every (256 / D)-th piece.
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int waves) {
+__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a) {
   constexpr int COLS = 16 * NT, PARTS = 256 / D;
   __shared__ float acc_s[256], top_s[4], sum_s[256];
   const int r = blockIdx.x, h = blockIdx.y, s = r / a.n, i = r - s * a.n;
+  const long long* head = (const long long*)a.ws;
+  const long long length = head[0], before = head[kHead + s];
   const Seq sq = seq_of<COLS>(a, s);
   if (i >= sq.m) return;
   const int G = a.Hq / a.c.Hkv, g = h / G, col = i * G + h - g * G, qb = col / COLS, c = col - qb * COLS;
-  double before;
-  const double total = count_units<COLS>(a, s, before);
-  const double run = run_length(total, waves);
-  const double from = before + (double)(g * (sq.items / a.c.Hkv) + qb) * (double)sq.steps;
-  const int w0 = (int)(from / run), w1 = (int)((from + (double)sq.steps - 1.0) / run);
+  const long long from = before + (long long)(g * (sq.items / a.c.Hkv) + qb) * (sq.steps + kItemCost) + kItemCost;
+  const int w0 = (int)quotient(from, length), w1 = (int)quotient(from + sq.steps - 1, length);
   if (w0 == w1) return;
-  auto slot = [&](int w) { return a.ws + (size_t)(2 * w + (w == w0)) * slot_floats<D, NT>(); };
+  const float* slots = a.ws + plan_floats(a.c.S);
+  auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == w0)) * slot_floats<D, NT>(); };
   const int t = threadIdx.x;
   float top = kNoRef;
   for (int w = w0 + t; w <= w1; w += 256) top = fmaxf(top, slot(w)[COLS * D + 2 * c]);
@@ -499,19 +617,19 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int wav
 // Query tiles a wave holds at once: all of a sequence's query vectors up to 64.
 int tiles_for(int vectors) { return vectors <= 16 ? 1 : vectors <= 32 ? 2 : 4; }
 
-int waves_for(const PagedView& c, int n, int Hq) {
+int runs_for(const PagedView& c, int n, int Hq) {
   const int cols = 16 * tiles_for(n * (Hq / c.Hkv));
   const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
-  return (int)std::min((double)kMaxWaves, std::ceil(steps / kMinSteps));
+  return (int)std::min((double)kMaxRuns, std::ceil((steps + kItemCost * items) / kMinSteps));
 }
 
 template <typename T, int D, int NT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
-  const int waves = waves_for(a.c, a.n, a.Hq);
-  hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3((waves + 3) / 4), dim3(256), 0, s, a, waves);
+  const int runs = runs_for(a.c, a.n, a.Hq);
+  hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(a.c.S * a.n, a.Hq), dim3(256), 0, s, a, waves);
+  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(a.c.S * a.n, a.Hq), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
@@ -537,7 +655,7 @@ hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
 
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(n * (Hq / c.Hkv));
-  return (size_t)2 * waves_for(c, n, Hq) * 16 * nt * (c.D + 2);
+  return plan_floats(c.S) + (size_t)2 * runs_for(c, n, Hq) * 16 * nt * (c.D + 2);
 }
 
 hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s) {
