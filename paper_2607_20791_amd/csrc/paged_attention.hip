@@ -96,13 +96,9 @@ RGD_DEV long long steps_of(const PagedAttnArgs& a, int s) {
 // 2^31, so a fraction is at least 2^-31 of the divisor away from a whole number).
 RGD_DEV long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
 
-// The runs.  Workspace: [0] steps per run, then the steps before each sequence
-// [S], for the joining kernel; behind them the pieces.
 struct Runs {
-  long long total, length;
+  long long total, length;  // units of the plan, units per run
 };
-constexpr int kHead = 1;
-__host__ __device__ inline size_t plan_floats(int S) { return ((size_t)(kHead + S) * 2 + 63) / 64 * 64; }
 
 // Finds the run of workgroup r (of `runs`): the sequence it starts in and the
 // steps before that one.  False: there is none.
@@ -114,16 +110,6 @@ RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& 
   for (int s0 = 64; s0 < a.c.S; s0 += 64) plan.total += lane_value(wave_scan(steps_of<COLS>(a, s0 + lane)), 63);
   plan.length = max((long long)kMinSteps, quotient(plan.total + runs - 1, runs));
   const long long start = r * plan.length;
-  if (r == 0 && threadIdx.x < 64) {
-    long long* head = (long long*)a.ws;
-    if (lane == 0) head[0] = plan.length;
-    long long base = 0;
-    for (int s0 = 0; s0 < a.c.S; s0 += 64) {
-      const long long v = s0 ? steps_of<COLS>(a, s0 + lane) : u, in = s0 ? wave_scan(v) : incl;
-      if (s0 + lane < a.c.S) head[kHead + s0 + lane] = base + in - v;
-      base += lane_value(in, 63);
-    }
-  }
   if (start >= plan.total) return false;
   long long base = 0;
   for (int s0 = 0;;) {
@@ -205,6 +191,7 @@ struct Item {
   Seq sq;
   int s, g, qb, t0, t1;
   bool valid;
+  long long at;  // its first unit in the plan
   RGD_DEV int end() const { return min(t1 * kStep, max(sq.len, 1)); }
   RGD_DEV int begin(int wave, int per) const { return t0 * kStep + wave * per; }
 };
@@ -216,6 +203,7 @@ template <int COLS>
 struct Walk {
   Seq sq;
   int s, item, u0, left;
+  long long at;
   RGD_DEV Item next(const PagedAttnArgs& a) {
     Item it{};
     if (left <= 0) return it;
@@ -233,6 +221,8 @@ struct Walk {
     it.t0 = max(0, u0 - kItemCost);
     it.t1 = u1 - kItemCost;
     it.valid = it.t1 > it.t0;  // else the next run has the item's first step
+    it.at = at;
+    at += sq.steps + kItemCost;
     left -= u1 - u0;
     u0 = 0;
     ++item;
@@ -250,7 +240,10 @@ struct Piece {
   static constexpr int E = BF ? 8 : 4;              // consecutive positions of a lane
   static constexpr int COLS = 16 * NT;
 
-  u32x4 q[NT][KL], k[NB][KL], v[VL];
+  // four tiles: the queries stay in LDS, shared by the waves
+  static constexpr bool QS = NT == 4;
+  u32x4 q[QS ? 1 : NT][KL], k[NB][KL], v[VL];
+  const u32x4* qs;
   f32x4 o[NT][VL];
   float m[NT], l[NT];  // per column; l: this lane's part
 
@@ -305,10 +298,11 @@ struct Piece {
 #pragma unroll
         for (int c = 0; c < KL; ++c) {
           if constexpr (BF) {
-            x = mfma_bf16(k[e][c], q[t][c], x);
+            x = mfma_bf16(k[e][c], q_at(t, c), x);
           } else {
+            const u32x4 qc = q_at(t, c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x = mfma_f32(__uint_as_float(k[e][c][j]), __uint_as_float(q[t][c][j]), x);
+            for (int j = 0; j < 4; ++j) x = mfma_f32(__uint_as_float(k[e][c][j]), __uint_as_float(qc[j]), x);
           }
         }
         s[t][e] = x;
@@ -361,10 +355,25 @@ struct Piece {
 
   static constexpr int PER = 16 * NB, STRIDE = kWaves * PER;  // a round's positions, the way to the wave's next round
 
+  RGD_DEV u32x4 q_at(int t, int c) const {
+    if constexpr (QS) return qs[(t * KL + c) * 64 + lane];
+    else return q[t][c];
+  }
+
+  // all waves, between two barriers
+  RGD_DEV void stage_q(const PagedAttnArgs& a, const Item& it, u32x4* dst, int wave) const {
+    const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
+    const int col = min(it.qb * COLS + wave * 16 + row, cols - 1), i = col / G;
+    const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
+#pragma unroll
+    for (int c = 0; c < KL; ++c) dst[(wave * KL + c) * 64 + lane] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
+  }
+
   RGD_DEV void load_q(const PagedAttnArgs& a, const Item& it) {
+    if (QS) return;
     const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+    for (int t = 0; t < (QS ? 0 : NT); ++t) {
       const int col = min(it.qb * COLS + t * 16 + row, cols - 1), i = col / G;  // columns behind the last one repeat it
       const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
@@ -491,9 +500,13 @@ RGD_DEV void store_row4(T* p, f32x4 v) {
   else *(f32x4*)p = v;
 }
 
-// Pieces: slot 2 r + 1 holds the start of the item that run r ends in, slot 2 r the
-// part of an item that an earlier run began.  Per slot [COLS][D] weighted sums,
-// then [COLS] (maximum, sum).
+// Workspace: per run a Cut, then the pieces: slot 2 r + 1 holds the start of the item
+// that run r ends in, slot 2 r the part of an item that an earlier run began.  Per slot
+// [COLS][D] weighted sums, then [COLS] (maximum, sum).
+struct Cut {
+  int s, g, qb, last;  // the item that starts in this run and goes on to run `last`; s = -1: none
+};
+__host__ __device__ constexpr size_t cut_floats(int runs) { return ((size_t)runs * 4 + 63) / 64 * 64; }
 template <int D, int NT>
 constexpr size_t slot_floats() {
   return (size_t)16 * NT * (D + 2);
@@ -505,11 +518,14 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
   constexpr int COLS = P::COLS, LD = D + 4;
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
+  __shared__ u32x4 q_s[P::QS ? NT * P::KL * 64 : 1];
   const int r = blockIdx.x, wave = uniform(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
   Runs plan;
   int s;
   long long before;
+  Cut* cut = (Cut*)a.ws + r;
+  if (threadIdx.x == 0) *cut = Cut{-1, 0, 0, 0};
   if (!find_run<COLS>(a, r, runs, plan, s, before)) return;
   const long long start = r * plan.length;
   Walk<COLS> walk;
@@ -517,17 +533,23 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
   walk.left = uniform((int)min(plan.length, plan.total - start));
   walk.sq = uniform(seq_of<COLS>(a, walk.s));
   walk.item = uniform((int)quotient(start - before, walk.sq.steps + kItemCost));
-  walk.u0 = uniform((int)(start - before - (long long)walk.item * (walk.sq.steps + kItemCost)));
+  walk.at = before + (long long)walk.item * (walk.sq.steps + kItemCost);
+  walk.u0 = uniform((int)(start - walk.at));
   const int G = a.Hq / a.c.Hkv;
   P x;
   x.lane = lane;
   x.row = row;
   x.grp = grp;
+  x.qs = q_s;
   Item it = walk.next(a);
   TableWalk table;
   table.start(a.c, it.s, it.begin(wave, P::PER) >> 4);
   x.start(a, it, table, wave);
   while (it.valid) {
+    if (P::QS) {
+      x.stage_q(a, it, q_s, wave);
+      __syncthreads();
+    }
     const Item next = walk.next(a);
     if (next.valid) table.start(a.c, next.s, next.begin(wave, P::PER) >> 4);
     x.run(a, it, next, table, wave);
@@ -543,7 +565,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
       }
     __syncthreads();
     const bool done = t0 == 0 && t1 == sq.steps;
-    float* slot = a.ws + plan_floats(a.c.S) + (size_t)(2 * r + (t0 == 0)) * slot_floats<D, NT>();
+    if (t0 == 0 && !done && threadIdx.x == 0)
+      *cut = Cut{s, g, qb, (int)quotient(it.at + kItemCost + sq.steps - 1, plan.length)};
+    float* slot = a.ws + cut_floats(runs) + (size_t)(2 * r + (t0 == 0)) * slot_floats<D, NT>();
     for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
       const int c = i / (D / 4), d = i % (D / 4) * 4, col = qb * COLS + c;
       float top = ml[0][c].x, sum = 0.f;
@@ -571,57 +595,59 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
   }
 }
 
-// The outputs of the items that several runs share: one workgroup per (row,
-// query head); each group of D threads sums every (256 / D)-th piece.
+// The outputs of the items that several runs share, by the run that an item starts
+// in: one workgroup per (run, column), D / 4 threads to a piece.
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a) {
-  constexpr int COLS = 16 * NT, PARTS = 256 / D;
-  __shared__ float acc_s[256], top_s[4], sum_s[256];
-  const int r = blockIdx.x, h = blockIdx.y, s = r / a.n, i = r - s * a.n;
-  const long long* head = (const long long*)a.ws;
-  const long long length = head[0], before = head[kHead + s];
-  const Seq sq = seq_of<COLS>(a, s);
-  if (i >= sq.m) return;
-  const int G = a.Hq / a.c.Hkv, g = h / G, col = i * G + h - g * G, qb = col / COLS, c = col - qb * COLS;
-  const long long from = before + (long long)(g * (sq.items / a.c.Hkv) + qb) * (sq.steps + kItemCost) + kItemCost;
-  const int w0 = (int)quotient(from, length), w1 = (int)quotient(from + sq.steps - 1, length);
-  if (w0 == w1) return;
-  const float* slots = a.ws + plan_floats(a.c.S);
-  auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == w0)) * slot_floats<D, NT>(); };
-  const int t = threadIdx.x;
+__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
+  constexpr int COLS = 16 * NT, W = D / 4, PARTS = 256 / W;
+  __shared__ f32x4 acc_s[PARTS][W];
+  __shared__ float sum_s[PARTS], top_s[4];
+  const int r = blockIdx.x, c = blockIdx.y, t = threadIdx.x;
+  const Cut cut = ((const Cut*)a.ws)[r];
+  if (cut.s < 0) return;
+  const int G = a.Hq / a.c.Hkv, col = cut.qb * COLS + c;
+  if (col >= new_tokens(a, cut.s) * G) return;
+  const float* slots = a.ws + cut_floats(runs);
+  auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == r)) * slot_floats<D, NT>(); };
   float top = kNoRef;
-  for (int w = w0 + t; w <= w1; w += 256) top = fmaxf(top, slot(w)[COLS * D + 2 * c]);
+  for (int w = r + t; w <= cut.last; w += 256) top = fmaxf(top, slot(w)[COLS * D + 2 * c]);
   top = block_max_once(top, top_s);
-  const int d = t % D, part = t / D;
-  float acc = 0.f, sum = 0.f;
-#pragma unroll 8
-  for (int w = w0 + part; w <= w1; w += PARTS) {
+  const int d = t % W, part = t / W;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float sum = 0.f;
+#pragma unroll 4
+  for (int w = r + part; w <= cut.last; w += PARTS) {
     const float* p = slot(w);
-    const float f = exp2_raw(p[COLS * D + 2 * c] - top);
-    acc += f * p[c * D + d];
-    sum += f * p[COLS * D + 2 * c + 1];
+    const float2 ml = *(const float2*)(p + COLS * D + 2 * c);
+    const float f = exp2_raw(ml.x - top);
+    acc += f * *(const f32x4*)(p + c * D + 4 * d);
+    sum += f * ml.y;
   }
-  acc_s[t] = acc;
-  sum_s[t] = sum;
+  acc_s[part][d] = acc;
+  if (d == 0) sum_s[part] = sum;
   __syncthreads();
-  if (t >= D) return;
+  if (t >= W) return;
 #pragma unroll
   for (int k = 1; k < PARTS; ++k) {
-    acc += acc_s[k * D + t];
-    sum += sum_s[k * D + t];
+    acc += acc_s[k][t];
+    sum += sum_s[k];
   }
-  store_f((T*)a.out + ((size_t)r * a.Hq + h) * D + t, sum == 0.f ? 0.f : acc / sum);
-  if (t == 0 && a.lse) a.lse[(size_t)r * a.Hq + h] = lse_of(top, sum);
+  const size_t at = ((size_t)cut.s * a.n + col / G) * a.Hq + cut.g * G + col % G;
+  store_row4((T*)a.out + at * D + 4 * t, acc * (sum == 0.f ? 0.f : 1.f / sum));
+  if (t == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
-// Query tiles a wave holds at once: all of a sequence's query vectors up to 64.
-int tiles_for(int vectors) { return vectors <= 16 ? 1 : vectors <= 32 ? 2 : 4; }
+// Query tiles a wave holds at once: all of a sequence's query vectors up to 64 (fp32
+// of 128 dimensions: 32, what the registers hold).
+int tiles_for(const PagedView& c, int vectors) {
+  return vectors <= 16 ? 1 : vectors <= 32 || (c.esz == 4 && c.D == 128) ? 2 : 4;
+}
 
 int runs_for(const PagedView& c, int n, int Hq) {
-  const int cols = 16 * tiles_for(n * (Hq / c.Hkv));
+  const int nt = tiles_for(c, n * (Hq / c.Hkv)), cols = 16 * nt;
   const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
-  return (int)std::min((double)kMaxRuns, std::ceil((steps + kItemCost * items) / kMinSteps));
+  return (int)std::min(nt == 1 ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
 }
 
 template <typename T, int D, int NT>
@@ -629,17 +655,19 @@ hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
   const int runs = runs_for(a.c, a.n, a.Hq);
   hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
-  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(a.c.S * a.n, a.Hq), dim3(256), 0, s, a);
+  const int cols = std::min(16 * NT, a.n * (a.Hq / a.c.Hkv));
+  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(runs, cols), dim3(256), 0, s, a, runs);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
-  switch (tiles_for(a.n * (a.Hq / a.c.Hkv))) {
+  switch (tiles_for(a.c, a.n * (a.Hq / a.c.Hkv))) {
     case 1: return launch<T, D, 1>(a, s);
     case 2: return launch<T, D, 2>(a, s);
-    default: return launch<T, D, 4>(a, s);
   }
+  if constexpr (sizeof(T) == 2 || D < 128) return launch<T, D, 4>(a, s);
+  return hipErrorInvalidValue;
 }
 
 template <typename T>
@@ -654,8 +682,8 @@ hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
-  const int nt = tiles_for(n * (Hq / c.Hkv));
-  return plan_floats(c.S) + (size_t)2 * runs_for(c, n, Hq) * 16 * nt * (c.D + 2);
+  const int nt = tiles_for(c, n * (Hq / c.Hkv)), runs = runs_for(c, n, Hq);
+  return cut_floats(runs) + (size_t)2 * runs * 16 * nt * (c.D + 2);
 }
 
 hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s) {
