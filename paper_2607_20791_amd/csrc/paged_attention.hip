@@ -145,13 +145,49 @@ RGD_DEV u32x4 keep_first(u32x4 v, int n) {
   return v;
 }
 
+// 1 in the first n places, 0 behind.
+template <typename T>
+RGD_DEV u32x4 ones(int n) {
+  const uint32_t one = sizeof(T) == 4 ? 0x3F800000u : 0x3F803F80u;
+  return keep_first<T>(u32x4{one, one, one, one}, n);
+}
+
+// Bits by type.
+template <typename T>
+constexpr uint32_t kInf = sizeof(T) == 4 ? 0x7F800000u : 0x7F80u;
+template <typename T>
+constexpr uint32_t kSign = sizeof(T) == 4 ? 0x80000000u : 0x8000u;
+
+// f(bits) of each value packed in v.
+template <typename T, typename F>
+RGD_DEV u32x4 each(u32x4 v, F f) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[j] = sizeof(T) == 4 ? f(v[j]) : f(v[j] & 0xFFFFu) | f(v[j] >> 16) << 16;
+  return v;
+}
+
+// 1 where a value is +inf (kind 0), -inf (1) or NaN (2).
+template <typename T>
+RGD_DEV u32x4 marks(u32x4 v, int kind) {
+  const uint32_t one = sizeof(T) == 4 ? 0x3F800000u : 0x3F80u;
+  return each<T>(v, [=](uint32_t x) {
+    const bool hit = kind == 2 ? (x & ~kSign<T>) > kInf<T> : x == (kind ? kInf<T> | kSign<T> : kInf<T>);
+    return hit ? one : 0u;
+  });
+}
+
+// 0 in the place of every value that is not finite.
+template <typename T>
+RGD_DEV u32x4 finite(u32x4 v) {
+  return each<T>(v, [](uint32_t x) { return (x & kInf<T>) == kInf<T> ? 0u : x; });
+}
+
 template <typename T>
 RGD_DEV bool any_nonfinite(u32x4 v) {
   bool bad = false;
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    bad = bad || (sizeof(T) == 4 ? (v[j] & 0x7F800000u) == 0x7F800000u
-                                 : (v[j] & 0x7F80u) == 0x7F80u || (v[j] & 0x7F800000u) == 0x7F800000u);
+    bad = bad || (v[j] & kInf<T>) == kInf<T> || (sizeof(T) == 2 && (v[j] >> 16 & kInf<T>) == kInf<T>);
   return bad;
 }
 
@@ -321,6 +357,15 @@ struct Piece {
     }
   }
 
+  // sum over the positions of x y, both held as V and the weights are
+  RGD_DEV f32x4 count(const u32x4& x, const u32x4& y) const {
+    f32x4 r = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (BF) return mfma_bf16(x, y, r);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r = mfma_f32(__uint_as_float(x[j]), __uint_as_float(y[j]), r);
+    return r;
+  }
+
   // Weights of tile t's scores (log2 units) against its running maximum, which moves
   // with them; hi + lo: the weights in two bf16.
   RGD_DEV void weights(int t, const float (&x)[E], float (&p)[E], u32x4& hi, u32x4& lo) {
@@ -453,34 +498,43 @@ struct Piece {
         v[d] = keep_first<T>(v[d], held);
         odd = odd || any_nonfinite<T>(v[d]);
       }
-      // 0 times a value that is not finite is not 0: where some tokens see such a
-      // value and others do not, each token's columns take the product with what it sees
-      const bool mixed = __any(odd);
+      float p[NT][E];
+      u32x4 hi[NT], lo[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const int seen = there ? lim[t] - pos : 0;
-        float x[E], p[E];
+        float x[E];
 #pragma unroll
         for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] * scale : -INFINITY;
-        u32x4 hi, lo;
-        weights(t, x, p, hi, lo);
-        if (!mixed) {
+        weights(t, x, p[t], hi[t], lo[t]);
+      }
+      if (__any(odd)) {
+        // 0 times a value that is not finite is not 0, so these leave the product: a
+        // column gets them by whether it sees one, not by its weight
+        u32x4 see[NT];
 #pragma unroll
-          for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p, hi, lo, o[t][d]);
-        } else {
-          const int c0 = min(qb * COLS + t * 16, cols - 1), c1 = min(qb * COLS + t * 16 + 15, cols - 1);
-#pragma unroll 1
-          for (int i = c0 / G; i <= c1 / G; ++i) {
-            const int see = sq.len - sq.m + i + 1;
-            const int n = there ? see - pos : 0;
+        for (int t = 0; t < NT; ++t) see[t] = ones<T>(there ? lim[t] - pos : 0);
 #pragma unroll
-            for (int d = 0; d < VL; ++d) {
-              const f32x4 r = weigh(keep_first<T>(v[d], n), p, hi, lo, o[t][d]);
-              if (lim[t] == see) o[t][d] = r;
+        for (int d = 0; d < VL; ++d) {
+#pragma unroll
+          for (int kind = 0; kind < 3; ++kind) {
+            const u32x4 at = marks<T>(v[d], kind);
+            const float is = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              const f32x4 r = count(at, see[t]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[t][d][e] += r[e] > 0.f ? is : 0.f;
+              __builtin_amdgcn_sched_barrier(0);  // one count's registers at a time
             }
           }
+          v[d] = finite<T>(v[d]);
         }
       }
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p[t], hi[t], lo[t], o[t][d]);
       if (more || on) load_v(a);
       p0 += STRIDE;
     }

@@ -311,6 +311,44 @@ def test_scores_far_apart_and_a_nan(rgd, bf16):
     assert bool(t.isfinite(out[0]).all()) and bool(t.isnan(out[1]).all())
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n,hk,G,d", [(3, 2, 4, 64), (7, 1, 4, 128), (16, 1, 4, 128), (12, 1, 5, 32)])
+def test_later_tokens_do_not_reach_earlier_ones(rgd, bf16, n, hk, G, d):
+    """Keys and values that are not finite at a new token's position: the tokens before it get the bits they
+    get without them, the others what the formula gives."""
+    t = torch()
+    lens = [n, 45, 64, 200]
+    x = _filled(rgd, lens, hk=hk, d=d, bf16=bf16, seed=n)
+    ref, _ = _attention(x, 0, hk * G, n, None)
+    q = t.randn(4 * n, hk * G, d, device="cuda").to(_dt(bf16))
+    ws = t.empty(rgd.paged_attention_workspace_bytes(x.c, n, hk * G), dtype=t.uint8, device="cuda")
+
+    def run():
+        out = t.zeros(4 * n, hk * G * d, dtype=_dt(bf16), device="cuda")
+        rgd.paged_attention(x.c, 0, q, n, None, ws, out)
+        return out.view(4, n, hk, G, d)
+
+    ref = run()
+    inf, nan = float("inf"), float("nan")
+    for s, (i, what) in enumerate(((n - 1, (nan, 0)), (n - 2, (inf, 1)), (1, (-inf, 1)), (n // 2, (nan, 1)))):
+        pos = lens[s] - n + i
+        page = int(x.pages[s, pos // 16])
+        if what[1]:
+            x.c.pool_v[0, page, 0, 3, pos % 16] = what[0]   # dimension 3 of KV head 0
+        else:
+            x.c.pool_k[0, page, 0, pos % 16] = what[0]
+        got = run()
+        assert t.equal(got[s, :i], ref[s, :i]), (s, i)
+        assert t.equal(got[:, :, 1:], ref[:, :, 1:])
+        late = got[s, i:, 0].float()
+        if not what[1]:
+            assert bool(t.isnan(late).all())
+        else:
+            rest = [e for e in range(d) if e != 3]
+            assert t.equal(got[s, i:, 0][..., rest], ref[s, i:, 0][..., rest])
+            assert bool((t.isnan(late[..., 3]) if what[0] != what[0] else late[..., 3] == what[0]).all())
+
+
 def test_offsets_beyond_32_bits(rgd):
     """A pool of more than 2^31 elements whose used pages lie at its end."""
     t = torch()
