@@ -649,46 +649,56 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
   }
 }
 
+// Columns per workgroup of the joining kernel: one where a sequence has few (its pieces
+// are then shared out over the workgroup), eight where it has many.
+constexpr int join_cols(int nt) { return nt == 1 ? 1 : 8; }
+
 // The outputs of the items that several runs share, by the run that an item starts
-// in: one workgroup per (run, column), D / 4 threads to a piece.
+// in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
-  constexpr int COLS = 16 * NT, W = D / 4, PARTS = 256 / W;
-  __shared__ f32x4 acc_s[PARTS][W];
-  __shared__ float sum_s[PARTS], top_s[4];
-  const int r = blockIdx.x, c = blockIdx.y, t = threadIdx.x;
+  constexpr int COLS = 16 * NT, W = D / 4, CB = join_cols(NT), PARTS = 256 / W / CB;
+  __shared__ f32x4 acc_s[CB][PARTS][W];
+  __shared__ float2 ml_s[CB][PARTS];
+  const int r = blockIdx.x, t = threadIdx.x;
   const Cut cut = ((const Cut*)a.ws)[r];
   if (cut.s < 0) return;
-  const int G = a.Hq / a.c.Hkv, col = cut.qb * COLS + c;
-  if (col >= new_tokens(a, cut.s) * G) return;
+  const int d = t % W, k = t / W / PARTS, part = t / W % PARTS, c = blockIdx.y * CB + k;
+  const int G = a.Hq / a.c.Hkv, col = cut.qb * COLS + c, cols = min(COLS, new_tokens(a, cut.s) * G - cut.qb * COLS);
   const float* slots = a.ws + cut_floats(runs);
   auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == r)) * slot_floats<D, NT>(); };
-  float top = kNoRef;
-  for (int w = r + t; w <= cut.last; w += 256) top = fmaxf(top, slot(w)[COLS * D + 2 * c]);
-  top = block_max_once(top, top_s);
-  const int d = t % W, part = t / W;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f;
+  float sum = 0.f, top = kNoRef;
+  if (c < cols) {
 #pragma unroll 4
-  for (int w = r + part; w <= cut.last; w += PARTS) {
-    const float* p = slot(w);
-    const float2 ml = *(const float2*)(p + COLS * D + 2 * c);
-    const float f = exp2_raw(ml.x - top);
-    acc += f * *(const f32x4*)(p + c * D + 4 * d);
-    sum += f * ml.y;
+    for (int w = r + part; w <= cut.last; w += PARTS) {
+      const float* p = slot(w);
+      const float2 ml = *(const float2*)(p + COLS * D + 2 * c);
+      const float nt = fmaxf(top, ml.x), down = exp2_raw(top - nt), f = exp2_raw(ml.x - nt);
+      acc = acc * down + f * *(const f32x4*)(p + c * D + 4 * d);
+      sum = sum * down + f * ml.y;
+      top = nt;
+    }
+    acc_s[k][part][d] = acc;
+    if (d == 0) ml_s[k][part] = float2{top, sum};
   }
-  acc_s[part][d] = acc;
-  if (d == 0) sum_s[part] = sum;
-  __syncthreads();
-  if (t >= W) return;
+  if (PARTS > 1) __syncthreads();
+  if (part > 0 || c >= cols) return;
+  if (PARTS > 1) {
 #pragma unroll
-  for (int k = 1; k < PARTS; ++k) {
-    acc += acc_s[k][t];
-    sum += sum_s[k];
+    for (int i = 0; i < PARTS; ++i) top = fmaxf(top, ml_s[k][i].x);
+    acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      const float f = exp2_raw(ml_s[k][i].x - top);
+      acc += f * acc_s[k][i][d];
+      sum += f * ml_s[k][i].y;
+    }
   }
   const size_t at = ((size_t)cut.s * a.n + col / G) * a.Hq + cut.g * G + col % G;
-  store_row4((T*)a.out + at * D + 4 * t, acc * (sum == 0.f ? 0.f : 1.f / sum));
-  if (t == 0 && a.lse) a.lse[at] = lse_of(top, sum);
+  store_row4((T*)a.out + at * D + 4 * d, acc * (sum == 0.f ? 0.f : 1.f / sum));
+  if (d == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
 // Query tiles a wave holds at once: all of a sequence's query vectors up to 64 (fp32
@@ -710,7 +720,7 @@ hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
   const int cols = std::min(16 * NT, a.n * (a.Hq / a.c.Hkv));
-  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(runs, cols), dim3(256), 0, s, a, runs);
+  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(runs, (cols + join_cols(NT) - 1) / join_cols(NT)), dim3(256), 0, s, a, runs);
   return hipGetLastError();
 }
 
