@@ -5,6 +5,15 @@
 // u q(x) < p(x); the first refusal draws from max(p - q, 0).  Sequences sampled
 // this way are distributed as if drawn from p one by one: x is emitted with
 // probability min(p, q) + (1 - sum min(p, q)) max(p - q, 0) / sum max(p - q, 0) = p.
+//
+// One read of all logits bounds it.  Pass 1 streams them and keeps the maximum of
+// every 1024 ids (a span): with a row's maximum its threshold is known, and
+// only spans whose maximum reaches it hold kept ids.  Those alone are read again,
+// for the rows' sums (pass 2), for the rest of p over q in the one row per sequence
+// that is drawn from (pass 3), and one span of them for the draw (pass 4).  Weights
+// and sums are fp64: the token drawn hangs on sums of up to 2^20 weights, which fp32
+// would leave wrong in one draw of a few.  T == 0: pass 1, then the first
+// id of each row's maximum.
 #include <algorithm>
 #include <cmath>
 
@@ -14,176 +23,505 @@ namespace rgd {
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kSpan = 1024;      // ids per span: one wave, 16 a lane
+constexpr int kSpansPerWg = 16;  // pass 1: four waves, four spans each
+constexpr int kMaxSpans = 1024;
+constexpr int kMaxParts = 16;    // workgroups that share a row in passes 2 and 3
 
-RGD_DEV double block_sum_f64(double v, double* red) {
+typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
+
+// 2^x to 1e-14 for x <= 0: the Taylor series of 2^f, |f| <= 1/2, to f^11.
+RGD_DEV double exp2_f64(double x) {
+  x = fmax(x, -1100.0);  // below: 0 either way (and -inf - rint(-inf) is not a number)
+  const double n = rint(x), g = (x - n) * 0.6931471805599453;
+  double s = 1.0 / 39916800.0;
+  s = fma(s, g, 1.0 / 3628800.0);
+  s = fma(s, g, 1.0 / 362880.0);
+  s = fma(s, g, 1.0 / 40320.0);
+  s = fma(s, g, 1.0 / 5040.0);
+  s = fma(s, g, 1.0 / 720.0);
+  s = fma(s, g, 1.0 / 120.0);
+  s = fma(s, g, 1.0 / 24.0);
+  s = fma(s, g, 1.0 / 6.0);
+  s = fma(s, g, 0.5);
+  s = fma(s, g, 1.0);
+  s = fma(s, g, 1.0);
+  return ldexp(s, (int)n);
+}
+
+RGD_DEV double wave_sum_f64(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+struct Job {
+  VerifyArgs a;
+  double per_z, low;  // log2(e) / T; kept: z - max >= low
+  int spans, parts2, parts3;
+  float* span_max;    // [rows][spans]
+  float* top;         // [rows]
+  double* sums;       // [rows][parts2]
+  double2* rest;      // [S][spans]: rest of p over q, and p, of the drawn row's listed spans
+  int* accepted;      // [S]
+};
+
+// Rows: the target's S (K + 1), then the drafts' S K.
+RGD_DEV long long target_row(const VerifyArgs& a, int s, int i) { return (long long)s * (a.K + 1) + i; }
+RGD_DEV long long draft_row(const VerifyArgs& a, int s, int i) {
+  return (long long)a.S * (a.K + 1) + (long long)s * a.K + i;
+}
+RGD_DEV int drafts_of(const VerifyArgs& a, int s) { return a.n_draft ? min(max(a.n_draft[s], 0), a.K) : a.K; }
+
+// The logits of a row, or null where it is not asked for.
+RGD_DEV const float* row_logits(const VerifyArgs& a, long long r) {
+  const long long nt = (long long)a.S * (a.K + 1);
+  if (r < nt) {
+    const int s = (int)(r / (a.K + 1)), i = (int)(r - (long long)s * (a.K + 1));
+    return i <= drafts_of(a, s) ? a.target + r * a.V : nullptr;
+  }
+  r -= nt;
+  const int s = (int)(r / a.K), i = (int)(r - (long long)s * a.K);
+  return i < drafts_of(a, s) ? a.draft + r * a.V : nullptr;
+}
+
+// This lane's ids of a span: 256 k + 4 lane + {0..3}; behind the row -inf.
+RGD_DEV void load_span(const float* z, int V, int span, f4 (&v)[4]) {
+  const int at = span * kSpan + (threadIdx.x & 63) * 4;
+  if ((span + 1) * kSpan <= V) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = *(const f4*)(z + at + 256 * k);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[k][e] = at + 256 * k + e < V ? z[at + 256 * k + e] : -INFINITY;
+  }
+}
+
+// ------------------------------------------------------------------ pass 1 --
+__global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
+  const long long r = blockIdx.x / groups;
+  const int first = (int)(blockIdx.x % groups) * kSpansPerWg + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const float* z = row_logits(j.a, r);
+  if (!z) return;
+  f4 v[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (first + 4 * k < j.spans) load_span(z, j.a.V, first + 4 * k, v[k]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (first + 4 * k >= j.spans) return;
+    float m = -INFINITY;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) m = fmaxf(m, fmaxf(fmaxf(v[k][q][0], v[k][q][1]), fmaxf(v[k][q][2], v[k][q][3])));
+    m = wave_max(m);  // NaN counts as -inf: fmaxf takes the other operand
+    if (lane == 0) j.span_max[r * j.spans + first + 4 * k] = m;
+  }
+}
+
+// The lowest kept logit of a row of maximum `top`: the smallest float z with
+// (double)z - top >= low, so that one fp32 comparison decides as fp64 does.
+RGD_DEV float threshold(float top, double low) {
+  float f = (float)((double)top + low);
+  for (int i = 0; i < 4 && (double)f - (double)top < low; ++i) f = nextafterf(f, INFINITY);
+  for (int i = 0; i < 4; ++i) {
+    const float g = nextafterf(f, -INFINITY);
+    if (!((double)g - (double)top >= low)) break;
+    f = g;
+  }
+  return f;
+}
+
+// One row's distribution.
+struct Dist {
+  const float* z;
+  float top, thr;
+  double per_z, scale;  // p = 2^((z - top) per_z) * scale
+  RGD_DEV double weight(float x) const { return x >= thr ? exp2_f64(((double)x - (double)top) * per_z) : 0.0; }
+  RGD_DEV double p(float x) const { return weight(x) * scale; }
+};
+
+RGD_DEV bool finite_top(float t) { return t > -INFINITY && t < INFINITY; }
+
+RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r) {
+  Dist d;
+  d.z = logits;
+  d.top = j.top[r];
+  d.thr = INFINITY;  // no distribution: nothing kept
+  d.per_z = j.per_z;
+  d.scale = 0.0;
+  if (!finite_top(d.top)) return d;
+  d.thr = threshold(d.top, j.low);
+  double W = 0.0;
+  for (int k = 0; k < j.parts2; ++k) W += j.sums[r * j.parts2 + k];
+  d.scale = 1.0 / W;
+  return d;
+}
+
+// The spans of row r whose maximum reaches thr, in order, by the whole workgroup
+// of 256: list[0 .. n).  Returns n.  red: 4 ints.
+RGD_DEV int list_spans(const Job& j, long long r, float thr, unsigned short* list, int* red) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  int mine = 0;
+  bool hit[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {  // four neighbouring spans a thread
+    const int sp = 4 * t + k;
+    hit[k] = sp < j.spans && j.span_max[r * j.spans + sp] >= thr;
+    mine += hit[k];
+  }
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += v;
+  }
+  __syncthreads();
+  if (lane == 63) red[w] = incl;
+  __syncthreads();
+  int at = incl - mine, n = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    at += k < w ? red[k] : 0;
+    n += red[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (hit[k]) list[at++] = (unsigned short)(4 * t + k);
+  __syncthreads();
+  return n;
+}
+
+// ------------------------------------------------------------------ pass 2 --
+// A row's maximum and this part's share of its kept sum.
+__global__ __launch_bounds__(256) void verify_sum_kernel(Job j) {
+  __shared__ float redf[4];
+  __shared__ int red[4];
+  __shared__ double redd[4];
+  __shared__ unsigned short list[kMaxSpans];
+  const long long r = blockIdx.x / j.parts2;
+  const int part = (int)(blockIdx.x % j.parts2), w = threadIdx.x >> 6;
+  const float* z = row_logits(j.a, r);
+  if (!z) return;
+  float m = -INFINITY;
+  for (int i = threadIdx.x; i < j.spans; i += 256) m = fmaxf(m, j.span_max[r * j.spans + i]);
+  m = block_max_once(m, redf);
+  if (part == 0 && threadIdx.x == 0) j.top[r] = m;
+  if (!finite_top(m)) return;
+  const float thr = threshold(m, j.low);
+  const int n = list_spans(j, r, thr, list, red);
+  double sum = 0.0;
+  for (int i = part * 4 + w; i < n; i += 4 * j.parts2) {
+    f4 v[4];
+    load_span(z, j.a.V, list[i], v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v[k][e] >= thr) sum += exp2_f64(((double)v[k][e] - (double)m) * j.per_z);
+  }
+  sum = wave_sum_f64(sum);
+  if ((threadIdx.x & 63) == 0) redd[w] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) j.sums[r * j.parts2 + part] = ((redd[0] + redd[1]) + redd[2]) + redd[3];
+}
+
+// ------------------------------------------------------------------ pass 3 --
+// What one sequence draws from.
+struct Draw {
+  Dist p, q;
+  int at;         // accepted drafts
+  int without;    // the id that is left out (a certain draft), or -1
+  bool minus_q;
+  RGD_DEV double2 rest(float zp, float zq, int id) const {
+    const double x = p.p(zp);
+    double r = x;
+    if (minus_q) r = fmax(x - q.p(zq), 0.0);
+    if (id == without) r = 0.0;
+    return double2{r, x};
+  }
+};
+
+RGD_DEV Draw draw_of(const Job& j, int s, int accepted) {
+  const VerifyArgs& a = j.a;
+  Draw d;
+  d.at = accepted;
+  const long long r = target_row(a, s, accepted);
+  d.p = dist_of(j, a.target + r * a.V, r);
+  const bool refused = accepted < drafts_of(a, s);
+  d.minus_q = refused && a.draft;
+  d.without = refused && !a.draft ? a.tokens[(long long)s * a.K + accepted] : -1;
+  d.q = d.p;
+  if (d.minus_q) {
+    const long long x = (long long)s * a.K + accepted;
+    d.q = dist_of(j, a.draft + x * a.V, draft_row(a, s, accepted));
+  }
+  return d;
+}
+
+// Accepted drafts of a sequence, one draft a thread (K <= 255), then the rest of the
+// drawn row in this part's spans.
+__global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
+  __shared__ int first[4], red[4];
+  __shared__ unsigned short list[kMaxSpans];
+  const VerifyArgs& a = j.a;
+  const int s = blockIdx.x / j.parts3, part = blockIdx.x % j.parts3, t = threadIdx.x, w = t >> 6;
+  const int nd = drafts_of(a, s);
+  bool ok = true;
+  if (t < nd) {
+    const int id = a.tokens[(long long)s * a.K + t];
+    ok = false;
+    if ((unsigned)id < (unsigned)a.V) {
+      const long long r = target_row(a, s, t), x = (long long)s * a.K + t;
+      const Dist p = dist_of(j, a.target + r * a.V, r);
+      const double px = p.p(p.z[id]);
+      double qx = 1.0;
+      if (a.draft) {
+        const Dist q = dist_of(j, a.draft + x * a.V, draft_row(a, s, t));
+        qx = q.p(q.z[id]);
+      }
+      ok = (double)a.u[(long long)s * (a.K + 1) + t] * qx < px;
+    }
+  }
+  const unsigned long long no = __ballot(!ok);
+  if ((t & 63) == 0) first[w] = no ? 64 * w + __builtin_ctzll(no) : 0x7FFFFFFF;
+  __syncthreads();
+  const int acc = min(min(min(first[0], first[1]), min(first[2], first[3])), nd);
+  if (part == 0 && t == 0) j.accepted[s] = acc;
+  const Draw d = draw_of(j, s, acc);
+  if (!finite_top(d.p.top)) return;
+  const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, red);
+  for (int i = part * 4 + w; i < n; i += 4 * j.parts3) {
+    f4 v[4], q[4];
+    const int sp = list[i];
+    load_span(d.p.z, a.V, sp, v);
+    if (d.minus_q) load_span(d.q.z, a.V, sp, q);
+    else
+      for (int k = 0; k < 4; ++k) q[k] = v[k];
+    double2 sum{0.0, 0.0};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v[k][e] >= d.p.thr) {
+          const double2 x = d.rest(v[k][e], q[k][e], sp * kSpan + 256 * k + (t & 63) * 4 + e);
+          sum.x += x.x;
+          sum.y += x.y;
+        }
+    sum.x = wave_sum_f64(sum.x);
+    sum.y = wave_sum_f64(sum.y);
+    if ((t & 63) == 0) j.rest[(long long)s * j.spans + i] = sum;
+  }
+}
+
+// ------------------------------------------------------------------ pass 4 --
+RGD_DEV double block_scan_f64(double v, double* red, double& total) {  // exclusive
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  double incl = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const double x = __shfl_up(incl, o, 64);
+    if (lane >= o) incl += x;
+  }
+  __syncthreads();
+  if (lane == 63) red[w] = incl;
+  __syncthreads();
+  double before = 0.0;
+  total = 0.0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    before += k < w ? red[k] : 0.0;
+    total += red[k];
+  }
+  return before + (incl - v);
+}
+
+RGD_DEV int block_min_i(int v, int* red) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = min(v, __shfl_xor(v, o, 64));
   __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  double t = 0.0;
-  for (int i = 0; i < kThreads / 64; ++i) t += red[i];
-  return t;
+  return min(min(red[0], red[1]), min(red[2], red[3]));
 }
 
-// One row's distribution: the maximum, the lowest kept z - max, the sum of the
-// weights.  alive: the maximum is finite.  T == 0: first holds the argmax.
-struct RowDist {
-  float top;
-  double W;
-  int first;
-  bool alive;
-};
-
-struct Rule {
-  double T, low;  // kept: z - max >= low
-};
-
-RGD_DEV double weight(const Rule& k, const RowDist& r, float z, int id) {
-  if (k.T == 0.0) return id == r.first ? 1.0 : 0.0;
-  const double x = (double)z - (double)r.top;
-  return x >= k.low ? exp(x / k.T) : 0.0;
-}
-
-RGD_DEV RowDist row_dist(const float* z, int V, const Rule& k, double* red, float* redf, int* redi) {
-  RowDist r;
-  float mx = -INFINITY;
-  for (int i = threadIdx.x; i < V; i += kThreads) mx = fmaxf(mx, z[i]);
-  r.top = block_max(mx, redf);
-  r.alive = r.top > -INFINITY && r.top < INFINITY;
-  r.first = 0x7FFFFFFF;
-  r.W = 1.0;
-  if (!r.alive) return r;
-  if (k.T == 0.0) {
-    int at = 0x7FFFFFFF;
-    for (int i = threadIdx.x; i < V; i += kThreads)
-      if (z[i] == r.top) at = min(at, i);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o, 64));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) redi[threadIdx.x >> 6] = at;
-    __syncthreads();
-    for (int i = 0; i < kThreads / 64; ++i) r.first = min(r.first, redi[i]);
-    return r;
-  }
-  double w = 0.0;
-  for (int i = threadIdx.x; i < V; i += kThreads) w += weight(k, r, z[i], i);
-  r.W = block_sum_f64(w, red);
-  return r;
-}
-
-// One workgroup per sequence, its rows one after the other.
-__global__ __launch_bounds__(kThreads) void verify_kernel(VerifyArgs a, Rule k) {
-  __shared__ double red[kThreads / 64];
-  __shared__ float redf[kThreads / 64];
-  __shared__ int redi[kThreads / 64];
+// The draw: the span, then the id, whose running sum first exceeds u times the total;
+// where rounding leaves none, the last one with weight.
+__global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
+  __shared__ double red[4];
+  __shared__ int redi[4];
+  __shared__ unsigned short list[kMaxSpans];
+  __shared__ double sh_before;
+  const VerifyArgs& a = j.a;
   const int s = blockIdx.x, t = threadIdx.x;
-  const int nd = a.n_draft ? min(max(a.n_draft[s], 0), a.K) : a.K;
-  const bool onehot = !a.draft || k.T == 0.0;
-  const float* u = a.u + (size_t)s * (a.K + 1);
-  int* out = a.out + (size_t)s * (a.K + 1);
-  const int* x = a.tokens + (size_t)s * a.K;
-  int i = 0;
-  RowDist p, q;
-  bool refused = false, inside = false;
-  const float *zp = nullptr, *zq = nullptr;
-  for (;; ++i) {
-    zp = a.target + ((size_t)s * (a.K + 1) + i) * a.V;
-    p = row_dist(zp, a.V, k, red, redf, redi);
-    if (i >= nd) break;
-    const int id = x[i];
-    inside = (unsigned)id < (unsigned)a.V;
-    double px = 0.0, qx = 0.0;
-    if (inside && p.alive) px = weight(k, p, zp[id], id) / p.W;
-    if (onehot) {
-      qx = 1.0;
-    } else {
-      zq = a.draft + ((size_t)s * a.K + i) * a.V;
-      q = row_dist(zq, a.V, k, red, redf, redi);
-      if (inside && q.alive) qx = weight(k, q, zq[id], id) / q.W;
-    }
-    if (!((double)u[i] * qx < px)) {
-      refused = true;
-      break;
-    }
-    if (t == 0) out[i] = id;
-  }
-  if (t == 0) a.n_accepted[s] = i;
-  for (int j = i + 1 + t; j <= a.K; j += kThreads) out[j] = -1;
-  if (!p.alive) {
-    if (t == 0) out[i] = -1;
+  const int acc = j.accepted[s];
+  int* out = a.out + (long long)s * (a.K + 1);
+  if (t == 0) a.n_accepted[s] = acc;
+  if (t <= a.K && t != acc) out[t] = t < acc ? a.tokens[(long long)s * a.K + t] : -1;
+  const Draw d = draw_of(j, s, acc);
+  if (!finite_top(d.p.top)) {
+    if (t == 0) out[acc] = -1;
     return;
   }
-  // the draw: thread t owns ids [t * per, (t + 1) * per)
-  const int per = (a.V + kThreads - 1) / kThreads, lo = min(a.V, t * per), hi = min(a.V, lo + per);
-  const int taken = refused && inside ? x[i] : -1;
-  const bool sub = refused && !onehot && q.alive;
-  auto rest = [&](int id, bool plain) {
-    double r = weight(k, p, zp[id], id) / p.W;
-    if (plain) return r;
-    if (sub) r -= weight(k, q, zq[id], id) / q.W;
-    else if (onehot && id == taken) r = 0.0;
-    return r > 0.0 ? r : 0.0;
-  };
-  bool plain = false;
-  double mine = 0.0, all = 0.0;
-  for (int round = 0; round < 2 && all == 0.0; ++round) {
-    plain = round == 1;  // nothing left (rounding): p itself
-    mine = 0.0;
-    for (int id = lo; id < hi; ++id) mine += rest(id, plain);
-    all = block_sum_f64(mine, red);
-  }
-  double incl = mine;
+  const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, redi);
+  double2 part[4];
+  double mine[2] = {0.0, 0.0}, total[2], before[2];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double v = __shfl_up(incl, o, 64);
-    if ((t & 63) >= o) incl += v;
+  for (int k = 0; k < 4; ++k) {
+    part[k] = 4 * t + k < n ? j.rest[(long long)s * j.spans + 4 * t + k] : double2{0.0, 0.0};
+    mine[0] += part[k].x;
+    mine[1] += part[k].y;
   }
-  __syncthreads();
-  if ((t & 63) == 63) red[t >> 6] = incl;
-  __syncthreads();
-  double run = incl - mine;
-  for (int w = 0; w < t >> 6; ++w) run += red[w];
-  const double target = (double)u[a.K] * all;
-  int found = 0x7FFFFFFF, last = -1;
-  for (int id = lo; id < hi; ++id) {
-    const double r = rest(id, plain);
-    if (r <= 0.0) continue;
-    run += r;
-    last = id;
-    if (run > target) {
-      found = id;
-      break;
+  before[0] = block_scan_f64(mine[0], red, total[0]);
+  before[1] = block_scan_f64(mine[1], red, total[1]);
+  const int use = total[0] > 0.0 ? 0 : 1;  // nothing left by rounding: p itself
+  const double goal = (double)a.u[(long long)s * (a.K + 1) + a.K] * total[use];
+  double run = before[use], at[4];
+  int hit = 0x7FFFFFFF, last = 0;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const double x = use ? part[k].y : part[k].x;
+    at[k] = run;
+    if (x > 0.0) {
+      run += x;
+      last = 4 * t + k;
+      if (hit == 0x7FFFFFFF && run > goal) hit = 4 * t + k;
     }
   }
+  hit = block_min_i(hit, redi);
+  if (hit == 0x7FFFFFFF) hit = -block_min_i(-last, redi);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    found = min(found, __shfl_xor(found, o, 64));
-    last = max(last, __shfl_xor(last, o, 64));
+  for (int k = 0; k < 4; ++k)
+    if (hit == 4 * t + k) sh_before = at[k];
+  __syncthreads();
+  // four ids a thread
+  const int sp = list[hit], id0 = sp * kSpan + 4 * t;
+  run = sh_before;
+  double x[4], sum = 0.0, unused;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[e] = 0.0;
+    if (id0 + e < a.V) {
+      const float zp = d.p.z[id0 + e];
+      const double2 v = d.rest(zp, d.minus_q ? d.q.z[id0 + e] : zp, id0 + e);
+      x[e] = use ? v.y : v.x;
+    }
+    sum += x[e];
   }
-  __shared__ int sf[kThreads / 64], sl[kThreads / 64];
-  if ((t & 63) == 0) {
-    sf[t >> 6] = found;
-    sl[t >> 6] = last;
+  run += block_scan_f64(sum, red, unused);
+  int found = 0x7FFFFFFF, end = -1;
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (x[e] > 0.0) {
+      run += x[e];
+      end = id0 + e;
+      if (found == 0x7FFFFFFF && run > goal) found = id0 + e;
+    }
+  found = block_min_i(found, redi);
+  end = -block_min_i(-end, redi);
+  if (t == 0) out[acc] = found != 0x7FFFFFFF ? found : max(end, 0);
+}
+
+// ------------------------------------------------------------------ T == 0 --
+// The first maximum of every row that is asked for, one row a wave; the drafts are
+// kept while they are it.
+__global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
+  __shared__ int best[256];
+  __shared__ int redi[4];
+  const VerifyArgs& a = j.a;
+  const int s = blockIdx.x, t = threadIdx.x, lane = t & 63;
+  const int nd = drafts_of(a, s);
+  for (int i = t >> 6; i <= nd; i += 4) {
+    const long long r = target_row(a, s, i);
+    const float* m = j.span_max + r * j.spans;
+    float top = -INFINITY;
+    for (int k = lane; k < j.spans; k += 64) top = fmaxf(top, m[k]);
+    top = wave_max(top);
+    int sp = 0x7FFFFFFF, id = 0x7FFFFFFF;
+    for (int k = lane; k < j.spans; k += 64)
+      if (m[k] == top) sp = min(sp, k);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sp = min(sp, __shfl_xor(sp, o, 64));
+    if (finite_top(top)) {
+      f4 v[4];
+      load_span(a.target + r * a.V, a.V, sp, v);
+#pragma unroll
+      for (int k = 3; k >= 0; --k)
+#pragma unroll
+        for (int e = 3; e >= 0; --e)
+          if (v[k][e] == top) id = sp * kSpan + 256 * k + lane * 4 + e;
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o, 64));
+    } else {
+      id = -1;
+    }
+    if (lane == 0) best[i] = id;
   }
   __syncthreads();
-  if (t == 0) {
-    for (int w = 0; w < kThreads / 64; ++w) {
-      found = min(found, sf[w]);
-      last = max(last, sl[w]);
-    }
-    out[i] = found != 0x7FFFFFFF ? found : last;
-  }
+  const int* x = a.tokens + (long long)s * a.K;
+  const bool no = t < nd && (best[t] < 0 || best[t] != x[t]);
+  const int acc = min(block_min_i(no ? t : 0x7FFFFFFF, redi), nd);
+  int* out = a.out + (long long)s * (a.K + 1);
+  if (t <= a.K) out[t] = t <= acc ? best[t] : -1;
+  if (t == 0) a.n_accepted[s] = acc;
+}
+
+struct Sizes {
+  long long rows;
+  int spans, parts2, parts3;
+  size_t span_max, top, sums, rest, accepted, bytes;
+};
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+// parts: few rows are shared by several workgroups (2048 and 1024 in all)
+Sizes sizes_of(int S, int K, int V) {
+  Sizes z;
+  z.rows = (long long)S * (2 * K + 1);
+  z.spans = (V + kSpan - 1) / kSpan;
+  z.parts2 = (int)std::min<long long>(kMaxParts, (2047 + z.rows) / z.rows);
+  z.parts3 = std::min(kMaxParts, (1023 + S) / S);
+  z.span_max = 0;
+  z.top = up256((size_t)z.rows * z.spans * 4);
+  z.sums = z.top + up256((size_t)z.rows * 4);
+  z.rest = z.sums + up256((size_t)z.rows * z.parts2 * 8);
+  z.accepted = z.rest + up256((size_t)S * z.spans * 16);
+  z.bytes = z.accepted + up256((size_t)S * 4);
+  return z;
 }
 
 }  // namespace
 
-size_t verify_workspace_bytes(int, int, int) { return 256; }
+size_t verify_workspace_bytes(int S, int K, int V) { return sizes_of(S, K, V).bytes; }
 
-hipError_t verify_drafts(const VerifyArgs& a, hipStream_t s) {
-  const Rule k{(double)a.T, a.min_p > 0.f ? (double)a.T * std::log((double)a.min_p) : -(double)INFINITY};
-  hipLaunchKernelGGL(verify_kernel, dim3(a.S), dim3(kThreads), 0, s, a, k);
+hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
+  const Sizes z = sizes_of(a0.S, a0.K, a0.V);
+  Job j{};
+  j.a = a0;
+  if (a0.T == 0.f) j.a.draft = nullptr;
+  const double T = a0.T;
+  j.per_z = T > 0.0 ? 1.4426950408889634 / T : 0.0;
+  j.low = a0.min_p > 0.f ? T * std::log((double)a0.min_p) : -(double)INFINITY;
+  j.spans = z.spans;
+  j.parts2 = z.parts2;
+  j.parts3 = z.parts3;
+  j.span_max = (float*)(a0.ws + z.span_max);
+  j.top = (float*)(a0.ws + z.top);
+  j.sums = (double*)(a0.ws + z.sums);
+  j.rest = (double2*)(a0.ws + z.rest);
+  j.accepted = (int*)(a0.ws + z.accepted);
+  const long long rows = (long long)a0.S * (j.a.draft ? 2 * a0.K + 1 : a0.K + 1);
+  const int groups = (z.spans + kSpansPerWg - 1) / kSpansPerWg;
+  if (rows * groups > 0x7FFFFFFFLL || rows * z.parts2 > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(verify_max_kernel, dim3((unsigned)(rows * groups)), dim3(256), 0, s, j, groups);
+  if (T == 0.0) {
+    hipLaunchKernelGGL(verify_greedy_kernel, dim3(a0.S), dim3(256), 0, s, j);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)(rows * z.parts2)), dim3(256), 0, s, j);
+  hipLaunchKernelGGL(verify_rest_kernel, dim3((unsigned)(a0.S * z.parts3)), dim3(256), 0, s, j);
+  hipLaunchKernelGGL(verify_draw_kernel, dim3(a0.S), dim3(256), 0, s, j);
   return hipGetLastError();
 }
 
