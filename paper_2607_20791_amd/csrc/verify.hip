@@ -7,10 +7,10 @@
 // probability min(p, q) + (1 - sum min(p, q)) max(p - q, 0) / sum max(p - q, 0) = p.
 //
 // One read of all logits bounds it.  Pass 1 streams them and keeps the maximum of
-// every 1024 ids (a span): with a row's maximum its threshold is known, and
+// every 256 ids (a span): with a row's maximum its threshold is known, and
 // only spans whose maximum reaches it hold kept ids.  Those alone are read again,
 // for the rows' sums (pass 2), for the rest of p over q in the one row per sequence
-// that is drawn from (pass 3), and one span of them for the draw (pass 4).  Weights
+// that is drawn from (pass 3), and four of them for the draw (pass 4).  Weights
 // and sums are fp64: the token drawn hangs on sums of up to 2^20 weights, which fp32
 // would leave wrong in one draw of a few.  T == 0: pass 1, then the first
 // id of each row's maximum.
@@ -23,9 +23,9 @@ namespace rgd {
 
 namespace {
 
-constexpr int kSpan = 1024;      // ids per span: one wave, 16 a lane
-constexpr int kSpansPerWg = 16;  // pass 1: four waves, four spans each
-constexpr int kMaxSpans = 1024;
+constexpr int kSpan = 256;       // ids per span: one wave, four a lane
+constexpr int kSpansPerWg = 64;  // pass 1: four waves, 16 spans each
+constexpr int kMaxSpans = 4096;
 constexpr int kMaxParts = 16;    // workgroups that share a row in passes 2 and 3
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
@@ -62,7 +62,7 @@ struct Job {
   float* span_max;    // [rows][spans]
   float* top;         // [rows]
   double* sums;       // [rows][parts2]
-  double2* rest;      // [S][spans]: rest of p over q, and p, of the drawn row's listed spans
+  double2* rest;      // [S][spans]: rest of p over q, and p, of the drawn row's groups
   int* accepted;      // [S]
 };
 
@@ -85,39 +85,55 @@ RGD_DEV const float* row_logits(const VerifyArgs& a, long long r) {
   return i < drafts_of(a, s) ? a.draft + r * a.V : nullptr;
 }
 
-// This lane's ids of a span: 256 k + 4 lane + {0..3}; behind the row -inf.
-RGD_DEV void load_span(const float* z, int V, int span, f4 (&v)[4]) {
+// This lane's ids of a span, 4 lane + {0..3}; behind the row -inf.
+RGD_DEV f4 load_span(const float* z, int V, int span) {
   const int at = span * kSpan + (threadIdx.x & 63) * 4;
-  if ((span + 1) * kSpan <= V) {
+  f4 v;
+  if ((span + 1) * kSpan <= V) return *(const f4*)(z + at);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = *(const f4*)(z + at + 256 * k);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[k][e] = at + 256 * k + e < V ? z[at + 256 * k + e] : -INFINITY;
-  }
+  for (int e = 0; e < 4; ++e) v[e] = at + e < V ? z[at + e] : -INFINITY;
+  return v;
 }
 
 // ------------------------------------------------------------------ pass 1 --
+template <int CTRL, int ROWS>
+RGD_DEV float max_step(float v) {
+  const int b = __float_as_int(v);
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, ROWS, 0xf, false)));
+}
+// the maximum over the wave, in its last lane
+RGD_DEV float last_lane_max(float v) {
+  v = max_step<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
+  v = max_step<0x112, 0xf>(v);
+  v = max_step<0x114, 0xf>(v);
+  v = max_step<0x118, 0xf>(v);
+  v = max_step<0x142, 0xa>(v);  // row_bcast 15, 31
+  return max_step<0x143, 0xc>(v);
+}
+
 __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
   const long long r = blockIdx.x / groups;
-  const int first = (int)(blockIdx.x % groups) * kSpansPerWg + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int first = ((int)(blockIdx.x % groups) * 4 + (threadIdx.x >> 6)) * 16, lane = threadIdx.x & 63;
   const float* z = row_logits(j.a, r);
-  if (!z) return;
-  f4 v[4][4];
+  if (!z || first >= j.spans) return;
+  f4 v[16];
+  if ((first + 16) * kSpan <= j.a.V) {
 #pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (first + 4 * k < j.spans) load_span(z, j.a.V, first + 4 * k, v[k]);
+    for (int k = 0; k < 16; ++k) v[k] = *(const f4*)(z + (first + k) * kSpan + lane * 4);
+  } else {
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    if (first + 4 * k >= j.spans) return;
-    float m = -INFINITY;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) m = fmaxf(m, fmaxf(fmaxf(v[k][q][0], v[k][q][1]), fmaxf(v[k][q][2], v[k][q][3])));
-    m = wave_max(m);  // NaN counts as -inf: fmaxf takes the other operand
-    if (lane == 0) j.span_max[r * j.spans + first + 4 * k] = m;
+    for (int k = 0; k < 16; ++k)
+      v[k] = first + k < j.spans ? load_span(z, j.a.V, first + k) : f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   }
+  float mine = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    // NaN counts as -inf: fmaxf takes the other operand
+    const float m = last_lane_max(fmaxf(fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])), -INFINITY));
+    const float s = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), 63));
+    mine = lane == k ? s : mine;
+  }
+  if (lane < 16 && first + lane < j.spans) j.span_max[r * j.spans + first + lane] = mine;
 }
 
 // The lowest kept logit of a row of maximum `top`: the smallest float z with
@@ -163,14 +179,15 @@ RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r) {
 // of 256: list[0 .. n).  Returns n.  red: 4 ints.
 RGD_DEV int list_spans(const Job& j, long long r, float thr, unsigned short* list, int* red) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  int mine = 0;
-  bool hit[4];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {  // four neighbouring spans a thread
-    const int sp = 4 * t + k;
-    hit[k] = sp < j.spans && j.span_max[r * j.spans + sp] >= thr;
-    mine += hit[k];
+  const int per = (j.spans + 255) / 256;  // neighbouring spans a thread, at most 16
+  const float* m = j.span_max + r * j.spans;
+  unsigned hits = 0;
+#pragma unroll 4
+  for (int k = 0; k < per; ++k) {
+    const int sp = per * t + k;
+    hits |= (m[min(sp, j.spans - 1)] >= thr && sp < j.spans) ? 1u << k : 0u;
   }
+  const int mine = __popc(hits);
   int incl = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -186,11 +203,39 @@ RGD_DEV int list_spans(const Job& j, long long r, float thr, unsigned short* lis
     at += k < w ? red[k] : 0;
     n += red[k];
   }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (hit[k]) list[at++] = (unsigned short)(4 * t + k);
+  for (; hits; hits &= hits - 1) list[at++] = (unsigned short)(per * t + __builtin_ctz(hits));
   __syncthreads();
   return n;
+}
+
+// Listed spans are taken four at a time (a group), one group a wave.
+constexpr int kGroup = 4;
+
+RGD_DEV void load_group(const float* z, int V, const unsigned short* list, int n, int group, f4 (&v)[kGroup]) {
+#pragma unroll
+  for (int k = 0; k < kGroup; ++k) v[k] = load_span(z, V, list[min(group * kGroup + k, n - 1)]);
+}
+
+// Bit 4 k + e: v[k][e] is kept (and the group has a span k).
+RGD_DEV unsigned kept_bits(const f4 (&v)[kGroup], float thr, int spans_left) {
+  unsigned m = 0;
+#pragma unroll
+  for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) m |= v[k][e] >= thr && k < spans_left ? 1u << (4 * k + e) : 0u;
+  return m;
+}
+
+// v[i / 4][i % 4] by selects
+RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
+  float a[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float lo = i & 1 ? v[k][1] : v[k][0], hi = i & 1 ? v[k][3] : v[k][2];
+    a[k] = i & 2 ? hi : lo;
+  }
+  const float lo = i & 4 ? a[1] : a[0], hi = i & 4 ? a[3] : a[2];
+  return i & 8 ? hi : lo;
 }
 
 // ------------------------------------------------------------------ pass 2 --
@@ -204,22 +249,21 @@ __global__ __launch_bounds__(256) void verify_sum_kernel(Job j) {
   const int part = (int)(blockIdx.x % j.parts2), w = threadIdx.x >> 6;
   const float* z = row_logits(j.a, r);
   if (!z) return;
-  float m = -INFINITY;
-  for (int i = threadIdx.x; i < j.spans; i += 256) m = fmaxf(m, j.span_max[r * j.spans + i]);
-  m = block_max_once(m, redf);
-  if (part == 0 && threadIdx.x == 0) j.top[r] = m;
-  if (!finite_top(m)) return;
-  const float thr = threshold(m, j.low);
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < j.spans; i += 256) top = fmaxf(top, j.span_max[r * j.spans + i]);
+  top = block_max_once(top, redf);
+  if (part == 0 && threadIdx.x == 0) j.top[r] = top;
+  if (!finite_top(top)) return;
+  const float thr = threshold(top, j.low);
   const int n = list_spans(j, r, thr, list, red);
   double sum = 0.0;
-  for (int i = part * 4 + w; i < n; i += 4 * j.parts2) {
-    f4 v[4];
-    load_span(z, j.a.V, list[i], v);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v[k][e] >= thr) sum += exp2_f64(((double)v[k][e] - (double)m) * j.per_z);
+  for (int g = part * 4 + w; g * kGroup < n; g += 4 * j.parts2) {
+    f4 v[kGroup];
+    load_group(z, j.a.V, list, n, g, v);
+    // a kept logit per lane and turn: few lanes have more than one or two
+    for (unsigned m = kept_bits(v, thr, n - g * kGroup); m; m &= m - 1)
+      sum += exp2_f64(((double)pick(v, __builtin_ctz(m)) - (double)top) * j.per_z);
   }
   sum = wave_sum_f64(sum);
   if ((threadIdx.x & 63) == 0) redd[w] = sum;
@@ -292,26 +336,20 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   const Draw d = draw_of(j, s, acc);
   if (!finite_top(d.p.top)) return;
   const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, red);
-  for (int i = part * 4 + w; i < n; i += 4 * j.parts3) {
-    f4 v[4], q[4];
-    const int sp = list[i];
-    load_span(d.p.z, a.V, sp, v);
-    if (d.minus_q) load_span(d.q.z, a.V, sp, q);
-    else
-      for (int k = 0; k < 4; ++k) q[k] = v[k];
+  for (int g = part * 4 + w; g * kGroup < n; g += 4 * j.parts3) {
+    f4 v[kGroup], q[kGroup] = {};
+    load_group(d.p.z, a.V, list, n, g, v);
+    if (d.minus_q) load_group(d.q.z, a.V, list, n, g, q);
     double2 sum{0.0, 0.0};
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (v[k][e] >= d.p.thr) {
-          const double2 x = d.rest(v[k][e], q[k][e], sp * kSpan + 256 * k + (t & 63) * 4 + e);
-          sum.x += x.x;
-          sum.y += x.y;
-        }
+    for (unsigned m = kept_bits(v, d.p.thr, n - g * kGroup); m; m &= m - 1) {
+      const int i = __builtin_ctz(m);
+      const double2 x = d.rest(pick(v, i), pick(q, i), list[g * kGroup + i / 4] * kSpan + (t & 63) * 4 + i % 4);
+      sum.x += x.x;
+      sum.y += x.y;
+    }
     sum.x = wave_sum_f64(sum.x);
     sum.y = wave_sum_f64(sum.y);
-    if ((t & 63) == 0) j.rest[(long long)s * j.spans + i] = sum;
+    if ((t & 63) == 0) j.rest[(long long)s * j.spans + g] = sum;
   }
 }
 
@@ -346,7 +384,7 @@ RGD_DEV int block_min_i(int v, int* red) {
   return min(min(red[0], red[1]), min(red[2], red[3]));
 }
 
-// The draw: the span, then the id, whose running sum first exceeds u times the total;
+// The draw: the group, then the id, whose running sum first exceeds u times the total;
 // where rounding leaves none, the last one with weight.
 __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   __shared__ double red[4];
@@ -365,11 +403,12 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
     return;
   }
   const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, redi);
+  const int groups = (n + kGroup - 1) / kGroup;  // at most 1024
   double2 part[4];
   double mine[2] = {0.0, 0.0}, total[2], before[2];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    part[k] = 4 * t + k < n ? j.rest[(long long)s * j.spans + 4 * t + k] : double2{0.0, 0.0};
+    part[k] = 4 * t + k < groups ? j.rest[(long long)s * j.spans + 4 * t + k] : double2{0.0, 0.0};
     mine[0] += part[k].x;
     mine[1] += part[k].y;
   }
@@ -395,14 +434,16 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   for (int k = 0; k < 4; ++k)
     if (hit == 4 * t + k) sh_before = at[k];
   __syncthreads();
-  // four ids a thread
-  const int sp = list[hit], id0 = sp * kSpan + 4 * t;
+  // one span a wave, four ids a thread
+  const int sp = hit * kGroup + (t >> 6);
+  const bool have = sp < n;
+  const int id0 = list[have ? sp : 0] * kSpan + 4 * (t & 63);
   run = sh_before;
   double x[4], sum = 0.0, unused;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[e] = 0.0;
-    if (id0 + e < a.V) {
+    if (have && id0 + e < a.V) {
       const float zp = d.p.z[id0 + e];
       const double2 v = d.rest(zp, d.minus_q ? d.q.z[id0 + e] : zp, id0 + e);
       x[e] = use ? v.y : v.x;
@@ -444,13 +485,10 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sp = min(sp, __shfl_xor(sp, o, 64));
     if (finite_top(top)) {
-      f4 v[4];
-      load_span(a.target + r * a.V, a.V, sp, v);
+      const f4 v = load_span(a.target + r * a.V, a.V, sp);
 #pragma unroll
-      for (int k = 3; k >= 0; --k)
-#pragma unroll
-        for (int e = 3; e >= 0; --e)
-          if (v[k][e] == top) id = sp * kSpan + 256 * k + lane * 4 + e;
+      for (int e = 3; e >= 0; --e)
+        if (v[e] == top) id = sp * kSpan + lane * 4 + e;
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) id = min(id, __shfl_xor(id, o, 64));
     } else {
