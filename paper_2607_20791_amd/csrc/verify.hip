@@ -55,15 +55,18 @@ RGD_DEV double wave_sum_f64(double v) {
   return v;
 }
 
+struct DrawInfo;
+
 struct Job {
   VerifyArgs a;
   double per_z, low;  // log2(e) / T; kept: z - max >= low
-  int spans, parts2, parts3;
+  int spans, groups, parts2, parts3;
   float* span_max;    // [rows][spans]
   float* top;         // [rows]
   double* sums;       // [rows][parts2]
-  double2* rest;      // [S][spans]: rest of p over q, and p, of the drawn row's groups
-  int* accepted;      // [S]
+  double2* rest;      // [S][groups]: rest of p over q, and p, of the drawn row's groups
+  DrawInfo* draws;             // [S]
+  unsigned short* listed;      // [S][spans]: the drawn row's spans that reach its threshold
 };
 
 // Rows: the target's S (K + 1), then the drafts' S K.
@@ -160,53 +163,69 @@ struct Dist {
 
 RGD_DEV bool finite_top(float t) { return t > -INFINITY && t < INFINITY; }
 
+// Row r, from pass 2's maximum and sums, all on their way at once.  A row without a
+// finite maximum keeps nothing.
 RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r) {
   Dist d;
   d.z = logits;
   d.top = j.top[r];
-  d.thr = INFINITY;  // no distribution: nothing kept
   d.per_z = j.per_z;
-  d.scale = 0.0;
-  if (!finite_top(d.top)) return d;
-  d.thr = threshold(d.top, j.low);
-  double W = 0.0;
-  for (int k = 0; k < j.parts2; ++k) W += j.sums[r * j.parts2 + k];
-  d.scale = 1.0 / W;
+  double part[kMaxParts], W = 0.0;
+#pragma unroll
+  for (int k = 0; k < kMaxParts; ++k) part[k] = j.sums[r * j.parts2 + min(k, j.parts2 - 1)];
+#pragma unroll
+  for (int k = 0; k < kMaxParts; ++k) W += k < j.parts2 ? part[k] : 0.0;
+  const bool alive = finite_top(d.top);
+  d.thr = alive ? threshold(d.top, j.low) : INFINITY;
+  d.scale = alive ? 1.0 / W : 0.0;
   return d;
 }
 
-// The spans of row r whose maximum reaches thr, in order, by the whole workgroup
-// of 256: list[0 .. n).  Returns n.  red: 4 ints.
-RGD_DEV int list_spans(const Job& j, long long r, float thr, unsigned short* list, int* red) {
-  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int per = (j.spans + 255) / 256;  // neighbouring spans a thread, at most 16
-  const float* m = j.span_max + r * j.spans;
-  unsigned hits = 0;
-#pragma unroll 4
-  for (int k = 0; k < per; ++k) {
-    const int sp = per * t + k;
-    hits |= (m[min(sp, j.spans - 1)] >= thr && sp < j.spans) ? 1u << k : 0u;
-  }
-  const int mine = __popc(hits);
-  int incl = mine;
+// The span maxima of a row, `per` neighbouring ones a thread of 256.
+struct SpanMax {
+  float m[kMaxSpans / 256];
+  int per;
+  RGD_DEV void load(const Job& j, long long r) {
+    per = (j.spans + 255) / 256;
+    const float* row = j.span_max + r * j.spans;
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int v = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += v;
+    for (int k = 0; k < kMaxSpans / 256; ++k)
+      if (k < per) m[k] = row[min(per * (int)threadIdx.x + k, j.spans - 1)];  // (the last one twice does no harm to a maximum)
   }
-  __syncthreads();
-  if (lane == 63) red[w] = incl;
-  __syncthreads();
-  int at = incl - mine, n = 0;
+  RGD_DEV float top() const {
+    float t = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    at += k < w ? red[k] : 0;
-    n += red[k];
+    for (int k = 0; k < kMaxSpans / 256; ++k)
+      if (k < per) t = fmaxf(t, m[k]);
+    return t;
   }
-  for (; hits; hits &= hits - 1) list[at++] = (unsigned short)(per * t + __builtin_ctz(hits));
-  __syncthreads();
-  return n;
-}
+  // the spans that reach thr, in order, by the whole workgroup: list[0 .. n); red: 4 ints
+  RGD_DEV int list(const Job& j, float thr, unsigned short* out, int* red) const {
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    unsigned hits = 0;
+#pragma unroll
+    for (int k = 0; k < kMaxSpans / 256; ++k)
+      if (k < per) hits |= m[k] >= thr && per * t + k < j.spans ? 1u << k : 0u;
+    const int mine = __popc(hits);
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int v = __shfl_up(incl, o, 64);
+      if (lane >= o) incl += v;
+    }
+    if (lane == 63) red[w] = incl;
+    __syncthreads();
+    int at = incl - mine, n = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      at += k < w ? red[k] : 0;
+      n += red[k];
+    }
+    for (; hits; hits &= hits - 1) out[at++] = (unsigned short)(per * t + __builtin_ctz(hits));
+    __syncthreads();
+    return n;
+  }
+};
 
 // Listed spans are taken four at a time (a group), one group a wave.
 constexpr int kGroup = 4;
@@ -247,23 +266,26 @@ __global__ __launch_bounds__(256) void verify_sum_kernel(Job j) {
   __shared__ unsigned short list[kMaxSpans];
   const long long r = blockIdx.x / j.parts2;
   const int part = (int)(blockIdx.x % j.parts2), w = threadIdx.x >> 6;
+  SpanMax spans;
+  spans.load(j, r);
   const float* z = row_logits(j.a, r);
   if (!z) return;
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < j.spans; i += 256) top = fmaxf(top, j.span_max[r * j.spans + i]);
-  top = block_max_once(top, redf);
+  const float top = block_max_once(spans.top(), redf);
   if (part == 0 && threadIdx.x == 0) j.top[r] = top;
   if (!finite_top(top)) return;
   const float thr = threshold(top, j.low);
-  const int n = list_spans(j, r, thr, list, red);
+  const int n = spans.list(j, thr, list, red);
   double sum = 0.0;
-  for (int g = part * 4 + w; g * kGroup < n; g += 4 * j.parts2) {
-    f4 v[kGroup];
-    load_group(z, j.a.V, list, n, g, v);
+  const int step = 4 * j.parts2, first = part * 4 + w;
+  f4 v[kGroup], next[kGroup];
+  if (first * kGroup < n) load_group(z, j.a.V, list, n, first, v);
+  for (int g = first; g * kGroup < n; g += step) {
+    if ((g + step) * kGroup < n) load_group(z, j.a.V, list, n, g + step, next);
     // a kept logit per lane and turn: few lanes have more than one or two
     for (unsigned m = kept_bits(v, thr, n - g * kGroup); m; m &= m - 1)
       sum += exp2_f64(((double)pick(v, __builtin_ctz(m)) - (double)top) * j.per_z);
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) v[k] = next[k];
   }
   sum = wave_sum_f64(sum);
   if ((threadIdx.x & 63) == 0) redd[w] = sum;
@@ -273,11 +295,28 @@ __global__ __launch_bounds__(256) void verify_sum_kernel(Job j) {
 
 // ------------------------------------------------------------------ pass 3 --
 // What one sequence draws from.
+struct DrawInfo {
+  float top[2], thr[2];  // of p and q
+  double scale[2];
+  int accepted;
+  int without;  // the id that is left out (a certain draft), or -1
+  int minus_q;
+  int n;        // listed spans; 0: no distribution
+};
+
 struct Draw {
   Dist p, q;
-  int at;         // accepted drafts
-  int without;    // the id that is left out (a certain draft), or -1
+  int without;
   bool minus_q;
+  RGD_DEV Draw(const Job& j, int s, const DrawInfo& i) {
+    const VerifyArgs& a = j.a;
+    p = Dist{a.target + target_row(a, s, i.accepted) * a.V, i.top[0], i.thr[0], j.per_z, i.scale[0]};
+    minus_q = i.minus_q;
+    q = p;
+    if (minus_q) q = Dist{a.draft + ((long long)s * a.K + i.accepted) * a.V, i.top[1], i.thr[1], j.per_z, i.scale[1]};
+    without = i.without;
+  }
+  // (the rest of p over q, p) of one id
   RGD_DEV double2 rest(float zp, float zq, int id) const {
     const double x = p.p(zp);
     double r = x;
@@ -287,59 +326,60 @@ struct Draw {
   }
 };
 
-RGD_DEV Draw draw_of(const Job& j, int s, int accepted) {
-  const VerifyArgs& a = j.a;
-  Draw d;
-  d.at = accepted;
-  const long long r = target_row(a, s, accepted);
-  d.p = dist_of(j, a.target + r * a.V, r);
-  const bool refused = accepted < drafts_of(a, s);
-  d.minus_q = refused && a.draft;
-  d.without = refused && !a.draft ? a.tokens[(long long)s * a.K + accepted] : -1;
-  d.q = d.p;
-  if (d.minus_q) {
-    const long long x = (long long)s * a.K + accepted;
-    d.q = dist_of(j, a.draft + x * a.V, draft_row(a, s, accepted));
-  }
-  return d;
-}
-
 // Accepted drafts of a sequence, one draft a thread (K <= 255), then the rest of the
 // drawn row in this part's spans.
 __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
+  __shared__ DrawInfo info;
   const VerifyArgs& a = j.a;
   const int s = blockIdx.x / j.parts3, part = blockIdx.x % j.parts3, t = threadIdx.x, w = t >> 6;
+  const int id = t < a.K ? a.tokens[(long long)s * a.K + t] : -1;
   const int nd = drafts_of(a, s);
   bool ok = true;
-  if (t < nd) {
-    const int id = a.tokens[(long long)s * a.K + t];
-    ok = false;
-    if ((unsigned)id < (unsigned)a.V) {
-      const long long r = target_row(a, s, t), x = (long long)s * a.K + t;
-      const Dist p = dist_of(j, a.target + r * a.V, r);
-      const double px = p.p(p.z[id]);
-      double qx = 1.0;
-      if (a.draft) {
-        const Dist q = dist_of(j, a.draft + x * a.V, draft_row(a, s, t));
-        qx = q.p(q.z[id]);
-      }
-      ok = (double)a.u[(long long)s * (a.K + 1) + t] * qx < px;
+  DrawInfo mine{};
+  if (t <= nd) {  // row nd: no draft to refuse
+    const bool inside = (unsigned)id < (unsigned)a.V, drafted = t < nd;
+    const long long r = target_row(a, s, t);
+    const float* zp = a.target + r * a.V;
+    const float xp = zp[inside ? id : 0];
+    const Dist p = dist_of(j, zp, r);
+    Dist q = p;
+    double qx = 1.0;
+    if (a.draft && drafted) {
+      const float* zq = a.draft + ((long long)s * a.K + t) * a.V;
+      const float xq = zq[inside ? id : 0];
+      q = dist_of(j, zq, draft_row(a, s, t));
+      qx = q.p(xq);
     }
+    if (drafted) ok = inside && (double)a.u[(long long)s * (a.K + 1) + t] * qx < p.p(xp);
+    mine = DrawInfo{{p.top, q.top}, {p.thr, q.thr}, {p.scale, q.scale}, t, drafted && !a.draft ? id : -1,
+                    drafted && a.draft, 0};
   }
   const unsigned long long no = __ballot(!ok);
   if ((t & 63) == 0) first[w] = no ? 64 * w + __builtin_ctzll(no) : 0x7FFFFFFF;
   __syncthreads();
   const int acc = min(min(min(first[0], first[1]), min(first[2], first[3])), nd);
-  if (part == 0 && t == 0) j.accepted[s] = acc;
-  const Draw d = draw_of(j, s, acc);
-  if (!finite_top(d.p.top)) return;
-  const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, red);
-  for (int g = part * 4 + w; g * kGroup < n; g += 4 * j.parts3) {
-    f4 v[kGroup], q[kGroup] = {};
-    load_group(d.p.z, a.V, list, n, g, v);
-    if (d.minus_q) load_group(d.q.z, a.V, list, n, g, q);
+  SpanMax spans;
+  spans.load(j, target_row(a, s, acc));
+  if (t == acc) info = mine;
+  __syncthreads();
+  DrawInfo di = info;
+  di.n = finite_top(di.top[0]) ? spans.list(j, di.thr[0], list, red) : 0;
+  if (part == 0) {  // for pass 4
+    for (int i = t; i < di.n; i += 256) j.listed[(long long)s * j.spans + i] = list[i];
+    if (t == 0) j.draws[s] = di;
+  }
+  const Draw d(j, s, di);
+  const int step = 4 * j.parts3, g0 = part * 4 + w, n = di.n;
+  f4 v[kGroup], q[kGroup] = {}, vn[kGroup], qn[kGroup] = {};
+  auto load = [&](int g, f4 (&x)[kGroup], f4 (&y)[kGroup]) {
+    load_group(d.p.z, a.V, list, n, g, x);
+    if (d.minus_q) load_group(d.q.z, a.V, list, n, g, y);
+  };
+  if (g0 * kGroup < n) load(g0, v, q);
+  for (int g = g0; g * kGroup < n; g += step) {
+    if ((g + step) * kGroup < n) load(g + step, vn, qn);
     double2 sum{0.0, 0.0};
     for (unsigned m = kept_bits(v, d.p.thr, n - g * kGroup); m; m &= m - 1) {
       const int i = __builtin_ctz(m);
@@ -349,7 +389,12 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
     }
     sum.x = wave_sum_f64(sum.x);
     sum.y = wave_sum_f64(sum.y);
-    if ((t & 63) == 0) j.rest[(long long)s * j.spans + g] = sum;
+    if ((t & 63) == 0) j.rest[(long long)s * j.groups + g] = sum;
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) {
+      v[k] = vn[k];
+      q[k] = qn[k];
+    }
   }
 }
 
@@ -389,33 +434,33 @@ RGD_DEV int block_min_i(int v, int* red) {
 __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   __shared__ double red[4];
   __shared__ int redi[4];
-  __shared__ unsigned short list[kMaxSpans];
   __shared__ double sh_before;
   const VerifyArgs& a = j.a;
   const int s = blockIdx.x, t = threadIdx.x;
-  const int acc = j.accepted[s];
+  const DrawInfo di = j.draws[s];
+  const int acc = di.accepted, n = di.n;
+  const float u = a.u[(long long)s * (a.K + 1) + a.K];
   int* out = a.out + (long long)s * (a.K + 1);
   if (t == 0) a.n_accepted[s] = acc;
   if (t <= a.K && t != acc) out[t] = t < acc ? a.tokens[(long long)s * a.K + t] : -1;
-  const Draw d = draw_of(j, s, acc);
-  if (!finite_top(d.p.top)) {
+  if (n == 0) {
     if (t == 0) out[acc] = -1;
     return;
   }
-  const int n = list_spans(j, target_row(a, s, acc), d.p.thr, list, redi);
+  const Draw d(j, s, di);
   const int groups = (n + kGroup - 1) / kGroup;  // at most 1024
   double2 part[4];
   double mine[2] = {0.0, 0.0}, total[2], before[2];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    part[k] = 4 * t + k < groups ? j.rest[(long long)s * j.spans + 4 * t + k] : double2{0.0, 0.0};
+    part[k] = 4 * t + k < groups ? j.rest[(long long)s * j.groups + 4 * t + k] : double2{0.0, 0.0};
     mine[0] += part[k].x;
     mine[1] += part[k].y;
   }
   before[0] = block_scan_f64(mine[0], red, total[0]);
   before[1] = block_scan_f64(mine[1], red, total[1]);
   const int use = total[0] > 0.0 ? 0 : 1;  // nothing left by rounding: p itself
-  const double goal = (double)a.u[(long long)s * (a.K + 1) + a.K] * total[use];
+  const double goal = (double)u * total[use];
   double run = before[use], at[4];
   int hit = 0x7FFFFFFF, last = 0;
 #pragma unroll
@@ -437,7 +482,7 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   // one span a wave, four ids a thread
   const int sp = hit * kGroup + (t >> 6);
   const bool have = sp < n;
-  const int id0 = list[have ? sp : 0] * kSpan + 4 * (t & 63);
+  const int id0 = j.listed[(long long)s * j.spans + (have ? sp : 0)] * kSpan + 4 * (t & 63);
   run = sh_before;
   double x[4], sum = 0.0, unused;
 #pragma unroll
@@ -507,8 +552,8 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
 
 struct Sizes {
   long long rows;
-  int spans, parts2, parts3;
-  size_t span_max, top, sums, rest, accepted, bytes;
+  int spans, groups, parts2, parts3;
+  size_t span_max, top, sums, rest, draws, listed, bytes;
 };
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -518,14 +563,16 @@ Sizes sizes_of(int S, int K, int V) {
   Sizes z;
   z.rows = (long long)S * (2 * K + 1);
   z.spans = (V + kSpan - 1) / kSpan;
+  z.groups = (z.spans + kGroup - 1) / kGroup;
   z.parts2 = (int)std::min<long long>(kMaxParts, (2047 + z.rows) / z.rows);
   z.parts3 = std::min(kMaxParts, (1023 + S) / S);
   z.span_max = 0;
   z.top = up256((size_t)z.rows * z.spans * 4);
   z.sums = z.top + up256((size_t)z.rows * 4);
   z.rest = z.sums + up256((size_t)z.rows * z.parts2 * 8);
-  z.accepted = z.rest + up256((size_t)S * z.spans * 16);
-  z.bytes = z.accepted + up256((size_t)S * 4);
+  z.draws = z.rest + up256((size_t)S * z.groups * 16);
+  z.listed = z.draws + up256((size_t)S * sizeof(DrawInfo));
+  z.bytes = z.listed + up256((size_t)S * z.spans * 2);
   return z;
 }
 
@@ -542,13 +589,15 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.per_z = T > 0.0 ? 1.4426950408889634 / T : 0.0;
   j.low = a0.min_p > 0.f ? T * std::log((double)a0.min_p) : -(double)INFINITY;
   j.spans = z.spans;
+  j.groups = z.groups;
   j.parts2 = z.parts2;
   j.parts3 = z.parts3;
   j.span_max = (float*)(a0.ws + z.span_max);
   j.top = (float*)(a0.ws + z.top);
   j.sums = (double*)(a0.ws + z.sums);
   j.rest = (double2*)(a0.ws + z.rest);
-  j.accepted = (int*)(a0.ws + z.accepted);
+  j.draws = (DrawInfo*)(a0.ws + z.draws);
+  j.listed = (unsigned short*)(a0.ws + z.listed);
   const long long rows = (long long)a0.S * (j.a.draft ? 2 * a0.K + 1 : a0.K + 1);
   const int groups = (z.spans + kSpansPerWg - 1) / kSpansPerWg;
   if (rows * groups > 0x7FFFFFFFLL || rows * z.parts2 > 0x7FFFFFFFLL) return hipErrorInvalidValue;
