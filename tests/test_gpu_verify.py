@@ -65,6 +65,13 @@ def test_against_the_oracle(rgd, V, T, min_p):
     _compare(rgd, target, None, target[:, :K].argmax(-1), None, T, min_p, u)
 
 
+@pytest.mark.parametrize("V", [262144, 262145, 1 << 20])
+def test_the_largest_vocabularies(rgd, V):
+    for T, min_p in ((1.0, 0.05), (0.0, 0.0), (2.0, 0.0)):
+        target, draft, tokens, u = _inputs(V % 1000, 2, 1, V, T, min_p=min_p)
+        _compare(rgd, target, draft, tokens, None, T, min_p, u)
+
+
 def test_ragged_counts_and_tokens_outside(rgd):
     target, draft, tokens, u = _inputs(3, 9, 5, 777)
     n = [0, 1, 2, 3, 4, 5, -4, 99, 5]
