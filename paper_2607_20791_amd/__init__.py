@@ -449,6 +449,13 @@ class PagedCache:
         self.pool_k, self.pool_v, self.pages, self.lens, self.refs, self.status = pool_k, pool_v, pages, lens, refs, status
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, P, H, ps, D
         self.max_seqs, self.max_pages = S, width
+        self._needs = {}  # workspace bytes by what they are for
+
+    def need(self, what, fn, *args):
+        n = self._needs.get(what)
+        if n is None:
+            n = self._needs[what] = _bytes(fn(self.ref, *args))
+        return n
 
 
 def _bytes(n):
@@ -458,7 +465,7 @@ def _bytes(n):
 
 
 def paged_workspace_bytes(cache):
-    return _bytes(lib.rgd_paged_workspace_bytes(cache.ref))
+    return cache.need("pages", lib.rgd_paged_workspace_bytes)
 
 
 def paged_select(cache, parent, keep, workspace):
@@ -496,7 +503,7 @@ def paged_append(cache, layer, k, v, n, n_new=None):
 
 
 def paged_attention_workspace_bytes(cache, n, n_heads):
-    return _bytes(lib.rgd_paged_attention_workspace_bytes(cache.ref, n, n_heads))
+    return cache.need((n, n_heads), lib.rgd_paged_attention_workspace_bytes, n, n_heads)
 
 
 def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):

@@ -37,7 +37,7 @@ namespace {
 constexpr int kStep = 32;      // positions per step of the plan
 constexpr int kMinSteps = 4;   // a run is no shorter: one step a wave
 constexpr int kItemCost = 8;   // what an item costs besides its steps, in steps
-constexpr int kMaxRuns = 512;  // two workgroups per CU
+constexpr int kMaxRuns = 512;  // two workgroups per CU; half of it where LDS or registers hold one
 constexpr int kWaves = 4;      // per workgroup
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -276,8 +276,8 @@ struct Piece {
   static constexpr int E = BF ? 8 : 4;              // consecutive positions of a lane
   static constexpr int COLS = 16 * NT;
 
-  // four tiles: the queries stay in LDS, shared by the waves
-  static constexpr bool QS = NT == 4;
+  // where registers are short the queries stay in LDS, shared by the waves
+  static constexpr bool QS = NT == 4 || (NT == 2 && sizeof(T) * D < 512);
   u32x4 q[QS ? 1 : NT][KL], k[NB][KL], v[VL];
   const u32x4* qs;
   f32x4 o[NT][VL];
@@ -405,7 +405,7 @@ struct Piece {
     else return q[t][c];
   }
 
-  // all waves, between two barriers
+  // a tile a wave, between two barriers
   RGD_DEV void stage_q(const PagedAttnArgs& a, const Item& it, u32x4* dst, int wave) const {
     const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
     const int col = min(it.qb * COLS + wave * 16 + row, cols - 1), i = col / G;
@@ -567,7 +567,7 @@ constexpr size_t slot_floats() {
 }
 
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
+__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
   using P = Piece<T, D, NT>;
   constexpr int COLS = P::COLS, LD = D + 4;
   __shared__ float part[kWaves][COLS][LD];
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void attn_run_kernel(PagedAtt
   x.start(a, it, table, wave);
   while (it.valid) {
     if (P::QS) {
-      x.stage_q(a, it, q_s, wave);
+      if (wave < NT) x.stage_q(a, it, q_s, wave);
       __syncthreads();
     }
     const Item next = walk.next(a);
@@ -711,7 +711,7 @@ int runs_for(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), cols = 16 * nt;
   const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
-  return (int)std::min(nt == 1 ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
+  return (int)std::min(nt == 1 || (nt == 2 && c.esz * c.D < 512) ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
 }
 
 template <typename T, int D, int NT>
