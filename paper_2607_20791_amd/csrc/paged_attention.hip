@@ -56,13 +56,17 @@ struct Seq {
 };
 
 template <int COLS>
-RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
+RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m) {
   Seq q;
-  q.len = paged_len(a.c, s);
-  q.m = new_tokens(a, s);
-  q.steps = max(1, (q.len + kStep - 1) / kStep);
-  q.items = a.c.Hkv * ((q.m * (a.Hq / a.c.Hkv) + COLS - 1) / COLS);
+  q.len = len;
+  q.m = m;
+  q.steps = max(1, (len + kStep - 1) / kStep);
+  q.items = a.c.Hkv * ((m * (a.Hq / a.c.Hkv) + COLS - 1) / COLS);
   return q;
+}
+template <int COLS>
+RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
+  return seq_of<COLS>(a, paged_len(a.c, s), new_tokens(a, s));
 }
 
 // Sum over the lanes up to this one (64-bit: long tables times many sequences).
@@ -85,11 +89,11 @@ RGD_DEV long long lane_value(long long v, int lane) {
   return ((long long)hi << 32) | (unsigned)lo;
 }
 
+// Units of the plan that this lane's sequence takes (none behind the last).
 template <int COLS>
-RGD_DEV long long steps_of(const PagedAttnArgs& a, int s) {
-  if (s >= a.c.S) return 0;
-  const Seq q = seq_of<COLS>(a, s);
-  return (long long)(q.steps + kItemCost) * q.items;
+RGD_DEV long long units_of(const PagedAttnArgs& a, int s, Seq& q) {
+  q = seq_of<COLS>(a, min(s, a.c.S - 1));
+  return s < a.c.S ? (long long)(q.steps + kItemCost) * q.items : 0;
 }
 
 // Floor of x / y for 0 <= x < 2^52, 0 < y (exact: the quotients here are below
@@ -100,14 +104,15 @@ struct Runs {
   long long total, length;  // units of the plan, units per run
 };
 
-// Finds the run of workgroup r (of `runs`): the sequence it starts in and the
-// steps before that one.  False: there is none.
+// Finds the run of workgroup r (of `runs`): the sequence it starts in and the units
+// before that one.  False: there is none.
 template <int COLS>
-RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& s, long long& before) {
+RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& s, Seq& sq, long long& before) {
   const int lane = threadIdx.x & 63;
-  long long u = steps_of<COLS>(a, lane), incl = wave_scan(u);
+  Seq q, more;
+  long long u = units_of<COLS>(a, lane, q), incl = wave_scan(u);
   plan.total = lane_value(incl, 63);
-  for (int s0 = 64; s0 < a.c.S; s0 += 64) plan.total += lane_value(wave_scan(steps_of<COLS>(a, s0 + lane)), 63);
+  for (int s0 = 64; s0 < a.c.S; s0 += 64) plan.total += lane_value(wave_scan(units_of<COLS>(a, s0 + lane, more)), 63);
   plan.length = max((long long)kMinSteps, quotient(plan.total + runs - 1, runs));
   const long long start = r * plan.length;
   if (start >= plan.total) return false;
@@ -118,11 +123,12 @@ RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& 
       const int l = __builtin_ctzll(hit);
       before = base + lane_value(incl - u, l);
       s = s0 + l;
+      sq = seq_of<COLS>(a, __builtin_amdgcn_readlane(q.len, l), __builtin_amdgcn_readlane(q.m, l));
       return true;
     }
     base += lane_value(incl, 63);
     s0 += 64;
-    u = steps_of<COLS>(a, s0 + lane);
+    u = units_of<COLS>(a, s0 + lane, q);
     incl = wave_scan(u);
   }
 }
@@ -578,14 +584,14 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAtt
   Runs plan;
   int s;
   long long before;
+  Walk<COLS> walk;
   Cut* cut = (Cut*)a.ws + r;
   if (threadIdx.x == 0) *cut = Cut{-1, 0, 0, 0};
-  if (!find_run<COLS>(a, r, runs, plan, s, before)) return;
+  if (!find_run<COLS>(a, r, runs, plan, s, walk.sq, before)) return;
   const long long start = r * plan.length;
-  Walk<COLS> walk;
   walk.s = uniform(s);
   walk.left = uniform((int)min(plan.length, plan.total - start));
-  walk.sq = uniform(seq_of<COLS>(a, walk.s));
+  walk.sq = uniform(walk.sq);
   walk.item = uniform((int)quotient(start - before, walk.sq.steps + kItemCost));
   walk.at = before + (long long)walk.item * (walk.sq.steps + kItemCost);
   walk.u0 = uniform((int)(start - walk.at));
