@@ -263,6 +263,15 @@ def test_attention_splits_a_long_sequence(rgd, bf16):
     _attention(x, 0, 4, 3, [3, 1, 2, 2], lse=False)
 
 
+@pytest.mark.parametrize("n", [1, 3])
+def test_attention_of_many_sequences(rgd, n):
+    """More sequences than a wave has lanes, in an uneven order."""
+    r = np.random.default_rng(n)
+    lens = (r.integers(0, 70, 700) * (r.random(700) < 0.6)).tolist() + [1200, 0, 3]
+    x = _filled(rgd, lens, hk=1, d=32, layers=1, seed=n)
+    _attention(x, 0, 2, n, None if n == 1 else r.integers(-1, 5, len(lens)))
+
+
 def test_attention_repeats_its_bits_and_does_not_need_a_clean_workspace(rgd):
     x = _filled(rgd, [700, 3, 64, 0, 1999], hk=2, d=128, seed=9)
     t = torch()
