@@ -402,14 +402,14 @@ int32_t rgd_kernel_probe_step(rgd_model* m, const float* logits, int32_t R, cons
  * [0, max_pages * page_size] counts as the nearest one inside; positions whose
  * table entry is outside [0, n_pages) are neither written nor attended to. */
 typedef struct rgd_paged_cache {
-  int32_t n_layers;
+  int32_t n_layers;   /* at most 65536 */
   int32_t n_pages;    /* at most 2^20 */
-  int32_t n_kv_heads; /* Hkv */
+  int32_t n_kv_heads; /* Hkv, at most 1024 */
   int32_t page_size;  /* positions per page: a multiple of 16, at most 4096 */
   int32_t head_dim;   /* D: 32, 64 or 128 */
   int32_t dtype;      /* rgd_dtype of K and V */
   int32_t max_seqs;   /* S, at most 65536 */
-  int32_t max_pages;  /* table entries per sequence */
+  int32_t max_pages;  /* table entries per sequence, at most 2^30 positions */
   void* pool_k;       /* dev [n_layers][n_pages][Hkv][page_size][D], as in rgd_kv_create */
   void* pool_v;       /* dev [n_layers][n_pages][Hkv][D][page_size] */
   int32_t* pages;     /* dev [S][max_pages] */
@@ -473,7 +473,7 @@ uint64_t rgd_paged_attention_workspace_bytes(const rgd_paged_cache* cache, int32
  * the log of the sum of exponentiated scores, for joining with attention over
  * other positions.  A token that sees nothing gets 0 and -inf; rows at or behind
  * n_new[s] are left as they were.  Slots behind a length and free pages may hold
- * anything.  1 <= n <= 1024, n_heads <= 1024.  Meant for few tokens: every 64
+ * anything.  1 <= n <= 1024, S * n <= 2^24, n_heads <= 1024.  Meant for few tokens: every 64
  * query vectors (tokens x query heads per KV head) of a sequence read its K and
  * V once.  Asynchronous. */
 int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,
@@ -504,9 +504,10 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * n_accepted dev int32 [S].  A draft outside [0, V) is refused.  NaN logits
  * count as -inf.  A target row whose maximum is not finite has no distribution:
  * its draft is refused and -1 stands for the drawn token; such a draft row has
- * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, T >= 0, min_p in
- * [0, 1].  Sums are taken in fp64, so that the draw is the exact one unless u[K]
- * meets the border of two tokens by 1e-11 of the total.  Asynchronous. */
+ * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, S (2 K + 1)
+ * ceil(V / 16384) <= 2^23, T >= 0, min_p in [0, 1].  Sums are taken in fp64, so
+ * that the draw is the exact one unless u[K] meets the border of two tokens by
+ * 1e-11 of the total.  Asynchronous. */
 int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t* draft_tokens,
                           const int32_t* n_draft, int32_t S, int32_t K, int32_t V, float T, float min_p,
                           const float* u, void* workspace, int32_t* out, int32_t* n_accepted, rgd_stream stream);

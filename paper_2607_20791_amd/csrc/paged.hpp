@@ -34,6 +34,7 @@ struct PagedAttnArgs {
   void* out; float* lse;
   float* ws;
 };
+bool paged_attention_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq);
 hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s);
 

@@ -96,8 +96,8 @@ RGD_DEV long long units_of(const PagedAttnArgs& a, int s, Seq& q) {
   return s < a.c.S ? (long long)(q.steps + kItemCost) * q.items : 0;
 }
 
-// Floor of x / y for 0 <= x < 2^52, 0 < y (exact: the quotients here are below
-// 2^31, so a fraction is at least 2^-31 of the divisor away from a whole number).
+// Floor of x / y for 0 <= x < 2^52, 0 < y.  Exact: a quotient that is no whole number
+// is at least 1 / y, more than 2^-52 of itself, away from the next one.
 RGD_DEV long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
 
 struct Runs {
@@ -750,6 +750,12 @@ hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
 }
 
 }  // namespace
+
+// the plan's units, whatever the lengths are, in numbers that it can count with
+bool paged_attention_fits(const PagedView& c, int n, int Hq) {
+  const int nt = tiles_for(c, n * (Hq / c.Hkv)), tiles = (n * (Hq / c.Hkv) + 16 * nt - 1) / (16 * nt);
+  return (double)c.S * c.Hkv * tiles * (std::ceil((double)c.width * c.ps / kStep) + kItemCost) < 549755813888.0;  // 2^39
+}
 
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), runs = runs_for(c, n, Hq);

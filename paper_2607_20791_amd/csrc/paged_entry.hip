@@ -54,7 +54,8 @@ const char* rows_ok(const PagedView& v, const void* p, int64_t ld, int64_t width
 const char* heads_ok(const PagedView& v, int32_t n, int32_t n_heads) {
   if (n < 1 || n > 1024) return "n must be in [1, 1024]";
   if (n_heads < 1 || n_heads > 1024 || n_heads % v.Hkv) return "n_heads must be a multiple of n_kv_heads, at most 1024";
-  if ((int64_t)v.S * n > (1 << 24)) return "too many rows";
+  if ((int64_t)v.S * n > (1 << 24)) return "max_seqs * n must be at most 2^24";
+  if (!paged_attention_fits(v, n, n_heads)) return "tables too long for so many sequences and heads";
   return nullptr;
 }
 
@@ -156,6 +157,7 @@ int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const v
 
 uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V) {
   if (S < 1 || S > 65536 || K < 1 || K > 255 || V < 2 || V > (1 << 20)) return 0;
+  if ((int64_t)S * (2 * K + 1) * ((V + 16383) / 16384) > (1 << 23)) return 0;
   return verify_workspace_bytes(S, K, V);
 }
 

@@ -68,6 +68,9 @@ def test_append_arguments(rgd):
 def test_attention_arguments(rgd):
     lib, d = rgd.lib, _desc(rgd)
     assert lib.rgd_paged_attention_workspace_bytes(d, 1, 4) > 0
+    huge = _desc(rgd, max_seqs=65536, max_pages=1 << 26, n_kv_heads=1024)
+    assert lib.rgd_paged_attention_workspace_bytes(huge, 1, 1024) == 0 and b"tables" in lib.rgd_last_error()
+    assert lib.rgd_paged_attention_workspace_bytes(_desc(rgd, max_seqs=65536), 257, 4) == 0
     for n, h in ((0, 4), (1025, 4), (1, 0), (1, 3), (1, 1026)):
         assert lib.rgd_paged_attention_workspace_bytes(d, n, h) == 0
 
@@ -82,7 +85,7 @@ def test_attention_arguments(rgd):
 
 def test_verify_arguments(rgd):
     lib = rgd.lib
-    for s, k, v in ((0, 4, 100), (65537, 4, 100), (1, 0, 100), (1, 256, 100), (1, 4, 1), (1, 4, (1 << 20) + 1)):
+    for s, k, v in ((65536, 255, 32), (65536, 64, 16385), (0, 4, 100), (65537, 4, 100), (1, 0, 100), (1, 256, 100), (1, 4, 1), (1, 4, (1 << 20) + 1)):
         assert lib.rgd_verify_workspace_bytes(s, k, v) == 0
     assert lib.rgd_verify_workspace_bytes(2, 4, 101) > 0
 
