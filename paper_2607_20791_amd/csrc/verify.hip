@@ -26,7 +26,9 @@ namespace {
 constexpr int kSpan = 256;       // ids per span: one wave, four a lane
 constexpr int kSpansPerWg = 64;  // pass 1: four waves, 16 spans each
 constexpr int kMaxSpans = 4096;
-constexpr int kMaxParts = 16;    // workgroups that share a row in passes 2 and 3
+constexpr int kChunk = 4096;     // ids of a wave in pass 1
+constexpr int kPart = 32;        // spans of a wave in pass 2
+constexpr int kMaxParts = 16;    // workgroups that share a row in pass 3
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
 
@@ -60,8 +62,9 @@ struct DrawInfo;
 struct Job {
   VerifyArgs a;
   double per_z, low;  // log2(e) / T; kept: z - max >= low
-  int spans, groups, parts2, parts3;
+  int spans, chunks, groups, parts2, parts3;
   float* span_max;    // [rows][spans]
+  float* chunk_max;   // [rows][chunks]
   float* top;         // [rows]
   double* sums;       // [rows][parts2]
   double2* rest;      // [S][groups]: rest of p over q, and p, of the drawn row's groups
@@ -137,6 +140,8 @@ __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
     mine = lane == k ? s : mine;
   }
   if (lane < 16 && first + lane < j.spans) j.span_max[r * j.spans + first + lane] = mine;
+  mine = last_lane_max(mine);
+  if (lane == 63) j.chunk_max[r * j.chunks + first * kSpan / kChunk] = mine;
 }
 
 // The lowest kept logit of a row of maximum `top`: the smallest float z with
@@ -163,18 +168,12 @@ struct Dist {
 
 RGD_DEV bool finite_top(float t) { return t > -INFINITY && t < INFINITY; }
 
-// Row r, from pass 2's maximum and sums, all on their way at once.  A row without a
-// finite maximum keeps nothing.
-RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r) {
+// Row r, of kept sum W.  A row without a finite maximum keeps nothing.
+RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r, double W) {
   Dist d;
   d.z = logits;
   d.top = j.top[r];
   d.per_z = j.per_z;
-  double part[kMaxParts], W = 0.0;
-#pragma unroll
-  for (int k = 0; k < kMaxParts; ++k) part[k] = j.sums[r * j.parts2 + min(k, j.parts2 - 1)];
-#pragma unroll
-  for (int k = 0; k < kMaxParts; ++k) W += k < j.parts2 ? part[k] : 0.0;
   const bool alive = finite_top(d.top);
   d.thr = alive ? threshold(d.top, j.low) : INFINITY;
   d.scale = alive ? 1.0 / W : 0.0;
@@ -191,13 +190,6 @@ struct SpanMax {
 #pragma unroll
     for (int k = 0; k < kMaxSpans / 256; ++k)
       if (k < per) m[k] = row[min(per * (int)threadIdx.x + k, j.spans - 1)];  // (the last one twice does no harm to a maximum)
-  }
-  RGD_DEV float top() const {
-    float t = -INFINITY;
-#pragma unroll
-    for (int k = 0; k < kMaxSpans / 256; ++k)
-      if (k < per) t = fmaxf(t, m[k]);
-    return t;
   }
   // the spans that reach thr, in order, by the whole workgroup: list[0 .. n); red: 4 ints
   RGD_DEV int list(const Job& j, float thr, unsigned short* out, int* red) const {
@@ -258,39 +250,55 @@ RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
 }
 
 // ------------------------------------------------------------------ pass 2 --
-// A row's maximum and this part's share of its kept sum.
-__global__ __launch_bounds__(256) void verify_sum_kernel(Job j) {
-  __shared__ float redf[4];
-  __shared__ int red[4];
-  __shared__ double redd[4];
-  __shared__ unsigned short list[kMaxSpans];
-  const long long r = blockIdx.x / j.parts2;
-  const int part = (int)(blockIdx.x % j.parts2), w = threadIdx.x >> 6;
-  SpanMax spans;
-  spans.load(j, r);
+// A row's maximum, from those of its chunks, and the kept sum of kPart of its spans, by
+// one wave.  Rows differ in kept ids by a factor of a hundred: small parts share that
+// out (64 rows of 152064 ids of 60 to 4600 kept ones each, all nine rows of them: P2NEW us, against 35 for
+// workgroups that put a row's spans in a list first).
+__global__ __launch_bounds__(256) void verify_sum_kernel(Job j, long long waves) {
+  const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (wave >= waves) return;
+  const long long r = wave / j.parts2;
+  const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, sp = part * kPart + lane;
+  float top = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 4; ++k)  // at most 256 chunks
+    if (64 * k < j.chunks) top = fmaxf(top, j.chunk_max[r * j.chunks + min(64 * k + lane, j.chunks - 1)]);
+  const bool mine = lane < kPart && sp < j.spans;
+  const float m = j.span_max[r * j.spans + min(sp, j.spans - 1)];
   const float* z = row_logits(j.a, r);
   if (!z) return;
-  const float top = block_max_once(spans.top(), redf);
-  if (part == 0 && threadIdx.x == 0) j.top[r] = top;
+  top = wave_max(top);
+  if (part == 0 && lane == 0) j.top[r] = top;
   if (!finite_top(top)) return;
   const float thr = threshold(top, j.low);
-  const int n = spans.list(j, thr, list, red);
+  unsigned long long todo = __ballot(mine && m >= thr);
+  // up to four spans at a time, the next ones on their way
+  auto take = [&](f4 (&v)[kGroup]) {
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) {
+      if (todo) {
+        v[k] = load_span(z, j.a.V, part * kPart + __builtin_ctzll(todo));
+        todo &= todo - 1;
+      } else {
+        v[k] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // weighs nothing
+      }
+    }
+  };
   double sum = 0.0;
-  const int step = 4 * j.parts2, first = part * 4 + w;
   f4 v[kGroup], next[kGroup];
-  if (first * kGroup < n) load_group(z, j.a.V, list, n, first, v);
-  for (int g = first; g * kGroup < n; g += step) {
-    if ((g + step) * kGroup < n) load_group(z, j.a.V, list, n, g + step, next);
+  bool more = todo != 0;
+  if (more) take(v);
+  while (more) {
+    more = todo != 0;
+    if (more) take(next);
     // a kept logit per lane and turn: few lanes have more than one or two
-    for (unsigned m = kept_bits(v, thr, n - g * kGroup); m; m &= m - 1)
-      sum += exp2_f64(((double)pick(v, __builtin_ctz(m)) - (double)top) * j.per_z);
+    for (unsigned b = kept_bits(v, thr, kGroup); b; b &= b - 1)
+      sum += exp2_f64(((double)pick(v, __builtin_ctz(b)) - (double)top) * j.per_z);
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) v[k] = next[k];
   }
   sum = wave_sum_f64(sum);
-  if ((threadIdx.x & 63) == 0) redd[w] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) j.sums[r * j.parts2 + part] = ((redd[0] + redd[1]) + redd[2]) + redd[3];
+  if (lane == 0) j.sums[wave] = sum;
 }
 
 // ------------------------------------------------------------------ pass 3 --
@@ -332,10 +340,21 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
   __shared__ DrawInfo info;
+  __shared__ double sums[2 * 255 + 1];  // of the target's rows 0 .. nd, then the drafts'
   const VerifyArgs& a = j.a;
   const int s = blockIdx.x / j.parts3, part = blockIdx.x % j.parts3, t = threadIdx.x, w = t >> 6;
   const int id = t < a.K ? a.tokens[(long long)s * a.K + t] : -1;
   const int nd = drafts_of(a, s);
+  for (int q = t / 16; q < (a.draft ? 2 * nd + 1 : nd + 1); q += 16) {  // 16 lanes a row
+    const double* part = j.sums + (q <= nd ? target_row(a, s, q) : draft_row(a, s, q - nd - 1)) * j.parts2;
+    double x = 0.0;
+#pragma unroll 8
+    for (int k = t % 16; k < j.parts2; k += 16) x += part[k];
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
+    if (t % 16 == 0) sums[q] = x;
+  }
+  __syncthreads();
   bool ok = true;
   DrawInfo mine{};
   if (t <= nd) {  // row nd: no draft to refuse
@@ -343,13 +362,13 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
     const long long r = target_row(a, s, t);
     const float* zp = a.target + r * a.V;
     const float xp = zp[inside ? id : 0];
-    const Dist p = dist_of(j, zp, r);
+    const Dist p = dist_of(j, zp, r, sums[t]);
     Dist q = p;
     double qx = 1.0;
     if (a.draft && drafted) {
       const float* zq = a.draft + ((long long)s * a.K + t) * a.V;
       const float xq = zq[inside ? id : 0];
-      q = dist_of(j, zq, draft_row(a, s, t));
+      q = dist_of(j, zq, draft_row(a, s, t), sums[nd + 1 + t]);
       qx = q.p(xq);
     }
     if (drafted) ok = inside && (double)a.u[(long long)s * (a.K + 1) + t] * qx < p.p(xp);
@@ -552,22 +571,24 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
 
 struct Sizes {
   long long rows;
-  int spans, groups, parts2, parts3;
-  size_t span_max, top, sums, rest, draws, listed, bytes;
+  int spans, chunks, groups, parts2, parts3;
+  size_t span_max, chunk_max, top, sums, rest, draws, listed, bytes;
 };
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// parts: few rows are shared by several workgroups (2048 and 1024 in all)
+// parts3: few sequences are shared by several workgroups (1024 in all)
 Sizes sizes_of(int S, int K, int V) {
   Sizes z;
   z.rows = (long long)S * (2 * K + 1);
   z.spans = (V + kSpan - 1) / kSpan;
   z.groups = (z.spans + kGroup - 1) / kGroup;
-  z.parts2 = (int)std::min<long long>(kMaxParts, (2047 + z.rows) / z.rows);
+  z.chunks = (V + kChunk - 1) / kChunk;
+  z.parts2 = (z.spans + kPart - 1) / kPart;
   z.parts3 = std::min(kMaxParts, (1023 + S) / S);
   z.span_max = 0;
-  z.top = up256((size_t)z.rows * z.spans * 4);
+  z.chunk_max = up256((size_t)z.rows * z.spans * 4);
+  z.top = z.chunk_max + up256((size_t)z.rows * z.chunks * 4);
   z.sums = z.top + up256((size_t)z.rows * 4);
   z.rest = z.sums + up256((size_t)z.rows * z.parts2 * 8);
   z.draws = z.rest + up256((size_t)S * z.groups * 16);
@@ -589,10 +610,12 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.per_z = T > 0.0 ? 1.4426950408889634 / T : 0.0;
   j.low = a0.min_p > 0.f ? T * std::log((double)a0.min_p) : -(double)INFINITY;
   j.spans = z.spans;
+  j.chunks = z.chunks;
   j.groups = z.groups;
   j.parts2 = z.parts2;
   j.parts3 = z.parts3;
   j.span_max = (float*)(a0.ws + z.span_max);
+  j.chunk_max = (float*)(a0.ws + z.chunk_max);
   j.top = (float*)(a0.ws + z.top);
   j.sums = (double*)(a0.ws + z.sums);
   j.rest = (double2*)(a0.ws + z.rest);
@@ -600,13 +623,13 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.listed = (unsigned short*)(a0.ws + z.listed);
   const long long rows = (long long)a0.S * (j.a.draft ? 2 * a0.K + 1 : a0.K + 1);
   const int groups = (z.spans + kSpansPerWg - 1) / kSpansPerWg;
-  if (rows * groups > 0x7FFFFFFFLL || rows * z.parts2 > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+  const long long waves = rows * z.parts2;  // at most 2^25: rows x 16384 ids are bounded
   hipLaunchKernelGGL(verify_max_kernel, dim3((unsigned)(rows * groups)), dim3(256), 0, s, j, groups);
   if (T == 0.0) {
     hipLaunchKernelGGL(verify_greedy_kernel, dim3(a0.S), dim3(256), 0, s, j);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)(rows * z.parts2)), dim3(256), 0, s, j);
+  hipLaunchKernelGGL(verify_sum_kernel, dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, j, waves);
   hipLaunchKernelGGL(verify_rest_kernel, dim3((unsigned)(a0.S * z.parts3)), dim3(256), 0, s, j);
   hipLaunchKernelGGL(verify_draw_kernel, dim3(a0.S), dim3(256), 0, s, j);
   return hipGetLastError();
