@@ -577,7 +577,7 @@ struct Sizes {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-// parts3: few sequences are shared by several workgroups (1024 in all)
+// parts3: few sequences are shared by several workgroups (768 in all: three per CU)
 Sizes sizes_of(int S, int K, int V) {
   Sizes z;
   z.rows = (long long)S * (2 * K + 1);
@@ -585,7 +585,7 @@ Sizes sizes_of(int S, int K, int V) {
   z.groups = (z.spans + kGroup - 1) / kGroup;
   z.chunks = (V + kChunk - 1) / kChunk;
   z.parts2 = (z.spans + kPart - 1) / kPart;
-  z.parts3 = std::min(kMaxParts, (1023 + S) / S);
+  z.parts3 = std::min(kMaxParts, (767 + S) / S);
   z.span_max = 0;
   z.chunk_max = up256((size_t)z.rows * z.spans * 4);
   z.top = z.chunk_max + up256((size_t)z.rows * z.chunks * 4);
