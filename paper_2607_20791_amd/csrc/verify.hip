@@ -251,10 +251,12 @@ RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
 
 // ------------------------------------------------------------------ pass 2 --
 // A row's maximum, from those of its chunks, and the kept sum of kPart of its spans, by
-// one wave.  Rows differ in kept ids by a factor of a hundred: small parts share that
-// out (64 rows of 152064 ids of 60 to 4600 kept ones each, all nine rows of them: P2NEW us, against 35 for
-// workgroups that put a row's spans in a list first).
-__global__ __launch_bounds__(256) void verify_sum_kernel(Job j, long long waves) {
+// one wave.  Rows differ in kept ids by a factor of a hundred; small parts share that
+// out: 576 rows of 152064 ids, 200 kept ones in the middle row and 4600 in the
+// hundredth-largest, 39% of the spans read again: 31 us, 35 for workgroups that put the
+// spans in a list first, 39 for 64 spans a wave and 32 for 16.  Vector instructions are
+// busy half of the time.
+__global__ __launch_bounds__(256, 6) void verify_sum_kernel(Job j, long long waves) {
   const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (wave >= waves) return;
   const long long r = wave / j.parts2;
