@@ -473,7 +473,9 @@ uint64_t rgd_paged_attention_workspace_bytes(const rgd_paged_cache* cache, int32
  * the log of the sum of exponentiated scores, for joining with attention over
  * other positions.  A token that sees nothing gets 0 and -inf; rows at or behind
  * n_new[s] are left as they were.  Slots behind a length and free pages may hold
- * anything.  1 <= n <= 1024, S * n <= 2^24, n_heads <= 1024.  Meant for few tokens: every 64
+ * anything.  A value of V that is not finite makes its dimension of the tokens
+ * that see it inf or NaN and no other; sums are fp32, so a sequence's sum of |V|
+ * in a dimension must stay below 2^128.  1 <= n <= 1024, S * n <= 2^24, n_heads <= 1024.  Meant for few tokens: every 64
  * query vectors (tokens x query heads per KV head) of a sequence read its K and
  * V once.  Asynchronous. */
 int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,

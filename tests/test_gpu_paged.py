@@ -358,6 +358,33 @@ def test_later_tokens_do_not_reach_earlier_ones(rgd, bf16, n, hk, G, d):
             assert bool((t.isnan(late[..., 3]) if what[0] != what[0] else late[..., 3] == what[0]).all())
 
 
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n,hk,G,d", [(1, 2, 4, 64), (5, 1, 4, 128), (16, 1, 4, 32)])
+def test_an_old_value_that_is_not_finite_stays_in_its_dimension(rgd, bf16, n, hk, G, d):
+    """Values long before the new tokens, which all of them see: the dimension is not finite, everything else
+    keeps its bits."""
+    t = torch()
+    lens = [300, 700, 90]
+    x = _filled(rgd, lens, hk=hk, d=d, bf16=bf16, seed=n)
+    q = t.randn(3 * n, hk * G, d, device="cuda").to(_dt(bf16))
+    ws = t.empty(rgd.paged_attention_workspace_bytes(x.c, n, hk * G), dtype=t.uint8, device="cuda")
+
+    def run():
+        out = t.zeros(3 * n, hk * G * d, dtype=_dt(bf16), device="cuda")
+        rgd.paged_attention(x.c, 0, q, n, None, ws, out)
+        return out.view(3, n, hk, G, d)
+
+    ref = run()
+    for s, (pos, dim, what) in enumerate(((5, 0, float("inf")), (400, 17, float("-inf")), (0, d - 1, float("nan")))):
+        x.c.pool_v[0, int(x.pages[s, pos // 16]), 0, dim, pos % 16] = what
+        ref[s, :, 0, :, dim] = 0
+        got = run()
+        assert not bool(t.isfinite(got[s, :, 0, :, dim]).any())
+        for i in range(s + 1):
+            got[i, :, 0, :, (0, 17, d - 1)[i]] = 0
+        assert t.equal(got, ref), s
+
+
 def test_offsets_beyond_32_bits(rgd):
     """A pool of more than 2^31 elements whose used pages lie at its end."""
     t = torch()
