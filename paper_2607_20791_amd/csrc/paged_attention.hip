@@ -24,6 +24,12 @@
 // the first, 2^-17 of the weight is lost), for which the matrix units have room;
 // sums stay in fp32.  fp32: 16 positions at a time on the fp32 MFMA, whose operands have these
 // layouts without a gather.
+//
+// Measured, 8 KV heads of 128, bf16, both kernels' times: one token of 64 sequences of up to 8192
+// positions (253 MB of K and V) 52 + 5 us, 4.8 TB/s, and of one of 131072 (537 MB) 97 + 6 us, 5.5 TB/s:
+// the reads bound them, of which the memory sees 1.02 and 1.06 times the bytes.  Five tokens
+// of 32 sequences of up to 4096 (75 MB) 22 + 5 us, 16 of 16 sequences of 4096 (268 MB) 65 + 6.  One token over
+// 512 positions 7.6 + 3.3 us: two launches and a chain of reads (lengths, table, K and V, pieces).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -35,9 +41,14 @@ namespace rgd {
 namespace {
 
 constexpr int kStep = 32;      // positions per step of the plan
-constexpr int kMinSteps = 4;   // a run is no shorter: one step a wave
-constexpr int kItemCost = 8;   // what an item costs besides its steps, in steps
-constexpr int kMaxRuns = 512;  // two workgroups per CU; half of it where LDS or registers hold one
+// A run is no shorter: one step a wave.  One sequence of 512: 7.9 us, with 8, 12 and 24 steps 8.6, 10.2 and 11.0.
+constexpr int kMinSteps = 4;
+// What an item costs besides its steps, in steps.  64 ragged sequences to 8192 with 4, 6, 8, 12: 54.5, 52.1, 52.9
+// and 54.9 us, 32 of five tokens to 4096: 25.9, 22.4, 21.9 and 20.9.
+constexpr int kItemCost = 8;
+// Two workgroups per CU; half of it where LDS or registers hold one.  Three per CU spill: one sequence of
+// 131072 takes 162 us in place of 109.
+constexpr int kMaxRuns = 512;
 constexpr int kWaves = 4;      // per workgroup
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -655,12 +666,14 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAtt
   }
 }
 
-// Columns per workgroup of the joining kernel: one where a sequence has few (its pieces
-// are then shared out over the workgroup), eight where it has many.
+// Columns per workgroup of the joining kernel: one where an item has few (its pieces
+// are then shared out over the workgroup), eight where it has many.  One sequence of 131072, cut into
+// 64 pieces a head: 6.1 us, 12.8 with eight; 16 tokens of 16 sequences of 4096: 5.6, 13.3 with one.
 constexpr int join_cols(int nt) { return nt == 1 ? 1 : 8; }
 
 // The outputs of the items that several runs share, by the run that an item starts
-// in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.
+// in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.  3.3 to 6.1 us: a launch
+// and two dependent reads, the cut and its pieces (1 MB to 5 MB, which lie in the caches).
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
   constexpr int COLS = 16 * NT, W = D / 4, CB = join_cols(NT), PARTS = 256 / W / CB;
@@ -708,7 +721,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int run
 }
 
 // Query tiles a wave holds at once: all of a sequence's query vectors up to 64 (fp32
-// of 128 dimensions: 32, what the registers hold).
+// of 128 dimensions: 32, what the registers hold), as each further item reads K and V again.  20
+// vectors of 32 sequences to 4096: 21.8 us in two tiles, 25.0 in two items of one; 64 vectors of 16
+// sequences of 4096: 65 us in four, 82 in two items of two, 145 in four of one.  (48 vectors of 32
+// sequences to 4096, 75 MB that the last-level cache holds: 34.6, 31.9 and 38.9.)
 int tiles_for(const PagedView& c, int vectors) {
   return vectors <= 16 ? 1 : vectors <= 32 || (c.esz == 4 && c.D == 128) ? 2 : 4;
 }
@@ -717,7 +733,8 @@ int runs_for(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), cols = 16 * nt;
   const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
-  return (int)std::min(nt == 1 || (nt == 2 && c.esz * c.D < 512) ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
+  const bool two = nt == 1 || (nt == 2 && c.esz * c.D < 512);  // workgroups per CU
+  return (int)std::min(two ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
 }
 
 template <typename T, int D, int NT>
@@ -726,7 +743,8 @@ hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
   const int cols = std::min(16 * NT, a.n * (a.Hq / a.c.Hkv));
-  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), dim3(runs, (cols + join_cols(NT) - 1) / join_cols(NT)), dim3(256), 0, s, a, runs);
+  const dim3 grid(runs, (cols + join_cols(NT) - 1) / join_cols(NT));
+  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), grid, dim3(256), 0, s, a, runs);
   return hipGetLastError();
 }
 

@@ -14,6 +14,10 @@
 // and sums are fp64: the token drawn hangs on sums of up to 2^20 weights, which fp32
 // would leave wrong in one draw of a few.  T == 0: pass 1, then the first
 // id of each row's maximum.
+//
+// Measured, passes 1 to 4: 64 sequences of up to 4 drafts with logits of their own (512 rows of
+// 152064 in all, 311 MB) 54 + 30 + 17 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 41 + 9 + 7 + 6; one
+// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 4.5 + 4.4 + 5.9 + 4.4, launches and latency.
 #include <algorithm>
 #include <cmath>
 
@@ -117,6 +121,9 @@ RGD_DEV float last_lane_max(float v) {
   return max_step<0x143, 0xc>(v);
 }
 
+// 16 KB a wave in flight at once, then the spans' maxima by row shifts between lanes.  311 MB: 54 us,
+// 5.7 TB/s: memory bounds it (reads counted there: 1.00 times the bytes).  Spans of 64 ids would
+// save pass 2 2 us and cost as much here; putting candidate ids aside here takes 73 us.
 __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
   const long long r = blockIdx.x / groups;
   const int first = ((int)(blockIdx.x % groups) * 4 + (threadIdx.x >> 6)) * 16, lane = threadIdx.x & 63;
@@ -189,7 +196,7 @@ struct SpanMax {
     const float* row = j.span_max + r * j.spans;
 #pragma unroll
     for (int k = 0; k < kMaxSpans / 256; ++k)
-      if (k < per) m[k] = row[min(per * (int)threadIdx.x + k, j.spans - 1)];  // (the last one twice does no harm to a maximum)
+      if (k < per) m[k] = row[min(per * (int)threadIdx.x + k, j.spans - 1)];
   }
   // the spans that reach thr, in order, by the whole workgroup: list[0 .. n); red: 4 ints
   RGD_DEV int list(const Job& j, float thr, unsigned short* out, int* red) const {
@@ -252,8 +259,8 @@ RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
 // ------------------------------------------------------------------ pass 2 --
 // A row's maximum, from those of its chunks, and the kept sum of kPart of its spans, by
 // one wave.  Rows differ in kept ids by a factor of a hundred; small parts share that
-// out: 576 rows of 152064 ids, 200 kept ones in the middle row and 4600 in the
-// hundredth-largest, 39% of the spans read again: 31 us, 35 for workgroups that put the
+// out: 512 rows of 152064 ids, 200 kept ones in the middle row and 4600 in the
+// hundredth-largest, 39% of the spans read again (132 MB): 30 us, 35 for workgroups that put the
 // spans in a list first, 39 for 64 spans a wave and 32 for 16.  Vector instructions are
 // busy half of the time.
 __global__ __launch_bounds__(256, 6) void verify_sum_kernel(Job j, long long waves) {
@@ -337,7 +344,9 @@ struct Draw {
 };
 
 // Accepted drafts of a sequence, one draft a thread (K <= 255), then the rest of the
-// drawn row in this part's spans.
+// drawn row in this part's spans.  64 sequences in 12 parts: 17 us, two dependent
+// chains (tokens and sums, accepted row, its maxima, its spans) beside 34 MB of reads; 20.8 us where
+// parts make more than three workgroups per CU.
 __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
@@ -451,7 +460,8 @@ RGD_DEV int block_min_i(int v, int* red) {
 }
 
 // The draw: the group, then the id, whose running sum first exceeds u times the total;
-// where rounding leaves none, the last one with weight.
+// where rounding leaves none, the last one with weight.  4.4 to 6.8 us: one chain of three reads
+// (the pass before's result, the groups' sums, a group's logits) and four scans.
 __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   __shared__ double red[4];
   __shared__ int redi[4];
@@ -532,7 +542,7 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
 
 // ------------------------------------------------------------------ T == 0 --
 // The first maximum of every row that is asked for, one row a wave; the drafts are
-// kept while they are it.
+// kept while they are it.  One workgroup a sequence: it reads 4 bytes of 1 KB that pass 1 did.
 __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
   __shared__ int best[256];
   __shared__ int redi[4];
@@ -625,7 +635,7 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.listed = (unsigned short*)(a0.ws + z.listed);
   const long long rows = (long long)a0.S * (j.a.draft ? 2 * a0.K + 1 : a0.K + 1);
   const int groups = (z.spans + kSpansPerWg - 1) / kSpansPerWg;
-  const long long waves = rows * z.parts2;  // at most 2^25: rows x 16384 ids are bounded
+  const long long waves = rows * z.parts2;  // at most 2^24: rows x 16384 ids are bounded
   hipLaunchKernelGGL(verify_max_kernel, dim3((unsigned)(rows * groups)), dim3(256), 0, s, j, groups);
   if (T == 0.0) {
     hipLaunchKernelGGL(verify_greedy_kernel, dim3(a0.S), dim3(256), 0, s, j);
