@@ -33,6 +33,8 @@ struct PagedAttnArgs {
   int n; const int* n_new; int Hq;
   void* out; float* lse;
   float* ws;
+  int G;           // query heads per KV head
+  unsigned inv_G;  // ceil(2^31 / G)
 };
 bool paged_attention_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq);

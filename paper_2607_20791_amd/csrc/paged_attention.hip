@@ -26,10 +26,11 @@
 // layouts without a gather.
 //
 // Measured, 8 KV heads of 128, bf16, both kernels' times: one token of 64 sequences of up to 8192
-// positions (253 MB of K and V) 52 + 5 us, 4.8 TB/s, and of one of 131072 (537 MB) 97 + 6 us, 5.5 TB/s:
+// positions (253 MB of K and V) 51 + 5 us, 5.0 TB/s, and of one of 131072 (537 MB) 96 + 6 us, 5.6 TB/s:
 // the reads bound them, of which the memory sees 1.02 and 1.06 times the bytes.  Five tokens
-// of 32 sequences of up to 4096 (75 MB) 22 + 5 us, 16 of 16 sequences of 4096 (268 MB) 65 + 6.  One token over
-// 512 positions 7.6 + 3.3 us: two launches and a chain of reads (lengths, table, K and V, pieces).
+// of 32 sequences of up to 4096 (73 MB) 22 + 5 us, 16 of 16 sequences of 4096 (268 MB) 65 + 5.  One token over
+// 512 positions 6.3 + 2.8 us: two launches and a chain of reads (lengths, table, K and V, pieces).  One token
+// of 1024 sequences of up to 500 (354 MB): 115 us, as an item is a step or two of one to three waves.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -41,11 +42,13 @@ namespace rgd {
 namespace {
 
 constexpr int kStep = 32;      // positions per step of the plan
-// A run is no shorter: one step a wave.  One sequence of 512: 7.9 us, with 8, 12 and 24 steps 8.6, 10.2 and 11.0.
+// A run is no shorter: one step a wave.  One sequence of 512: 6.3 us, with 8 steps 7.0.
 constexpr int kMinSteps = 4;
-// What an item costs besides its steps, in steps.  64 ragged sequences to 8192 with 4, 6, 8, 12: 54.5, 52.1, 52.9
-// and 54.9 us, 32 of five tokens to 4096: 25.9, 22.4, 21.9 and 20.9.
-constexpr int kItemCost = 8;
+// What an item costs besides its steps, in steps: more with more outputs.  One token (one tile) of 64 ragged
+// sequences to 8192 with 2, 3, 4, 6 and 8: 58.8, 52.8, 51.0, 51.6 and 51.8 us, of 1024 to 500: 122, 117, 115, 119 and
+// 124; five (two tiles) of 32 to 4096 with 4, 6, 8 and 12: 26.4, 21.7, 21.5 and 21.0; twelve (four tiles)
+// with 4, 6, 8, 12 and 16: 49.2, 39.9, 32.4, 32.3 and 31.2.
+constexpr int item_cost(int nt) { return 4 * nt; }
 // Two workgroups per CU; half of it where LDS or registers hold one.  Three per CU spill: one sequence of
 // 131072 takes 162 us in place of 109.
 constexpr int kMaxRuns = 512;
@@ -60,10 +63,14 @@ RGD_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 // New tokens of sequence s.
 RGD_DEV int new_tokens(const PagedAttnArgs& a, int s) { return a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n; }
 
+// Floor of col / G for col < 2^20, G <= 1024: the product passes col / G by less than col / 2^31,
+// which is less than 1 / G.
+RGD_DEV int token_of(const PagedAttnArgs& a, int col) { return (int)__umulhi((unsigned)col << 1, a.inv_G); }
+
 struct Seq {
   int len, m;   // positions, new tokens
   int steps;    // per item; at least one, so that tokens that see nothing get their zeros
-  int items;    // KV heads x query tiles; 0 without new tokens
+  int tiles;    // query tiles; 0 without new tokens.  Items: KV heads x query tiles
 };
 
 template <int COLS>
@@ -72,12 +79,20 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m) {
   q.len = len;
   q.m = m;
   q.steps = max(1, (len + kStep - 1) / kStep);
-  q.items = a.c.Hkv * ((m * (a.Hq / a.c.Hkv) + COLS - 1) / COLS);
+  q.tiles = (m * a.G + COLS - 1) / COLS;
   return q;
 }
 template <int COLS>
 RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
   return seq_of<COLS>(a, paged_len(a.c, s), new_tokens(a, s));
+}
+// The same for an s that the whole wave shares, by scalar loads: a vector load's wait would be one
+// for the K and V on their way, too.
+template <int COLS>
+RGD_DEV Seq uniform_seq(const PagedAttnArgs& a, int s) {
+  typedef const int __attribute__((address_space(4))) * Scalar;
+  const int len = ((Scalar)a.c.lens)[s], m = a.n_new ? ((Scalar)a.n_new)[s] : a.n;
+  return seq_of<COLS>(a, min(max(len, 0), a.c.width * a.c.ps), min(max(m, 0), a.n));
 }
 
 // Sum over the lanes up to this one (64-bit: long tables times many sequences).
@@ -104,7 +119,7 @@ RGD_DEV long long lane_value(long long v, int lane) {
 template <int COLS>
 RGD_DEV long long units_of(const PagedAttnArgs& a, int s, Seq& q) {
   q = seq_of<COLS>(a, min(s, a.c.S - 1));
-  return s < a.c.S ? (long long)(q.steps + kItemCost) * q.items : 0;
+  return s < a.c.S ? (long long)(q.steps + item_cost(COLS / 16)) * (a.c.Hkv * q.tiles) : 0;
 }
 
 // Floor of x / y for 0 <= x < 2^52, 0 < y.  Exact: a quotient that is no whole number
@@ -119,29 +134,33 @@ struct Runs {
 // before that one.  False: there is none.
 template <int COLS>
 RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& s, Seq& sq, long long& before) {
-  const int lane = threadIdx.x & 63;
-  Seq q, more;
-  long long u = units_of<COLS>(a, lane, q), incl = wave_scan(u);
+  const int lane = threadIdx.x & 63, per = (a.c.S + 63) / 64;  // sequences a lane: one, or neighbouring ones
+  Seq q;
+  long long u = 0;
+#pragma unroll 8
+  for (int k = 0; k < per; ++k) u += units_of<COLS>(a, lane * per + k, q);
+  long long incl = wave_scan(u);
   plan.total = lane_value(incl, 63);
-  for (int s0 = 64; s0 < a.c.S; s0 += 64) plan.total += lane_value(wave_scan(units_of<COLS>(a, s0 + lane, more)), 63);
   plan.length = max((long long)kMinSteps, quotient(plan.total + runs - 1, runs));
   const long long start = r * plan.length;
   if (start >= plan.total) return false;
-  long long base = 0;
-  for (int s0 = 0;;) {
-    const unsigned long long hit = __ballot(base + incl > start);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      before = base + lane_value(incl - u, l);
-      s = s0 + l;
-      sq = seq_of<COLS>(a, __builtin_amdgcn_readlane(q.len, l), __builtin_amdgcn_readlane(q.m, l));
-      return true;
+  int l = __builtin_ctzll(__ballot(incl > start));
+  before = lane_value(incl - u, l);
+  s = l * per;
+  if (per > 1)
+    for (;; s += 64) {
+      u = units_of<COLS>(a, s + lane, q);
+      incl = wave_scan(u);
+      if (const unsigned long long hit = __ballot(before + incl > start)) {
+        l = __builtin_ctzll(hit);
+        before += lane_value(incl - u, l);
+        s += l;
+        break;
+      }
+      before += lane_value(incl, 63);
     }
-    base += lane_value(incl, 63);
-    s0 += 64;
-    u = units_of<COLS>(a, s0 + lane, q);
-    incl = wave_scan(u);
-  }
+  sq = seq_of<COLS>(a, __builtin_amdgcn_readlane(q.len, l), __builtin_amdgcn_readlane(q.m, l));
+  return true;
 }
 
 RGD_DEV f32x4 mfma_bf16(const u32x4& x, const u32x4& y, f32x4 c) {
@@ -249,36 +268,40 @@ struct Item {
   RGD_DEV int begin(int wave, int per) const { return t0 * kStep + wave * per; }
 };
 
-RGD_DEV Seq uniform(const Seq& q) { return Seq{uniform(q.len), uniform(q.m), uniform(q.steps), uniform(q.items)}; }
+RGD_DEV Seq uniform(const Seq& q) { return Seq{uniform(q.len), uniform(q.m), uniform(q.steps), uniform(q.tiles)}; }
 
 // The items of a run, one after the other.
 template <int COLS>
 struct Walk {
+  static constexpr int COST = item_cost(COLS / 16);
   Seq sq;
-  int s, item, u0, left;
+  int s, g, qb, u0, left;
   long long at;
   RGD_DEV Item next(const PagedAttnArgs& a) {
     Item it{};
     if (left <= 0) return it;
-    if (item == sq.items) {  // steps are left, so a sequence with new tokens follows
-      item = 0;
-      do sq = uniform(seq_of<COLS>(a, ++s));
-      while (sq.items == 0);
+    if (g == a.c.Hkv) {  // steps are left, so a sequence with new tokens follows
+      g = 0;
+      do sq = uniform_seq<COLS>(a, ++s);
+      while (sq.tiles == 0);
     }
-    // an item's first kItemCost units of the plan are its fixed cost, in front of its steps
-    const int u1 = min(sq.steps + kItemCost, u0 + left), tiles = sq.items / a.c.Hkv;
+    // an item's first COST units of the plan are its fixed cost, in front of its steps
+    const int u1 = min(sq.steps + COST, u0 + left);
     it.sq = sq;
     it.s = s;
-    it.g = item / tiles;
-    it.qb = item - it.g * tiles;
-    it.t0 = max(0, u0 - kItemCost);
-    it.t1 = u1 - kItemCost;
+    it.g = g;
+    it.qb = qb;
+    it.t0 = max(0, u0 - COST);
+    it.t1 = u1 - COST;
     it.valid = it.t1 > it.t0;  // else the next run has the item's first step
     it.at = at;
-    at += sq.steps + kItemCost;
+    at += sq.steps + COST;
     left -= u1 - u0;
     u0 = 0;
-    ++item;
+    if (++qb == sq.tiles) {
+      qb = 0;
+      ++g;
+    }
     return it;
   }
 };
@@ -424,8 +447,8 @@ struct Piece {
 
   // a tile a wave, between two barriers
   RGD_DEV void stage_q(const PagedAttnArgs& a, const Item& it, u32x4* dst, int wave) const {
-    const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
-    const int col = min(it.qb * COLS + wave * 16 + row, cols - 1), i = col / G;
+    const int G = a.G, cols = it.sq.m * G;
+    const int col = min(it.qb * COLS + wave * 16 + row, cols - 1), i = token_of(a, col);
     const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
     for (int c = 0; c < KL; ++c) dst[(wave * KL + c) * 64 + lane] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
@@ -433,10 +456,10 @@ struct Piece {
 
   RGD_DEV void load_q(const PagedAttnArgs& a, const Item& it) {
     if (QS) return;
-    const int G = a.Hq / a.c.Hkv, cols = it.sq.m * G;
+    const int G = a.G, cols = it.sq.m * G;
 #pragma unroll
     for (int t = 0; t < (QS ? 0 : NT); ++t) {
-      const int col = min(it.qb * COLS + t * 16 + row, cols - 1), i = col / G;  // columns behind the last one repeat it
+      const int col = min(it.qb * COLS + t * 16 + row, cols - 1), i = token_of(a, col);  // columns behind the last one repeat it
       const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
       for (int c = 0; c < KL; ++c) q[t][c] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
@@ -449,6 +472,7 @@ struct Piece {
     walk = w;
     load_q(a, it);
     load_k(a, it.g, p0);
+    __builtin_amdgcn_sched_barrier(0);  // K's wait leaves V's loads on their way, here and where the paths meet
     load_v(a);
   }
 
@@ -456,20 +480,19 @@ struct Piece {
   // way; leaves those of the next item on theirs (walk_next: its table's first entries).
   RGD_DEV void run(const PagedAttnArgs& a, const Item& it, const Item& next, const TableWalk& walk_next, int wave) {
     const Seq& sq = it.sq;
-    const int G = a.Hq / a.c.Hkv, cols = sq.m * G, qb = it.qb, g = it.g;
+    const int cols = sq.m * a.G, qb = it.qb, g = it.g, p1 = it.end();
+    int p0 = it.begin(wave, PER);
     int lim[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      lim[t] = sq.len - sq.m + min(qb * COLS + t * 16 + row, cols - 1) / G + 1;
+      lim[t] = sq.len - sq.m + token_of(a, min(qb * COLS + t * 16 + row, cols - 1)) + 1;
       m[t] = kNoRef;
       l[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < VL; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = sq.len - sq.m + (qb * COLS) / G + 1;  // all of the tile's tokens see that much
+    const int least = sq.len - sq.m + token_of(a, qb * COLS) + 1;  // all of the tile's tokens see that much
     const float scale = kLog2e / sqrtf((float)D);
-    const int p1 = it.end();
-    int p0 = it.begin(wave, PER);
     if (p0 >= p1) {
       start(a, next, walk_next, wave);
       return;
@@ -509,11 +532,14 @@ struct Piece {
       const int pos = p0 + grp * E;  // of this lane's first score
       const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
       bool odd = false;
-      const int held = there ? sq.len - pos : 0;
+      if (here != ALL || p0 + PER > sq.len) {
+        const int held = there ? sq.len - pos : 0;
 #pragma unroll
-      for (int d = 0; d < VL; ++d) {
-        v[d] = keep_first<T>(v[d], held);
-        odd = odd || any_nonfinite<T>(v[d]);
+        for (int d = 0; d < VL; ++d) v[d] = keep_first<T>(v[d], held);
+      }
+      if (least < min(p0 + PER, sq.len)) {  // not every column sees every value
+#pragma unroll
+        for (int d = 0; d < VL; ++d) odd = odd || any_nonfinite<T>(v[d]);
       }
       float p[NT][E];
       u32x4 hi[NT], lo[NT];
@@ -574,8 +600,10 @@ RGD_DEV void store_row4(T* p, f32x4 v) {
 // Workspace: per run a Cut, then the pieces: slot 2 r + 1 holds the start of the item
 // that run r ends in, slot 2 r the part of an item that an earlier run began.  Per slot
 // [COLS][D] weighted sums, then [COLS] (maximum, sum).
-struct Cut {
-  int s, g, qb, last;  // the item that starts in this run and goes on to run `last`; s = -1: none
+struct Cut {  // the item that starts in this run and goes on to run `last`
+  int s, g;   // s = -1: none
+  int qb;
+  short last, cols;  // cols: the item's query vectors
 };
 __host__ __device__ constexpr size_t cut_floats(int runs) { return ((size_t)runs * 4 + 63) / 64 * 64; }
 template <int D, int NT>
@@ -583,10 +611,13 @@ constexpr size_t slot_floats() {
   return (size_t)16 * NT * (D + 2);
 }
 
+// Whether a CU holds two workgroups (row: bytes of a row of K).
+constexpr bool two_per_cu(int nt, size_t row) { return nt == 1 || (nt == 2 && row < 512); }
+
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
+__global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
   using P = Piece<T, D, NT>;
-  constexpr int COLS = P::COLS, LD = D + 4;
+  constexpr int COLS = P::COLS, LD = D + 4, COST = item_cost(NT);
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
   __shared__ u32x4 q_s[P::QS ? NT * P::KL * 64 : 1];
@@ -603,10 +634,12 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAtt
   walk.s = uniform(s);
   walk.left = uniform((int)min(plan.length, plan.total - start));
   walk.sq = uniform(walk.sq);
-  walk.item = uniform((int)quotient(start - before, walk.sq.steps + kItemCost));
-  walk.at = before + (long long)walk.item * (walk.sq.steps + kItemCost);
+  const int item = uniform((int)quotient(start - before, walk.sq.steps + COST));
+  walk.g = item / walk.sq.tiles;
+  walk.qb = item - walk.g * walk.sq.tiles;
+  walk.at = before + (long long)item * (walk.sq.steps + COST);
   walk.u0 = uniform((int)(start - walk.at));
-  const int G = a.Hq / a.c.Hkv;
+  const int G = a.G;
   P x;
   x.lane = lane;
   x.row = row;
@@ -637,23 +670,25 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAtt
     __syncthreads();
     const bool done = t0 == 0 && t1 == sq.steps;
     if (t0 == 0 && !done && threadIdx.x == 0)
-      *cut = Cut{s, g, qb, (int)quotient(it.at + kItemCost + sq.steps - 1, plan.length)};
+      *cut = Cut{s, g, qb, (short)quotient(it.at + COST + sq.steps - 1, plan.length), (short)cols};
     float* slot = a.ws + cut_floats(runs) + (size_t)(2 * r + (t0 == 0)) * slot_floats<D, NT>();
     for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
       const int c = i / (D / 4), d = i % (D / 4) * 4, col = qb * COLS + c;
       float top = ml[0][c].x, sum = 0.f;
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) top = fmaxf(top, ml[w][c].x);
+      for (int w = 1; w < kWaves; ++w)
+        top = fmaxf(top, ml[w][c].x);
       f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float f = exp2_raw(ml[w][c].x - top);
-        sum += f * ml[w][c].y;
-        o += f * *(const f32x4*)&part[w][c][d];
-      }
+      for (int w = 0; w < kWaves; ++w)
+        {
+          const float f = exp2_raw(ml[w][c].x - top);
+          sum += f * ml[w][c].y;
+          o += f * *(const f32x4*)&part[w][c][d];
+        }
       if (done) {
-        const size_t row_out = (size_t)s * a.n + col / G;
-        const int h = g * G + col % G;
+        const int i = token_of(a, col), h = g * G + col - i * G;
+        const size_t row_out = (size_t)s * a.n + i;
         store_row4((T*)a.out + (row_out * a.Hq + h) * D + d, o * (sum == 0.f ? 0.f : 1.f / sum));
         if (a.lse && d == 0) a.lse[row_out * a.Hq + h] = lse_of(top, sum);
       } else {
@@ -668,12 +703,12 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attn_run_kernel(PagedAtt
 
 // Columns per workgroup of the joining kernel: one where an item has few (its pieces
 // are then shared out over the workgroup), eight where it has many.  One sequence of 131072, cut into
-// 64 pieces a head: 6.1 us, 12.8 with eight; 16 tokens of 16 sequences of 4096: 5.6, 13.3 with one.
+// 64 pieces a head: 5.7 us, 12.8 with eight; 16 tokens of 16 sequences of 4096: 5.2, 13.3 with one.
 constexpr int join_cols(int nt) { return nt == 1 ? 1 : 8; }
 
 // The outputs of the items that several runs share, by the run that an item starts
-// in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.  3.3 to 6.1 us: a launch
-// and two dependent reads, the cut and its pieces (1 MB to 5 MB, which lie in the caches).
+// in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.  2.8 to 5.7 us: a launch and
+// one round trip, two where an item has more pieces than fit the threads (1 to 5 MB, which lie in the caches).
 template <typename T, int D, int NT>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
   constexpr int COLS = 16 * NT, W = D / 4, CB = join_cols(NT), PARTS = 256 / W / CB;
@@ -681,16 +716,25 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int run
   __shared__ float2 ml_s[CB][PARTS];
   const int r = blockIdx.x, t = threadIdx.x;
   const Cut cut = ((const Cut*)a.ws)[r];
-  if (cut.s < 0) return;
   const int d = t % W, k = t / W / PARTS, part = t / W % PARTS, c = blockIdx.y * CB + k;
-  const int G = a.Hq / a.c.Hkv, col = cut.qb * COLS + c, cols = min(COLS, new_tokens(a, cut.s) * G - cut.qb * COLS);
   const float* slots = a.ws + cut_floats(runs);
   auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == r)) * slot_floats<D, NT>(); };
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float sum = 0.f, top = kNoRef;
+  // the first piece is asked for together with the cut; where there is none, it is not used
+  const float* first = slot(min(r + part, runs - 1));
+  f32x4 acc = *(const f32x4*)(first + c * D + 4 * d);
+  const float2 ml0 = *(const float2*)(first + COLS * D + 2 * c);
+  asm volatile("" ::"v"(acc), "v"(ml0.x), "v"(ml0.y));
+  if (cut.s < 0) return;
+  const int G = a.G, col = cut.qb * COLS + c, cols = cut.cols;
+  float sum = ml0.y, top = ml0.x;
   if (c < cols) {
+    if (r + part > cut.last) {
+      acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      sum = 0.f;
+      top = kNoRef;
+    }
 #pragma unroll 4
-    for (int w = r + part; w <= cut.last; w += PARTS) {
+    for (int w = r + part + PARTS; w <= cut.last; w += PARTS) {
       const float* p = slot(w);
       const float2 ml = *(const float2*)(p + COLS * D + 2 * c);
       const float nt = fmaxf(top, ml.x), down = exp2_raw(top - nt), f = exp2_raw(ml.x - nt);
@@ -715,16 +759,17 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int run
       sum += f * ml_s[k][i].y;
     }
   }
-  const size_t at = ((size_t)cut.s * a.n + col / G) * a.Hq + cut.g * G + col % G;
+  const int i = token_of(a, col);
+  const size_t at = ((size_t)cut.s * a.n + i) * a.Hq + cut.g * G + col - i * G;
   store_row4((T*)a.out + at * D + 4 * d, acc * (sum == 0.f ? 0.f : 1.f / sum));
   if (d == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
 // Query tiles a wave holds at once: all of a sequence's query vectors up to 64 (fp32
 // of 128 dimensions: 32, what the registers hold), as each further item reads K and V again.  20
-// vectors of 32 sequences to 4096: 21.8 us in two tiles, 25.0 in two items of one; 64 vectors of 16
+// vectors of 32 sequences to 4096: 21.5 us in two tiles, 25.0 in two items of one; 64 vectors of 16
 // sequences of 4096: 65 us in four, 82 in two items of two, 145 in four of one.  (48 vectors of 32
-// sequences to 4096, 75 MB that the last-level cache holds: 34.6, 31.9 and 38.9.)
+// sequences to 4096, 73 MB that the last-level cache holds: 31.2, 31.9 and 38.9.)
 int tiles_for(const PagedView& c, int vectors) {
   return vectors <= 16 ? 1 : vectors <= 32 || (c.esz == 4 && c.D == 128) ? 2 : 4;
 }
@@ -733,8 +778,8 @@ int runs_for(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), cols = 16 * nt;
   const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
-  const bool two = nt == 1 || (nt == 2 && c.esz * c.D < 512);  // workgroups per CU
-  return (int)std::min(two ? (double)kMaxRuns : kMaxRuns / 2.0, std::ceil((steps + kItemCost * items) / kMinSteps));
+  const double most = two_per_cu(nt, c.esz * c.D) ? kMaxRuns : kMaxRuns / 2;
+  return (int)std::min(most, std::ceil((steps + item_cost(nt) * items) / kMinSteps));
 }
 
 template <typename T, int D, int NT>
@@ -742,7 +787,7 @@ hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
   const int runs = runs_for(a.c, a.n, a.Hq);
   hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
-  const int cols = std::min(16 * NT, a.n * (a.Hq / a.c.Hkv));
+  const int cols = std::min(16 * NT, a.n * a.G);
   const dim3 grid(runs, (cols + join_cols(NT) - 1) / join_cols(NT));
   hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), grid, dim3(256), 0, s, a, runs);
   return hipGetLastError();
@@ -750,7 +795,7 @@ hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
-  switch (tiles_for(a.c, a.n * (a.Hq / a.c.Hkv))) {
+  switch (tiles_for(a.c, a.n * a.G)) {
     case 1: return launch<T, D, 1>(a, s);
     case 2: return launch<T, D, 2>(a, s);
   }
@@ -772,7 +817,7 @@ hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
 // the plan's units, whatever the lengths are, in numbers that it can count with
 bool paged_attention_fits(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), tiles = (n * (Hq / c.Hkv) + 16 * nt - 1) / (16 * nt);
-  return (double)c.S * c.Hkv * tiles * (std::ceil((double)c.width * c.ps / kStep) + kItemCost) < 549755813888.0;  // 2^39
+  return (double)c.S * c.Hkv * tiles * (std::ceil((double)c.width * c.ps / kStep) + item_cost(nt)) < 549755813888.0;  // 2^39
 }
 
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
@@ -780,7 +825,10 @@ size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
   return cut_floats(runs) + (size_t)2 * runs * 16 * nt * (c.D + 2);
 }
 
-hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s) {
+hipError_t paged_attention(const PagedAttnArgs& a0, hipStream_t s) {
+  PagedAttnArgs a = a0;
+  a.G = a.Hq / a.c.Hkv;
+  a.inv_G = (unsigned)(((1ull << 31) + a.G - 1) / a.G);
   return a.c.esz == 2 ? launch_dim<bf16_t>(a, s) : launch_dim<float>(a, s);
 }
 
