@@ -507,7 +507,7 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * count as -inf.  A target row whose maximum is not finite has no distribution:
  * its draft is refused and -1 stands for the drawn token; such a draft row has
  * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, S (2 K + 1)
- * ceil(V / 16384) <= 2^23, T >= 0, min_p in [0, 1].  Sums are taken in fp64, so
+ * ceil(V / 8192) <= 2^23, T >= 0, min_p in [0, 1].  Sums are taken in fp64, so
  * that the draw is the exact one unless u[K] meets the border of two tokens by
  * 1e-11 of the total.  Asynchronous. */
 int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t* draft_tokens,

@@ -157,7 +157,7 @@ int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const v
 
 uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V) {
   if (S < 1 || S > 65536 || K < 1 || K > 255 || V < 2 || V > (1 << 20)) return 0;
-  if ((int64_t)S * (2 * K + 1) * ((V + 16383) / 16384) > (1 << 23)) return 0;
+  if ((int64_t)S * (2 * K + 1) * ((V + 8191) / 8192) > (1 << 23)) return 0;
   return verify_workspace_bytes(S, K, V);
 }
 

@@ -16,8 +16,8 @@
 // id of each row's maximum.
 //
 // Measured, passes 1 to 4: 64 sequences of up to 4 drafts with logits of their own (512 rows of
-// 152064 in all, 311 MB) 54 + 30 + 17 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 41 + 9 + 7 + 6; one
-// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 4.5 + 4.4 + 5.9 + 4.4, launches and latency.
+// 152064 in all, 311 MB) 47 + 36 + 18 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 36 + 10 + 7 + 6; one
+// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.5 + 4.5 + 5.9 + 4.4, launches and latency.
 #include <algorithm>
 #include <cmath>
 
@@ -28,9 +28,9 @@ namespace rgd {
 namespace {
 
 constexpr int kSpan = 256;       // ids per span: one wave, four a lane
-constexpr int kSpansPerWg = 64;  // pass 1: four waves, 16 spans each
+constexpr int kWaveSpans = 8;    // pass 1: spans of a wave
+constexpr int kChunk = kWaveSpans * kSpan;
 constexpr int kMaxSpans = 4096;
-constexpr int kChunk = 4096;     // ids of a wave in pass 1
 constexpr int kPart = 32;        // spans of a wave in pass 2
 constexpr int kMaxParts = 16;    // workgroups that share a row in pass 3
 
@@ -121,32 +121,35 @@ RGD_DEV float last_lane_max(float v) {
   return max_step<0x143, 0xc>(v);
 }
 
-// 16 KB a wave in flight at once, then the spans' maxima by row shifts between lanes.  311 MB: 54 us,
-// 5.7 TB/s: memory bounds it (reads counted there: 1.00 times the bytes).  Spans of 64 ids would
-// save pass 2 2 us and cost as much here; putting candidate ids aside here takes 73 us.
+// 8 KB a wave in flight at once, then the spans' maxima by row shifts between lanes.  311 MB: 47 us,
+// 6.6 TB/s: memory bounds it (reads counted there: 1.00 times the bytes).  The loads are nontemporal: without
+// that 54 us, and pass 2, which then finds some of its spans in the last-level cache, 31 in
+// place of 36.  One sequence of 4 drafts: 3.5 us, with 16 spans a wave 4.5.  Putting candidate ids aside here
+// costs 19 us.
 __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
   const long long r = blockIdx.x / groups;
-  const int first = ((int)(blockIdx.x % groups) * 4 + (threadIdx.x >> 6)) * 16, lane = threadIdx.x & 63;
+  const int first = ((int)(blockIdx.x % groups) * 4 + (threadIdx.x >> 6)) * kWaveSpans, lane = threadIdx.x & 63;
   const float* z = row_logits(j.a, r);
   if (!z || first >= j.spans) return;
-  f4 v[16];
-  if ((first + 16) * kSpan <= j.a.V) {
+  f4 v[kWaveSpans];
+  if ((first + kWaveSpans) * kSpan <= j.a.V) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) v[k] = *(const f4*)(z + (first + k) * kSpan + lane * 4);
+    for (int k = 0; k < kWaveSpans; ++k)
+      v[k] = __builtin_nontemporal_load((const f4*)(z + (first + k) * kSpan + lane * 4));
   } else {
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
+    for (int k = 0; k < kWaveSpans; ++k)
       v[k] = first + k < j.spans ? load_span(z, j.a.V, first + k) : f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
   }
   float mine = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 16; ++k) {
+  for (int k = 0; k < kWaveSpans; ++k) {
     // NaN counts as -inf: fmaxf takes the other operand
     const float m = last_lane_max(fmaxf(fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])), -INFINITY));
     const float s = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), 63));
     mine = lane == k ? s : mine;
   }
-  if (lane < 16 && first + lane < j.spans) j.span_max[r * j.spans + first + lane] = mine;
+  if (lane < kWaveSpans && first + lane < j.spans) j.span_max[r * j.spans + first + lane] = mine;
   mine = last_lane_max(mine);
   if (lane == 63) j.chunk_max[r * j.chunks + first * kSpan / kChunk] = mine;
 }
@@ -270,7 +273,7 @@ __global__ __launch_bounds__(256, 6) void verify_sum_kernel(Job j, long long wav
   const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, sp = part * kPart + lane;
   float top = -INFINITY;
 #pragma unroll
-  for (int k = 0; k < 4; ++k)  // at most 256 chunks
+  for (int k = 0; k < 8; ++k)  // at most 512 chunks
     if (64 * k < j.chunks) top = fmaxf(top, j.chunk_max[r * j.chunks + min(64 * k + lane, j.chunks - 1)]);
   const bool mine = lane < kPart && sp < j.spans;
   const float m = j.span_max[r * j.spans + min(sp, j.spans - 1)];
@@ -634,8 +637,8 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.draws = (DrawInfo*)(a0.ws + z.draws);
   j.listed = (unsigned short*)(a0.ws + z.listed);
   const long long rows = (long long)a0.S * (j.a.draft ? 2 * a0.K + 1 : a0.K + 1);
-  const int groups = (z.spans + kSpansPerWg - 1) / kSpansPerWg;
-  const long long waves = rows * z.parts2;  // at most 2^24: rows x 16384 ids are bounded
+  const int groups = (z.spans + 4 * kWaveSpans - 1) / (4 * kWaveSpans);
+  const long long waves = rows * z.parts2;  // at most 2^23: rows x 8192 ids are bounded
   hipLaunchKernelGGL(verify_max_kernel, dim3((unsigned)(rows * groups)), dim3(256), 0, s, j, groups);
   if (T == 0.0) {
     hipLaunchKernelGGL(verify_greedy_kernel, dim3(a0.S), dim3(256), 0, s, j);
