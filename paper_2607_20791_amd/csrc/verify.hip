@@ -6,18 +6,18 @@
 // this way are distributed as if drawn from p one by one: x is emitted with
 // probability min(p, q) + (1 - sum min(p, q)) max(p - q, 0) / sum max(p - q, 0) = p.
 //
-// One read of all logits bounds it.  Pass 1 streams them and keeps the maximum of
-// every 256 ids (a span): with a row's maximum its threshold is known, and
-// only spans whose maximum reaches it hold kept ids.  Those alone are read again,
-// for the rows' sums (pass 2), for the rest of p over q in the one row per sequence
-// that is drawn from (pass 3), and four of them for the draw (pass 4).  Weights
+// One read of all logits bounds it.  Pass 1 streams them and keeps the maxima of every
+// 64 ids (a quarter of a span): with a row's maximum its threshold is known, and only
+// quarters whose maximum reaches it hold kept ids.  Those alone are read again for the rows'
+// sums (pass 2), the spans that hold any for the rest of p over q in the one row per sequence
+// that is drawn from (pass 3), and four spans for the draw (pass 4).  Weights
 // and sums are fp64: the token drawn hangs on sums of up to 2^20 weights, which fp32
 // would leave wrong in one draw of a few.  T == 0: pass 1, then the first
 // id of each row's maximum.
 //
 // Measured, passes 1 to 4: 64 sequences of up to 4 drafts with logits of their own (512 rows of
-// 152064 in all, 311 MB) 47 + 36 + 18 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 36 + 10 + 7 + 6; one
-// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.5 + 4.5 + 5.9 + 4.4, launches and latency.
+// 152064 in all, 311 MB) 47 + 26 + 18 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 38 + 8 + 7 + 6; one
+// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.3 + 4.5 + 6.2 + 4.4, launches and latency.
 #include <algorithm>
 #include <cmath>
 
@@ -28,6 +28,7 @@ namespace rgd {
 namespace {
 
 constexpr int kSpan = 256;       // ids per span: one wave, four a lane
+constexpr int kQuarter = 64;     // ids per quarter of a span: 16 lanes
 constexpr int kWaveSpans = 8;    // pass 1: spans of a wave
 constexpr int kChunk = kWaveSpans * kSpan;
 constexpr int kMaxSpans = 4096;
@@ -67,7 +68,7 @@ struct Job {
   VerifyArgs a;
   double per_z, low;  // log2(e) / T; kept: z - max >= low
   int spans, chunks, groups, parts2, parts3;
-  float* span_max;    // [rows][spans]
+  float* quarter_max; // [rows][spans][4]
   float* chunk_max;   // [rows][chunks]
   float* top;         // [rows]
   double* sums;       // [rows][parts2]
@@ -111,6 +112,13 @@ RGD_DEV float max_step(float v) {
   const int b = __float_as_int(v);
   return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(b, b, CTRL, ROWS, 0xf, false)));
 }
+// the maximum over 16 lanes, in all of them
+RGD_DEV float row_max(float v) {
+  v = max_step<0x128, 0xf>(v);  // row_ror 8, 4, 2, 1
+  v = max_step<0x124, 0xf>(v);
+  v = max_step<0x122, 0xf>(v);
+  return max_step<0x121, 0xf>(v);
+}
 // the maximum over the wave, in its last lane
 RGD_DEV float last_lane_max(float v) {
   v = max_step<0x111, 0xf>(v);  // row_shr 1, 2, 4, 8
@@ -121,10 +129,10 @@ RGD_DEV float last_lane_max(float v) {
   return max_step<0x143, 0xc>(v);
 }
 
-// 8 KB a wave in flight at once, then the spans' maxima by row shifts between lanes.  311 MB: 47 us,
+// 8 KB a wave in flight at once, then the quarters' maxima by rotations of 16 lanes.  311 MB: 47 us,
 // 6.6 TB/s: memory bounds it (reads counted there: 1.00 times the bytes).  The loads are nontemporal: without
-// that 54 us, and pass 2, which then finds some of its spans in the last-level cache, 31 in
-// place of 36.  One sequence of 4 drafts: 3.5 us, with 16 spans a wave 4.5.  Putting candidate ids aside here
+// that 54 us, and 5 us less in pass 2, which then finds some of its ids in the last-level cache.  One
+// sequence of 4 drafts: 3.3 us, with 16 spans a wave 4.5.  Putting candidate ids aside here
 // costs 19 us.
 __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
   const long long r = blockIdx.x / groups;
@@ -145,11 +153,11 @@ __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
 #pragma unroll
   for (int k = 0; k < kWaveSpans; ++k) {
     // NaN counts as -inf: fmaxf takes the other operand
-    const float m = last_lane_max(fmaxf(fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])), -INFINITY));
-    const float s = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), 63));
-    mine = lane == k ? s : mine;
+    const float m = row_max(fmaxf(fmaxf(fmaxf(v[k][0], v[k][1]), fmaxf(v[k][2], v[k][3])), -INFINITY));
+    mine = (lane & 15) == k ? m : mine;
   }
-  if (lane < kWaveSpans && first + lane < j.spans) j.span_max[r * j.spans + first + lane] = mine;
+  const int sp = first + (lane & 15);
+  if ((lane & 15) < kWaveSpans && sp < j.spans) j.quarter_max[(r * j.spans + sp) * 4 + lane / 16] = mine;
   mine = last_lane_max(mine);
   if (lane == 63) j.chunk_max[r * j.chunks + first * kSpan / kChunk] = mine;
 }
@@ -196,10 +204,13 @@ struct SpanMax {
   int per;
   RGD_DEV void load(const Job& j, long long r) {
     per = (j.spans + 255) / 256;
-    const float* row = j.span_max + r * j.spans;
+    const f4* row = (const f4*)j.quarter_max + r * j.spans;
 #pragma unroll
     for (int k = 0; k < kMaxSpans / 256; ++k)
-      if (k < per) m[k] = row[min(per * (int)threadIdx.x + k, j.spans - 1)];
+      if (k < per) {
+        const f4 q = row[min(per * (int)threadIdx.x + k, j.spans - 1)];
+        m[k] = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
+      }
   }
   // the spans that reach thr, in order, by the whole workgroup: list[0 .. n); red: 4 ints
   RGD_DEV int list(const Job& j, float thr, unsigned short* out, int* red) const {
@@ -261,48 +272,59 @@ RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
 
 // ------------------------------------------------------------------ pass 2 --
 // A row's maximum, from those of its chunks, and the kept sum of kPart of its spans, by
-// one wave.  Rows differ in kept ids by a factor of a hundred; small parts share that
-// out: 512 rows of 152064 ids, 200 kept ones in the middle row and 4600 in the
-// hundredth-largest, 39% of the spans read again (132 MB): 30 us, 35 for workgroups that put the
-// spans in a list first, 39 for 64 spans a wave and 32 for 16.  Vector instructions are
-// busy half of the time.
-__global__ __launch_bounds__(256, 6) void verify_sum_kernel(Job j, long long waves) {
+// one wave, which puts their quarters with kept ids in a list and reads sixteen at a time.  Rows
+// differ in kept ids by a factor of a hundred; small parts share that out: 512 rows of
+// 152064 ids, 200 kept ones in the middle row and 4600 in the hundredth-largest: 26.5 us, 36 by whole
+// spans, of which 39% hold kept ids (132 MB).  With those, 35 us for workgroups in place of waves
+// where waves took 31, 39 for 64 spans a wave and 32 for 16.
+__global__ __launch_bounds__(256, 5) void verify_sum_kernel(Job j, long long waves) {
+  __shared__ unsigned char lists[4][4 * kPart];
   const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (wave >= waves) return;
   const long long r = wave / j.parts2;
-  const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, sp = part * kPart + lane;
+  const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, V = j.a.V;
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < 8; ++k)  // at most 512 chunks
     if (64 * k < j.chunks) top = fmaxf(top, j.chunk_max[r * j.chunks + min(64 * k + lane, j.chunks - 1)]);
-  const bool mine = lane < kPart && sp < j.spans;
-  const float m = j.span_max[r * j.spans + min(sp, j.spans - 1)];
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  const int pair = part * kPart * 2 + lane, pairs = j.spans * 2;  // this lane's two quarters
+  const f2 m = ((const f2*)j.quarter_max)[r * pairs + min(pair, pairs - 1)];
   const float* z = row_logits(j.a, r);
   if (!z) return;
   top = wave_max(top);
   if (part == 0 && lane == 0) j.top[r] = top;
   if (!finite_top(top)) return;
   const float thr = threshold(top, j.low);
-  unsigned long long todo = __ballot(mine && m >= thr);
-  // up to four spans at a time, the next ones on their way
-  auto take = [&](f4 (&v)[kGroup]) {
+  const bool h0 = pair < pairs && m[0] >= thr, h1 = pair < pairs && m[1] >= thr;
+  const unsigned long long b0 = __ballot(h0), b1 = __ballot(h1), below = (1ull << lane) - 1;
+  const int n = __popcll(b0) + __popcll(b1), at = __popcll(b0 & below) + __popcll(b1 & below);
+  unsigned char* list = lists[threadIdx.x >> 6];
+  if (h0) list[at] = 2 * lane;
+  if (h1) list[at + h0] = 2 * lane + 1;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's lanes read what its lanes wrote
+  __builtin_amdgcn_wave_barrier();
+  // sixteen quarters at a time, each by 16 lanes, the next ones on their way
+  const bool whole = (part + 1) * kPart * kSpan <= V;
+  auto take = [&](int i0, f4 (&v)[kGroup]) {
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) {
-      if (todo) {
-        v[k] = load_span(z, j.a.V, part * kPart + __builtin_ctzll(todo));
-        todo &= todo - 1;
+      const int i = i0 + 4 * k + lane / 16, id = part * kPart * kSpan + list[min(i, n - 1)] * kQuarter + (lane & 15) * 4;
+      if (i >= n) {
+        v[k] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      } else if (whole) {
+        v[k] = *(const f4*)(z + id);
       } else {
-        v[k] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};  // weighs nothing
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[k][e] = id + e < V ? z[id + e] : -INFINITY;
       }
     }
   };
   double sum = 0.0;
   f4 v[kGroup], next[kGroup];
-  bool more = todo != 0;
-  if (more) take(v);
-  while (more) {
-    more = todo != 0;
-    if (more) take(next);
+  if (n > 0) take(0, v);
+  for (int i0 = 0; i0 < n; i0 += 4 * kGroup) {
+    if (i0 + 4 * kGroup < n) take(i0 + 4 * kGroup, next);
     // a kept logit per lane and turn: few lanes have more than one or two
     for (unsigned b = kept_bits(v, thr, kGroup); b; b &= b - 1)
       sum += exp2_f64(((double)pick(v, __builtin_ctz(b)) - (double)top) * j.per_z);
@@ -347,9 +369,10 @@ struct Draw {
 };
 
 // Accepted drafts of a sequence, one draft a thread (K <= 255), then the rest of the
-// drawn row in this part's spans.  64 sequences in 12 parts: 17 us, two dependent
-// chains (tokens and sums, accepted row, its maxima, its spans) beside 34 MB of reads; 20.8 us where
-// parts make more than three workgroups per CU.
+// drawn row in this part's spans.  64 sequences in 12 parts: 18 us: 7 for two
+// dependent chains (tokens and sums, accepted row, its maxima, its spans), 7 for 34 MB of reads, 4 for the
+// weights; 3 us more where parts make more than three workgroups per CU.  By quarters it takes 19: fewer
+// bytes, but fewer groups to share, each with more kept ids.
 __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
@@ -554,13 +577,14 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
   const int nd = drafts_of(a, s);
   for (int i = t >> 6; i <= nd; i += 4) {
     const long long r = target_row(a, s, i);
-    const float* m = j.span_max + r * j.spans;
+    const f4* m = (const f4*)j.quarter_max + r * j.spans;
+    auto span_max = [&](int k) { return fmaxf(fmaxf(m[k][0], m[k][1]), fmaxf(m[k][2], m[k][3])); };
     float top = -INFINITY;
-    for (int k = lane; k < j.spans; k += 64) top = fmaxf(top, m[k]);
+    for (int k = lane; k < j.spans; k += 64) top = fmaxf(top, span_max(k));
     top = wave_max(top);
     int sp = 0x7FFFFFFF, id = 0x7FFFFFFF;
     for (int k = lane; k < j.spans; k += 64)
-      if (m[k] == top) sp = min(sp, k);
+      if (span_max(k) == top) sp = min(sp, k);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sp = min(sp, __shfl_xor(sp, o, 64));
     if (finite_top(top)) {
@@ -587,7 +611,7 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
 struct Sizes {
   long long rows;
   int spans, chunks, groups, parts2, parts3;
-  size_t span_max, chunk_max, top, sums, rest, draws, listed, bytes;
+  size_t quarter_max, chunk_max, top, sums, rest, draws, listed, bytes;
 };
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
@@ -601,8 +625,8 @@ Sizes sizes_of(int S, int K, int V) {
   z.chunks = (V + kChunk - 1) / kChunk;
   z.parts2 = (z.spans + kPart - 1) / kPart;
   z.parts3 = std::min(kMaxParts, (767 + S) / S);
-  z.span_max = 0;
-  z.chunk_max = up256((size_t)z.rows * z.spans * 4);
+  z.quarter_max = 0;
+  z.chunk_max = up256((size_t)z.rows * z.spans * 16);
   z.top = z.chunk_max + up256((size_t)z.rows * z.chunks * 4);
   z.sums = z.top + up256((size_t)z.rows * 4);
   z.rest = z.sums + up256((size_t)z.rows * z.parts2 * 8);
@@ -629,7 +653,7 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.groups = z.groups;
   j.parts2 = z.parts2;
   j.parts3 = z.parts3;
-  j.span_max = (float*)(a0.ws + z.span_max);
+  j.quarter_max = (float*)(a0.ws + z.quarter_max);
   j.chunk_max = (float*)(a0.ws + z.chunk_max);
   j.top = (float*)(a0.ws + z.top);
   j.sums = (double*)(a0.ws + z.sums);
