@@ -233,24 +233,36 @@ __global__ __launch_bounds__(kPlan) void reserve_plan_kernel(PagedView c, const 
 }
 
 // Page `from` of one layer of one pool to page `to`: bytes (a multiple of 16) by
-// the whole workgroup.  A page of one layer is 32 KB in the common sizes, enough for a workgroup's
-// requests; which pages are copied is known on the device only, so a fixed grid takes them in turn.
+// the whole workgroup, eight requests of a thread in flight.  A page of one layer is 32 KB in the
+// common sizes, enough for a workgroup; which pages are copied is known on the device only, so a fixed
+// grid takes them in turn.  Stores go past the caches; so do loads where each page is read once (ONCE).
+template <bool ONCE>
 RGD_DEV void copy_page(char* pool, size_t page_bytes, size_t layer_page0, int from, int to) {
   const u32x4* src = (const u32x4*)(pool + (layer_page0 + from) * page_bytes);
   u32x4* dst = (u32x4*)(pool + (layer_page0 + to) * page_bytes);
   const size_t n = page_bytes / 16;
-  for (size_t i = threadIdx.x; i < n; i += 256) dst[i] = src[i];
+  auto load = [&](size_t i) { return ONCE ? __builtin_nontemporal_load(src + i) : src[i]; };
+  size_t i = threadIdx.x;
+  for (; i + 7 * 256 < n; i += 8 * 256) {
+    u32x4 v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = load(i + 256 * k);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) __builtin_nontemporal_store(v[k], dst + i + 256 * k);
+  }
+  for (; i < n; i += 256) __builtin_nontemporal_store(load(i), dst + i);
 }
 
-// The pages that reserve copies.  256 branches that grow from 32 prompts' last pages, 8 layers of 32 KB
-// K and V pages, 117 MB read and written: 20.6 us, 5.7 TB/s (part of it from the last-level cache).
+// The pages that reserve copies.  Branches of 32 prompts grow from their prompts' last pages, 8 layers of 32 KB
+// K and V pages, 117 MB read and written: 12.4 us, 9 TB/s, as a prompt's page is read once for all its branches
+// (20 us with cached stores or with loads past the caches, 17 with cached stores and eight requests in flight).
 __global__ __launch_bounds__(256) void copy_pairs_kernel(PagedView c, const int* ws, size_t page_bytes) {
   const int n = ws[0];
   const int* pairs = ws + 4;
   const long long items = (long long)n * 2 * c.L;
   for (long long i = blockIdx.x; i < items; i += gridDim.x) {
     const int k = (int)(i / (2 * c.L)), which = (int)(i % (2 * c.L));
-    copy_page(which & 1 ? c.pool_v : c.pool_k, page_bytes, (size_t)(which >> 1) * c.n_pages, pairs[2 * k],
+    copy_page<false>(which & 1 ? c.pool_v : c.pool_k, page_bytes, (size_t)(which >> 1) * c.n_pages, pairs[2 * k],
               pairs[2 * k + 1]);
   }
 }
@@ -302,8 +314,9 @@ __global__ __launch_bounds__(kPlan) void compact_plan_kernel(PagedView c, int* l
   }
 }
 
-// The tables follow the map, then the pages move, each read and written once.  1.04 GB read and
-// written: 207 us, 5.0 TB/s, what a large copy reaches, and no more at the memory than these bytes.
+// The tables follow the map, then the pages move, each read and written once.  1.04 GB read and written:
+// 194 us, 5.3 TB/s, what a large copy reaches, and no more at the memory than these bytes (198 us with
+// cached loads, 203 with cached stores too, 207 with one request in flight).
 __global__ __launch_bounds__(256) void compact_move_kernel(PagedView c, const int* ws, size_t page_bytes) {
   const int moves = ws[0];
   const int* map = ws + 4;
@@ -319,7 +332,7 @@ __global__ __launch_bounds__(256) void compact_move_kernel(PagedView c, const in
   const long long items = (long long)moves * 2 * c.L;
   for (long long i = blockIdx.x; i < items; i += gridDim.x) {
     const int k = (int)(i / (2 * c.L)), which = (int)(i % (2 * c.L));
-    copy_page(which & 1 ? c.pool_v : c.pool_k, page_bytes, (size_t)(which >> 1) * c.n_pages, list[moves + k], list[k]);
+    copy_page<true>(which & 1 ? c.pool_v : c.pool_k, page_bytes, (size_t)(which >> 1) * c.n_pages, list[moves + k], list[k]);
   }
 }
 
