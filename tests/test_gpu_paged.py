@@ -146,6 +146,20 @@ def test_a_long_table_and_a_large_pool(rgd):
     x.check()
 
 
+@pytest.mark.parametrize("hk,d,ps,bf16", [(5, 128, 48, True), (8, 128, 16, True), (3, 64, 64, False)])
+def test_pages_of_many_bytes_are_copied_and_moved(rgd, hk, d, ps, bf16):
+    """Pages of one and several rounds of a workgroup's copies, and of a part of one."""
+    x = Case(rgd, 4, 3, 14, layers=3, hk=hk, d=d, ps=ps, bf16=bf16, seed=hk)
+    assert x.reserve([ps + 5, 0, 2 * ps, 3])
+    x.append(1, 7, None)
+    x.select([0, 0, 0, 3], None)
+    assert x.reserve([4, 1, ps, 0])
+    x.check()
+    x.select(None, [0, -1, 1, -1])
+    assert x.compact() > 0
+    x.check()
+
+
 @pytest.mark.parametrize("bf16,d,ps,hk,stride", [(True, 32, 16, 3, 0), (True, 64, 32, 2, 16), (True, 128, 16, 8, 4096),
                                                  (False, 32, 16, 1, 8), (False, 64, 48, 2, 0), (False, 128, 16, 4, 128),
                                                  (True, 128, 4096, 1, 0)])
