@@ -26,9 +26,9 @@
 // layouts without a gather.
 //
 // Measured, 8 KV heads of 128, bf16, both kernels' times: one token of 64 sequences of up to 8192
-// positions (253 MB of K and V) 51 + 5 us, 5.0 TB/s, and of one of 131072 (537 MB) 96 + 6 us, 5.6 TB/s:
+// positions (253 MB of K and V) 47 + 5 us, 5.4 TB/s, and of one of 131072 (537 MB) 96 + 6 us, 5.6 TB/s:
 // the reads bound them, of which the memory sees 1.02 and 1.06 times the bytes.  Five tokens
-// of 32 sequences of up to 4096 (73 MB) 22 + 5 us, 16 of 16 sequences of 4096 (268 MB) 65 + 5.  One token over
+// of 32 sequences of up to 4096 (73 MB) 21 + 5 us, 16 of 16 sequences of 4096 (268 MB) 63 + 5.  One token over
 // 512 positions 6.3 + 2.8 us: two launches and a chain of reads (lengths, table, K and V, pieces).  One token
 // of 1024 sequences of up to 500 (354 MB): 115 us, as an item is a step or two of one to three waves.
 #include <algorithm>
@@ -306,8 +306,8 @@ struct Walk {
   }
 };
 
-// D dimensions, NT tiles of 16 query vectors.
-template <typename T, int D, int NT>
+// D dimensions, NT tiles of 16 query vectors; PAST: V is loaded past the caches.
+template <typename T, int D, int NT, bool PAST>
 struct Piece {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int NB = BF ? 2 : 1;             // 16-position blocks per round
@@ -362,7 +362,8 @@ struct Piece {
     else at = vb[0] + (size_t)row * a.c.ps * 4 + grp * 16;
     const size_t step = (size_t)16 * a.c.ps * sizeof(T);
 #pragma unroll
-    for (int d = 0; d < VL; ++d) v[d] = *(const u32x4*)(at + d * step);
+    for (int d = 0; d < VL; ++d)
+      v[d] = PAST ? __builtin_nontemporal_load((const u32x4*)(at + d * step)) : *(const u32x4*)(at + d * step);
   }
 
   RGD_DEV void scores(f32x4 (&s)[NT][NB]) const {
@@ -614,9 +615,9 @@ constexpr size_t slot_floats() {
 // Whether a CU holds two workgroups (row: bytes of a row of K).
 constexpr bool two_per_cu(int nt, size_t row) { return nt == 1 || (nt == 2 && row < 512); }
 
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, bool PAST>
 __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
-  using P = Piece<T, D, NT>;
+  using P = Piece<T, D, NT, PAST>;
   constexpr int COLS = P::COLS, LD = D + 4, COST = item_cost(NT);
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
@@ -785,7 +786,13 @@ int runs_for(const PagedView& c, int n, int Hq) {
 template <typename T, int D, int NT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
   const int runs = runs_for(a.c, a.n, a.Hq);
-  hipLaunchKernelGGL((attn_run_kernel<T, D, NT>), dim3(runs), dim3(256), 0, s, a, runs);
+  // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
+  // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
+  // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
+  if (a.c.ps <= Piece<T, D, NT, true>::PER)
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true>), dim3(runs), dim3(256), 0, s, a, runs);
+  else
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false>), dim3(runs), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
   const int cols = std::min(16 * NT, a.n * a.G);
   const dim3 grid(runs, (cols + join_cols(NT) - 1) / join_cols(NT));
