@@ -271,6 +271,15 @@ def test_attention_of_several_tokens(rgd, bf16, n, hk, G, d, ps):
 
 
 @pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("ps,n", [(32, 1), (64, 1), (48, 6), (16, 16), (64, 16)])
+def test_attention_at_every_page_size(rgd, bf16, d, ps, n):
+    """One, two and four query tiles over pages of one and several rounds."""
+    x = _filled(rgd, [0, 1, 31, 33, 63, 65, 129, 200, 400], hk=2, d=d, ps=ps, bf16=bf16, seed=ps + n)
+    _attention(x, 1, 8, n, None)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
 def test_attention_splits_a_long_sequence(rgd, bf16):
     x = _filled(rgd, [3001, 1, 0, 1500], hk=1, d=64, bf16=bf16, seed=5)
     _attention(x, 1, 4, 1, None, spread=3.0)
