@@ -16,8 +16,8 @@
 // id of each row's maximum.
 //
 // Measured, passes 1 to 4: 64 sequences of up to 4 drafts with logits of their own (512 rows of
-// 152064 in all, 311 MB) 47 + 26 + 18 + 7 us; 32 greedy probes of up to 15 tokens (230 MB) 38 + 8 + 7 + 6; one
-// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.3 + 4.5 + 6.2 + 4.4, launches and latency.
+// 152064 in all, 311 MB) 47 + 26 + 18 + 6 us; 32 greedy probes of up to 15 tokens (230 MB) 38 + 8 + 7 + 5; one
+// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.3 + 4.5 + 6.2 + 4.0, launches and latency.
 #include <algorithm>
 #include <cmath>
 
@@ -377,13 +377,14 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
   __shared__ DrawInfo info;
-  __shared__ double sums[2 * 255 + 1];  // of the target's rows 0 .. nd, then the drafts'
+  __shared__ double sums[2 * 255 + 1];  // of the target's rows, then the drafts'
   const VerifyArgs& a = j.a;
   const int s = blockIdx.x / j.parts3, part = blockIdx.x % j.parts3, t = threadIdx.x, w = t >> 6;
   const int id = t < a.K ? a.tokens[(long long)s * a.K + t] : -1;
   const int nd = drafts_of(a, s);
-  for (int q = t / 16; q < (a.draft ? 2 * nd + 1 : nd + 1); q += 16) {  // 16 lanes a row
-    const double* part = j.sums + (q <= nd ? target_row(a, s, q) : draft_row(a, s, q - nd - 1)) * j.parts2;
+  // 16 lanes a row; all K of them, so that the loads need not wait for the count
+  for (int q = t / 16; q < (a.draft ? 2 * a.K + 1 : a.K + 1); q += 16) {
+    const double* part = j.sums + (q <= a.K ? target_row(a, s, q) : draft_row(a, s, q - a.K - 1)) * j.parts2;
     double x = 0.0;
 #pragma unroll 8
     for (int k = t % 16; k < j.parts2; k += 16) x += part[k];
@@ -405,7 +406,7 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
     if (a.draft && drafted) {
       const float* zq = a.draft + ((long long)s * a.K + t) * a.V;
       const float xq = zq[inside ? id : 0];
-      q = dist_of(j, zq, draft_row(a, s, t), sums[nd + 1 + t]);
+      q = dist_of(j, zq, draft_row(a, s, t), sums[a.K + 1 + t]);
       qx = q.p(xq);
     }
     if (drafted) ok = inside && (double)a.u[(long long)s * (a.K + 1) + t] * qx < p.p(xp);
@@ -455,25 +456,37 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
 }
 
 // ------------------------------------------------------------------ pass 4 --
-RGD_DEV double block_scan_f64(double v, double* red, double& total) {  // exclusive
+// Exclusive scans of N values each; red: 4 N doubles.
+template <int N>
+RGD_DEV void block_scan_f64(const double (&v)[N], double* red, double (&before)[N], double (&total)[N]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  double incl = v;
+  double incl[N];
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const double x = __shfl_up(incl, o, 64);
-    if (lane >= o) incl += x;
-  }
-  __syncthreads();
-  if (lane == 63) red[w] = incl;
-  __syncthreads();
-  double before = 0.0;
-  total = 0.0;
+  for (int i = 0; i < N; ++i) incl[i] = v[i];
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    before += k < w ? red[k] : 0.0;
-    total += red[k];
+  for (int o = 1; o < 64; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const double x = __shfl_up(incl[i], o, 64);
+      if (lane >= o) incl[i] += x;
+    }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (lane == 63) red[4 * i + w] = incl[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    before[i] = incl[i] - v[i];
+    total[i] = 0.0;
+    double ahead = 0.0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      ahead += k < w ? red[4 * i + k] : 0.0;
+      total[i] += red[4 * i + k];
+    }
+    before[i] = ahead + before[i];
   }
-  return before + (incl - v);
 }
 
 RGD_DEV int block_min_i(int v, int* red) {
@@ -484,16 +497,40 @@ RGD_DEV int block_min_i(int v, int* red) {
   __syncthreads();
   return min(min(red[0], red[1]), min(red[2], red[3]));
 }
+// The first thread's `hit` that is one (>= 0), or where there is none the last thread's `last`; both rise with
+// the thread.  red: 8 ints.
+RGD_DEV int first_or_last(int hit, int last, int* red) {
+  const unsigned long long h = __ballot(hit >= 0), l = __ballot(last >= 0);
+  const int hv = h ? __builtin_amdgcn_readlane(hit, __builtin_ctzll(h)) : -1;
+  const int lv = l ? __builtin_amdgcn_readlane(last, 63 - __builtin_clzll(l)) : -1;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) {
+    red[threadIdx.x >> 6] = hv;
+    red[4 + (threadIdx.x >> 6)] = lv;
+  }
+  __syncthreads();
+  int first = -1, end = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    first = first < 0 ? red[w] : first;
+    end = max(end, red[4 + w]);
+  }
+  return first >= 0 ? first : end;
+}
 
 // The draw: the group, then the id, whose running sum first exceeds u times the total;
-// where rounding leaves none, the last one with weight.  4.4 to 6.8 us: one chain of three reads
-// (the pass before's result, the groups' sums, a group's logits) and four scans.
+// where rounding leaves none, the last one with weight.  4.0 to 6.0 us: one chain of two reads
+// (the pass before's result with the groups' sums, a group's logits), two scans and two searches by ballots
+// (4.4 to 6.8 with the groups' sums asked for after the result, and by minima over the workgroup).
 __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
-  __shared__ double red[4];
-  __shared__ int redi[4];
+  __shared__ double red[8];
+  __shared__ int redi[8];
   __shared__ double sh_before;
   const VerifyArgs& a = j.a;
   const int s = blockIdx.x, t = threadIdx.x;
+  double2 part[4];  // asked for before the number of groups is known
+#pragma unroll
+  for (int k = 0; k < 4; ++k) part[k] = j.rest[(long long)s * j.groups + min(4 * t + k, j.groups - 1)];
   const DrawInfo di = j.draws[s];
   const int acc = di.accepted, n = di.n;
   const float u = a.u[(long long)s * (a.K + 1) + a.K];
@@ -506,20 +543,18 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   }
   const Draw d(j, s, di);
   const int groups = (n + kGroup - 1) / kGroup;  // at most 1024
-  double2 part[4];
   double mine[2] = {0.0, 0.0}, total[2], before[2];
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
-    part[k] = 4 * t + k < groups ? j.rest[(long long)s * j.groups + 4 * t + k] : double2{0.0, 0.0};
+    if (4 * t + k >= groups) part[k] = double2{0.0, 0.0};
     mine[0] += part[k].x;
     mine[1] += part[k].y;
   }
-  before[0] = block_scan_f64(mine[0], red, total[0]);
-  before[1] = block_scan_f64(mine[1], red, total[1]);
+  block_scan_f64<2>(mine, red, before, total);
   const int use = total[0] > 0.0 ? 0 : 1;  // nothing left by rounding: p itself
   const double goal = (double)u * total[use];
   double run = before[use], at[4];
-  int hit = 0x7FFFFFFF, last = 0;
+  int hit = -1, last = -1;
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const double x = use ? part[k].y : part[k].x;
@@ -527,11 +562,10 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
     if (x > 0.0) {
       run += x;
       last = 4 * t + k;
-      if (hit == 0x7FFFFFFF && run > goal) hit = 4 * t + k;
+      if (hit < 0 && run > goal) hit = 4 * t + k;
     }
   }
-  hit = block_min_i(hit, redi);
-  if (hit == 0x7FFFFFFF) hit = -block_min_i(-last, redi);
+  hit = first_or_last(hit, last, redi);
 #pragma unroll
   for (int k = 0; k < 4; ++k)
     if (hit == 4 * t + k) sh_before = at[k];
@@ -541,7 +575,7 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
   const bool have = sp < n;
   const int id0 = j.listed[(long long)s * j.spans + (have ? sp : 0)] * kSpan + 4 * (t & 63);
   run = sh_before;
-  double x[4], sum = 0.0, unused;
+  double x[4], sum[1] = {0.0}, ahead[1], unused[1];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     x[e] = 0.0;
@@ -550,20 +584,20 @@ __global__ __launch_bounds__(256) void verify_draw_kernel(Job j) {
       const double2 v = d.rest(zp, d.minus_q ? d.q.z[id0 + e] : zp, id0 + e);
       x[e] = use ? v.y : v.x;
     }
-    sum += x[e];
+    sum[0] += x[e];
   }
-  run += block_scan_f64(sum, red, unused);
-  int found = 0x7FFFFFFF, end = -1;
+  block_scan_f64<1>(sum, red, ahead, unused);
+  run += ahead[0];
+  int found = -1, end = -1;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (x[e] > 0.0) {
       run += x[e];
       end = id0 + e;
-      if (found == 0x7FFFFFFF && run > goal) found = id0 + e;
+      if (found < 0 && run > goal) found = id0 + e;
     }
-  found = block_min_i(found, redi);
-  end = -block_min_i(-end, redi);
-  if (t == 0) out[acc] = found != 0x7FFFFFFF ? found : max(end, 0);
+  const int id = first_or_last(found, end, redi);
+  if (t == 0) out[acc] = id;
 }
 
 // ------------------------------------------------------------------ T == 0 --
