@@ -270,7 +270,7 @@ __global__ __launch_bounds__(256) void copy_pairs_kernel(PagedView c, const int*
 // --------------------------------------------------------------- compact ----
 // One workgroup: the number n of live pages, then in order the free pages below
 // n and the live ones at or above it (as many of each).  ws: [0] moves, map
-// [n_pages], list [n_pages].  16384 pages: 8.9 us (29.6 with one
+// [n_pages], list [n_pages].  16384 pages: 8.1 us (29.6 with one
 // load a thread in flight).
 __global__ __launch_bounds__(kPlan) void compact_plan_kernel(PagedView c, int* live, int* ws) {
   __shared__ int red[kPlan / 64];
