@@ -71,6 +71,9 @@ def test_attention_arguments(rgd):
     huge = _desc(rgd, max_seqs=65536, max_pages=1 << 26, n_kv_heads=1024)
     assert lib.rgd_paged_attention_workspace_bytes(huge, 1, 1024) == 0 and b"tables" in lib.rgd_last_error()
     assert lib.rgd_paged_attention_workspace_bytes(_desc(rgd, max_seqs=65536), 257, 4) == 0
+    # 4096 sequences of 2^28 positions, 8 KV heads: a run of 256 would be past 31 bits of steps
+    assert lib.rgd_paged_attention_workspace_bytes(
+        _desc(rgd, max_seqs=4096, max_pages=65536, page_size=4096, n_kv_heads=8), 1, 512) == 0
     for n, h in ((0, 4), (1025, 4), (1, 0), (1, 3), (1, 1026)):
         assert lib.rgd_paged_attention_workspace_bytes(d, n, h) == 0
 
