@@ -503,7 +503,8 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * token is drawn from max(p_i - q_i, 0), after n_draft acceptances from p_i, by
  * u[K]: the smallest id whose running weight exceeds u[K] times the total.
  * out dev int32 [S][K+1]: the accepted drafts, the drawn token, then -1;
- * n_accepted dev int32 [S].  A draft outside [0, V) is refused.  NaN logits
+ * n_accepted dev int32 [S]; neither may overlap the other or an input.  A draft
+ * outside [0, V) is refused.  NaN logits
  * count as -inf.  A target row whose maximum is not finite has no distribution:
  * its draft is refused and -1 stands for the drawn token; such a draft row has
  * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, S (2 K + 1)

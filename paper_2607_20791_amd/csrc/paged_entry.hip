@@ -42,6 +42,10 @@ const char* view_of(const rgd_paged_cache* c, PagedView& v) {
 
 int32_t bad(const char* why) { return set_error(RGD_E_INVALID_ARG, why); }
 
+bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
+  return a && b && (uintptr_t)a < (uintptr_t)b + (uintptr_t)nb && (uintptr_t)b < (uintptr_t)a + (uintptr_t)na;
+}
+
 int32_t launched(hipError_t e) { return e == hipSuccess ? (int32_t)RGD_OK : set_error(RGD_E_HIP, hipGetErrorString(e)); }
 
 // rows of `width` elements, ld elements apart
@@ -138,9 +142,7 @@ int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const v
   const int64_t width = (int64_t)n_heads * a.c.D, rows = (int64_t)a.c.S * n;
   if (const char* why = rows_ok(a.c, q, ldq, width)) return bad(why);
   if (!aligned(out, 16) || !aligned(workspace, 256)) return bad("out must be 16-byte, the workspace 256-byte aligned");
-  const uintptr_t q0 = (uintptr_t)q, q1 = q0 + (uintptr_t)(((rows - 1) * ldq + width) * a.c.esz);
-  const uintptr_t o0 = (uintptr_t)out, o1 = o0 + (uintptr_t)(rows * width * a.c.esz);
-  if (q0 < o1 && o0 < q1) return bad("out overlaps q");
+  if (overlap(q, ((rows - 1) * ldq + width) * a.c.esz, out, rows * width * a.c.esz)) return bad("out overlaps q");
   const size_t layer0 = (size_t)layer * a.c.n_pages * a.c.page_elems() * a.c.esz;
   a.pool_k = a.c.pool_k + layer0;
   a.pool_v = a.c.pool_v + layer0;
@@ -170,6 +172,14 @@ int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t
   if (!(T >= 0.f && T < 3e38f)) return bad("T must be >= 0 and finite");
   if (!(min_p >= 0.f && min_p <= 1.f)) return bad("min_p must be in [0,1]");
   if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+  const int64_t s = S, k = K, kept = s * (k + 1) * 4, counts = s * 4;  // bytes of out, of n_accepted
+  const struct {
+    const void* p;
+    int64_t n;
+  } inputs[] = {{target, kept * V}, {draft, s * k * 4 * V}, {draft_tokens, s * k * 4}, {n_draft, counts}, {u, kept}};
+  for (const auto& in : inputs)
+    if (overlap(out, kept, in.p, in.n) || overlap(n_accepted, counts, in.p, in.n)) return bad("an output overlaps an input");
+  if (overlap(out, kept, n_accepted, counts)) return bad("out overlaps n_accepted");
   VerifyArgs a{target, draft, draft_tokens, n_draft, S, K, V, T, min_p, u, out, n_accepted, (char*)workspace};
   return launched(verify_drafts(a, (hipStream_t)stream));
 }

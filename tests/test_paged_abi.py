@@ -18,6 +18,7 @@ GOOD = dict(n_layers=2, n_pages=8, n_kv_heads=2, page_size=16, head_dim=64, dtyp
 WS = C.c_void_p(0x10000)
 P = C.c_void_p(0x40000)
 OUT = C.c_void_p(0x80000)
+W2 = C.c_void_p(0x90000)
 
 
 def _desc(rgd, **kw):
@@ -95,6 +96,9 @@ def test_verify_arguments(rgd):
     def call(target=P, tokens=P, S=2, K=4, V=101, T=1.0, min_p=0.1, u=P, ws=WS, out=OUT, count=OUT):
         return lib.rgd_verify_drafts(target, None, tokens, None, S, K, V, T, min_p, u, ws, out, count, None)
 
+    for kw in (dict(out=P), dict(count=P), dict(tokens=OUT, count=W2), dict(u=C.c_void_p(0x80000 - 36), count=W2),
+               dict(u=C.c_void_p(0x80000 + 36), count=W2), dict(count=C.c_void_p(0x80000 + 36))):
+        assert call(**kw) == INVALID and b"overlap" in lib.rgd_last_error(), kw
     nan = float("nan")
     for kw in (dict(target=None), dict(tokens=None), dict(u=None), dict(ws=None), dict(out=None), dict(count=None),
                dict(S=0), dict(K=0), dict(V=1), dict(T=-1.0), dict(T=nan), dict(T=float("inf")), dict(min_p=1.5),
