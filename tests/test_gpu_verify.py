@@ -72,6 +72,38 @@ def test_the_largest_vocabularies(rgd, V):
         _compare(rgd, target, draft, tokens, None, T, min_p, u)
 
 
+@pytest.mark.parametrize("V", [63, 64, 65, 255, 256, 257, 2047, 2048, 2049, 8191, 8192, 16385])
+def test_vocabularies_at_the_borders_of_what_a_wave_reads(rgd, V):
+    for T, min_p in ((1.0, 0.05), (1.5, 0.0), (0.0, 0.0)):
+        target, draft, tokens, u = _inputs(V, 5, 3, V, T, min_p=min_p)
+        _compare(rgd, target, draft, tokens, [3, 0, 1, 2, 3], T, min_p, u)
+        target[:, :, -3:] += 12  # what is kept lies at the row's end, a NaN among it
+        target[:, :, -2] = np.nan
+        _compare(rgd, target, draft, tokens, None, T, min_p, u)
+        _compare(rgd, target, None, np.full((5, 3), V - 1), None, T, min_p, u)
+
+
+def test_logits_beyond_32_bits(rgd):
+    """More than 2^31 logits: the last sequence's draws, the others without drafts."""
+    t = torch()
+    S, K, V = 20, 110, 1 << 20
+    assert S * (K + 1) * V > 2**31
+    target, draft, tokens, u = _inputs(5, 1, 3, V, 1.0, min_p=0.05)
+    z, x = t.zeros(S, K + 1, V, device="cuda"), t.zeros(S, K, dtype=t.int32, device="cuda")
+    z[-1, :4] = t.from_numpy(target[0]).cuda()
+    x[-1, :3] = t.from_numpy(tokens[0].astype(np.int32)).cuda()
+    nd = t.zeros(S, dtype=t.int32, device="cuda")
+    nd[-1] = 3
+    us = t.full((S, K + 1), 0.5, device="cuda")
+    us[-1, :3], us[-1, K] = t.from_numpy(u[0, :3]).cuda(), float(u[0, 3])
+    out, cnt = (t.empty(*s, dtype=t.int32, device="cuda") for s in ((S, K + 1), (S,)))
+    ws = t.empty(rgd.verify_workspace_bytes(S, K, V), dtype=t.uint8, device="cuda")
+    rgd.verify_drafts(z, None, x, nd, 1.0, float(np.float32(0.05)), us, ws, out, cnt)
+    want, n = ov.verify(target[0], None, tokens[0], 3, 1.0, float(np.float32(0.05)), u[0])
+    assert int(cnt[-1]) == n and out[-1, :4].tolist() == want.tolist()
+    assert bool((cnt[:-1] == 0).all()) and bool((out[:-1, 0] == V // 2).all())  # equal logits: half of the ids
+
+
 def test_ragged_counts_and_tokens_outside(rgd):
     target, draft, tokens, u = _inputs(3, 9, 5, 777)
     n = [0, 1, 2, 3, 4, 5, -4, 99, 5]
