@@ -824,7 +824,8 @@ hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
 // the plan's units, whatever the lengths are, in numbers that it can count with
 bool paged_attention_fits(const PagedView& c, int n, int Hq) {
   const int nt = tiles_for(c, n * (Hq / c.Hkv)), tiles = (n * (Hq / c.Hkv) + 16 * nt - 1) / (16 * nt);
-  return (double)c.S * c.Hkv * tiles * (std::ceil((double)c.width * c.ps / kStep) + item_cost(nt)) < 274877906944.0;  // 2^38: a run's share of it is counted in ints
+  const double units = (double)c.S * c.Hkv * tiles * (std::ceil((double)c.width * c.ps / kStep) + item_cost(nt));
+  return units < 274877906944.0;  // 2^38: a run's share of it is counted in ints
 }
 
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {

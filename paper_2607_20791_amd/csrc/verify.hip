@@ -16,8 +16,8 @@
 // id of each row's maximum.
 //
 // Measured, passes 1 to 4: 64 sequences of up to 4 drafts with logits of their own (512 rows of
-// 152064 in all, 311 MB) 47 + 26 + 18 + 6 us; 32 greedy probes of up to 15 tokens (230 MB) 38 + 8 + 7 + 5; one
-// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.3 + 4.5 + 6.2 + 4.0, launches and latency.
+// 152064 in all, 311 MB) 47 + 27 + 19 + 6 us; 32 greedy probes of up to 15 tokens (230 MB) 38 + 8 + 7 + 5; one
+// sequence of 4 drafts (9 rows of 128256, 4.6 MB) 3.3 + 4.5 + 6.1 + 4.0, launches and latency.
 #include <algorithm>
 #include <cmath>
 
@@ -32,8 +32,9 @@ constexpr int kQuarter = 64;     // ids per quarter of a span: 16 lanes
 constexpr int kWaveSpans = 8;    // pass 1: spans of a wave
 constexpr int kChunk = kWaveSpans * kSpan;
 constexpr int kMaxSpans = 4096;
-constexpr int kPart = 32;        // spans of a wave in pass 2
+constexpr int kMaxPart = 32;     // spans of a wave in pass 2, at most
 constexpr int kMaxParts = 16;    // workgroups that share a row in pass 3
+constexpr int kResident = 5120;  // waves of pass 2 at a time: 20 per CU
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
 
@@ -67,7 +68,7 @@ struct DrawInfo;
 struct Job {
   VerifyArgs a;
   double per_z, low;  // log2(e) / T; kept: z - max >= low
-  int spans, chunks, groups, parts2, parts3;
+  int spans, chunks, groups, part, parts2, parts3;
   float* quarter_max; // [rows][spans][4]
   float* chunk_max;   // [rows][chunks]
   float* top;         // [rows]
@@ -258,6 +259,12 @@ RGD_DEV unsigned kept_bits(const f4 (&v)[kGroup], float thr, int spans_left) {
   return m;
 }
 
+// Whether some lane has so many kept logits of its 16 that all of them are weighed one after the other, in
+// place of one kept logit per lane and turn, of which few lanes have more than one or two.  72 rows of
+// 152064 ids that are all kept: pass 2 takes 24 us in place of 49, pass 3 20 in place of 27; a bound of 4 is
+// as fast as 6, 9 slower between few and all.
+RGD_DEV bool dense(unsigned bits) { return __any(__popc(bits) > 6); }
+
 // v[i / 4][i % 4] by selects
 RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
   float a[4];
@@ -271,24 +278,24 @@ RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
 }
 
 // ------------------------------------------------------------------ pass 2 --
-// A row's maximum, from those of its chunks, and the kept sum of kPart of its spans, by
+// A row's maximum, from those of its chunks, and the kept sum of j.part of its spans, by
 // one wave, which puts their quarters with kept ids in a list and reads sixteen at a time.  Rows
 // differ in kept ids by a factor of a hundred; small parts share that out: 512 rows of
-// 152064 ids, 200 kept ones in the middle row and 4600 in the hundredth-largest: 26.5 us, 36 by whole
+// 152064 ids, 200 kept ones in the middle row and 4600 in the hundredth-largest: 27.5 us, 36 by whole
 // spans, of which 39% hold kept ids (132 MB).  With those, 35 us for workgroups in place of waves
 // where waves took 31, 39 for 64 spans a wave and 32 for 16.
 __global__ __launch_bounds__(256, 5) void verify_sum_kernel(Job j, long long waves) {
-  __shared__ unsigned char lists[4][4 * kPart];
+  __shared__ unsigned char lists[4][4 * kMaxPart];
   const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (wave >= waves) return;
   const long long r = wave / j.parts2;
-  const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, V = j.a.V;
+  const int part = (int)(wave - r * j.parts2), lane = threadIdx.x & 63, V = j.a.V, first = part * j.part;
   float top = -INFINITY;
 #pragma unroll
   for (int k = 0; k < 8; ++k)  // at most 512 chunks
     if (64 * k < j.chunks) top = fmaxf(top, j.chunk_max[r * j.chunks + min(64 * k + lane, j.chunks - 1)]);
   typedef float f2 __attribute__((ext_vector_type(2)));
-  const int pair = part * kPart * 2 + lane, pairs = j.spans * 2;  // this lane's two quarters
+  const int pair = first * 2 + lane, pairs = j.spans * 2;  // this lane's two quarters
   const f2 m = ((const f2*)j.quarter_max)[r * pairs + min(pair, pairs - 1)];
   const float* z = row_logits(j.a, r);
   if (!z) return;
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(256, 5) void verify_sum_kernel(Job j, long long wav
   if (part == 0 && lane == 0) j.top[r] = top;
   if (!finite_top(top)) return;
   const float thr = threshold(top, j.low);
-  const bool h0 = pair < pairs && m[0] >= thr, h1 = pair < pairs && m[1] >= thr;
+  const bool mine = lane < 2 * j.part && pair < pairs, h0 = mine && m[0] >= thr, h1 = mine && m[1] >= thr;
   const unsigned long long b0 = __ballot(h0), b1 = __ballot(h1), below = (1ull << lane) - 1;
   const int n = __popcll(b0) + __popcll(b1), at = __popcll(b0 & below) + __popcll(b1 & below);
   unsigned char* list = lists[threadIdx.x >> 6];
@@ -305,11 +312,11 @@ __global__ __launch_bounds__(256, 5) void verify_sum_kernel(Job j, long long wav
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the wave's lanes read what its lanes wrote
   __builtin_amdgcn_wave_barrier();
   // sixteen quarters at a time, each by 16 lanes, the next ones on their way
-  const bool whole = (part + 1) * kPart * kSpan <= V;
+  const bool whole = (first + j.part) * kSpan <= V;
   auto take = [&](int i0, f4 (&v)[kGroup]) {
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) {
-      const int i = i0 + 4 * k + lane / 16, id = part * kPart * kSpan + list[min(i, n - 1)] * kQuarter + (lane & 15) * 4;
+      const int i = i0 + 4 * k + lane / 16, id = first * kSpan + list[min(i, n - 1)] * kQuarter + (lane & 15) * 4;
       if (i >= n) {
         v[k] = f4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
       } else if (whole) {
@@ -325,9 +332,19 @@ __global__ __launch_bounds__(256, 5) void verify_sum_kernel(Job j, long long wav
   if (n > 0) take(0, v);
   for (int i0 = 0; i0 < n; i0 += 4 * kGroup) {
     if (i0 + 4 * kGroup < n) take(i0 + 4 * kGroup, next);
-    // a kept logit per lane and turn: few lanes have more than one or two
-    for (unsigned b = kept_bits(v, thr, kGroup); b; b &= b - 1)
-      sum += exp2_f64(((double)pick(v, __builtin_ctz(b)) - (double)top) * j.per_z);
+    const unsigned bits = kept_bits(v, thr, kGroup);
+    if (dense(bits)) {
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double w = exp2_f64(((double)v[k][e] - (double)top) * j.per_z);
+          sum += bits >> (4 * k + e) & 1 ? w : 0.0;
+        }
+    } else {
+      for (unsigned b = bits; b; b &= b - 1)
+        sum += exp2_f64(((double)pick(v, __builtin_ctz(b)) - (double)top) * j.per_z);
+    }
 #pragma unroll
     for (int k = 0; k < kGroup; ++k) v[k] = next[k];
   }
@@ -369,11 +386,11 @@ struct Draw {
 };
 
 // Accepted drafts of a sequence, one draft a thread (K <= 255), then the rest of the
-// drawn row in this part's spans.  64 sequences in 12 parts: 18 us: 7 for two
+// drawn row in this part's spans.  64 sequences in 12 parts: 19 us: 7 for two
 // dependent chains (tokens and sums, accepted row, its maxima, its spans), 7 for 34 MB of reads, 4 for the
 // weights; 3 us more where parts make more than three workgroups per CU.  By quarters it takes 19: fewer
 // bytes, but fewer groups to share, each with more kept ids.
-__global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
+__global__ __launch_bounds__(256, 3) void verify_rest_kernel(Job j) {
   __shared__ int first[4], red[4];
   __shared__ unsigned short list[kMaxSpans];
   __shared__ DrawInfo info;
@@ -386,8 +403,13 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   for (int q = t / 16; q < (a.draft ? 2 * a.K + 1 : a.K + 1); q += 16) {
     const double* part = j.sums + (q <= a.K ? target_row(a, s, q) : draft_row(a, s, q - a.K - 1)) * j.parts2;
     double x = 0.0;
-#pragma unroll 8
-    for (int k = t % 16; k < j.parts2; k += 16) x += part[k];
+    for (int k0 = t % 16; k0 < j.parts2; k0 += 8 * 16) {  // eight loads at a time, whatever the number of parts
+      double y[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = part[min(k0 + 16 * i, j.parts2 - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x += k0 + 16 * i < j.parts2 ? y[i] : 0.0;
+    }
 #pragma unroll
     for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o, 16);
     if (t % 16 == 0) sums[q] = x;
@@ -438,11 +460,25 @@ __global__ __launch_bounds__(256) void verify_rest_kernel(Job j) {
   for (int g = g0; g * kGroup < n; g += step) {
     if ((g + step) * kGroup < n) load(g + step, vn, qn);
     double2 sum{0.0, 0.0};
-    for (unsigned m = kept_bits(v, d.p.thr, n - g * kGroup); m; m &= m - 1) {
-      const int i = __builtin_ctz(m);
-      const double2 x = d.rest(pick(v, i), pick(q, i), list[g * kGroup + i / 4] * kSpan + (t & 63) * 4 + i % 4);
-      sum.x += x.x;
-      sum.y += x.y;
+    const unsigned bits = kept_bits(v, d.p.thr, n - g * kGroup);
+    if (dense(bits)) {
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const int id = list[min(g * kGroup + k, n - 1)] * kSpan + (t & 63) * 4;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const double2 x = d.rest(v[k][e], q[k][e], id + e);
+          sum.x += bits >> (4 * k + e) & 1 ? x.x : 0.0;
+          sum.y += bits >> (4 * k + e) & 1 ? x.y : 0.0;
+        }
+      }
+    } else {
+      for (unsigned m = bits; m; m &= m - 1) {
+        const int i = __builtin_ctz(m);
+        const double2 x = d.rest(pick(v, i), pick(q, i), list[g * kGroup + i / 4] * kSpan + (t & 63) * 4 + i % 4);
+        sum.x += x.x;
+        sum.y += x.y;
+      }
     }
     sum.x = wave_sum_f64(sum.x);
     sum.y = wave_sum_f64(sum.y);
@@ -644,7 +680,7 @@ __global__ __launch_bounds__(256) void verify_greedy_kernel(Job j) {
 
 struct Sizes {
   long long rows;
-  int spans, chunks, groups, parts2, parts3;
+  int spans, chunks, groups, part, parts2, parts3;
   size_t quarter_max, chunk_max, top, sums, rest, draws, listed, bytes;
 };
 
@@ -657,7 +693,10 @@ Sizes sizes_of(int S, int K, int V) {
   z.spans = (V + kSpan - 1) / kSpan;
   z.groups = (z.spans + kGroup - 1) / kGroup;
   z.chunks = (V + kChunk - 1) / kChunk;
-  z.parts2 = (z.spans + kPart - 1) / kPart;
+  // smaller parts as long as all waves are resident at once: 72 rows with some thousand kept ids, 20.2 -> 14.8 us
+  z.part = kMaxPart;
+  while (z.part > 8 && z.rows * ((z.spans + z.part / 2 - 1) / (z.part / 2)) <= kResident) z.part /= 2;
+  z.parts2 = (z.spans + z.part - 1) / z.part;
   z.parts3 = std::min(kMaxParts, (767 + S) / S);
   z.quarter_max = 0;
   z.chunk_max = up256((size_t)z.rows * z.spans * 16);
@@ -685,6 +724,7 @@ hipError_t verify_drafts(const VerifyArgs& a0, hipStream_t s) {
   j.spans = z.spans;
   j.chunks = z.chunks;
   j.groups = z.groups;
+  j.part = z.part;
   j.parts2 = z.parts2;
   j.parts3 = z.parts3;
   j.quarter_max = (float*)(a0.ws + z.quarter_max);
