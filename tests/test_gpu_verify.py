@@ -104,6 +104,14 @@ def test_logits_beyond_32_bits(rgd):
     assert bool((cnt[:-1] == 0).all()) and bool((out[:-1, 0] == V // 2).all())  # equal logits: half of the ids
 
 
+@pytest.mark.parametrize("S", [12, 60, 100])
+def test_rows_in_parts_of_every_size(rgd, S):
+    """Few rows are summed in small parts, many in larger ones; with min-p and with every id kept."""
+    for T, min_p in ((1.0, 0.05), (3.0, 0.0)):
+        target, draft, tokens, u = _inputs(S, S, 2, 50257, T, min_p=min_p)
+        _compare(rgd, target, draft, tokens, None, T, min_p, u)
+
+
 def test_ragged_counts_and_tokens_outside(rgd):
     target, draft, tokens, u = _inputs(3, 9, 5, 777)
     n = [0, 1, 2, 3, 4, 5, -4, 99, 5]
