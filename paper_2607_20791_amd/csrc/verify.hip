@@ -263,7 +263,7 @@ RGD_DEV unsigned kept_bits(const f4 (&v)[kGroup], float thr, int spans_left) {
 // place of one kept logit per lane and turn, of which few lanes have more than one or two.  72 rows of
 // 152064 ids that are all kept: pass 2 takes 24 us in place of 49, pass 3 20 in place of 27; a bound of 4 is
 // as fast as 6, 9 slower between few and all.
-RGD_DEV bool dense(unsigned bits) { return __any(__popc(bits) > 6); }
+RGD_DEV bool dense(unsigned bits) { return __builtin_expect(__any(__popc(bits) > 6), 0); }
 
 // v[i / 4][i % 4] by selects
 RGD_DEV float pick(const f4 (&v)[kGroup], int i) {
