@@ -381,11 +381,12 @@ def _refuse(msg):
 
 
 def _tensor(device, name, t, dtype, shape):
-    """The address of a contiguous tensor of this type, shape (None: any) and device; anything else is refused."""
+    """The address of a contiguous tensor of this type, shape (None: any) and device (its index); anything else is
+    refused."""
     if t is None:
         _refuse(f"{name} is None")
-    if t.dtype != dtype or t.device != device:
-        _refuse(f"{name} must be a {dtype} tensor on {device}, got {t.dtype} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != device:
+        _refuse(f"{name} must be a {dtype} tensor on GPU {device}, got {t.dtype} on {t.device}")
     if shape is not None and t.shape != shape:
         _refuse(f"{name} must have the shape {tuple(shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
@@ -406,8 +407,9 @@ def _workspace(device, ws, need):
 
 def _rows(device, name, t, dtype, shape):
     """Address and row stride of a tensor [rows][heads][D] whose rows may lie apart (a slice of a fused projection)."""
-    if t.dtype != dtype or t.device != device or t.shape != shape:
-        _refuse(f"{name} must be a {dtype} tensor {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
+        _refuse(f"{name} must be a {dtype} tensor {tuple(shape)} on GPU {device}, got {t.dtype} {tuple(t.shape)} on "
+                f"{t.device}")
     row, head, one = t.stride()
     if (shape[2] > 1 and one != 1) or (shape[1] > 1 and head != shape[2]):
         _refuse(f"{name}: the heads of a row must be contiguous")
@@ -416,12 +418,11 @@ def _rows(device, name, t, dtype, shape):
 
 def _launch(device, fn, *args):
     """fn(*args, stream) on the operands' device and its current stream."""
-    i = device.index
-    if torch.cuda.current_device() == i:
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+    if torch._C._cuda_getDevice() == device:  # (there are tensors on it, so it is initialised)
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(device)))
         return
-    with torch.cuda.device(i):
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+    with torch.cuda.device(device):
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(device)))
 
 
 class PagedCache:
@@ -438,14 +439,14 @@ class PagedCache:
         if pages.dim() != 2:
             _refuse("pages must have two dimensions")
         S, width = pages.shape
-        dev, i32 = pool_k.device, torch.int32
+        dev, i32 = pool_k.get_device(), torch.int32
         self.desc = PagedCacheDesc(L, P, H, ps, D, types[pool_k.dtype], S, width,
                                    _tensor(dev, "pool_k", pool_k, pool_k.dtype, None),
                                    _tensor(dev, "pool_v", pool_v, pool_k.dtype, (L, P, H, D, ps)),
                                    _tensor(dev, "pages", pages, i32, None), _tensor(dev, "lens", lens, i32, (S,)),
                                    _tensor(dev, "refs", refs, i32, (P,)), _tensor(dev, "status", status, i32, (1,)))
         self.ref = C.byref(self.desc)
-        self.device, self.dtype = dev, pool_k.dtype
+        self.device, self.gpu, self.dtype = pool_k.device, dev, pool_k.dtype
         self.pool_k, self.pool_v, self.pages, self.lens, self.refs, self.status = pool_k, pool_v, pages, lens, refs, status
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = L, P, H, ps, D
         self.max_seqs, self.max_pages = S, width
@@ -471,7 +472,7 @@ def paged_workspace_bytes(cache):
 def paged_select(cache, parent, keep, workspace):
     """Sequence s becomes the first keep[s] positions (None or negative: all) of
     sequence parent[s] (None or outside the cache: itself), all at once."""
-    dev, shape = cache.device, (cache.max_seqs,)
+    dev, shape = cache.gpu, (cache.max_seqs,)
     _launch(dev, lib.rgd_paged_select, cache.ref, _optional(dev, "parent", parent, torch.int32, shape),
             _optional(dev, "keep", keep, torch.int32, shape), _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
@@ -479,14 +480,14 @@ def paged_select(cache, parent, keep, workspace):
 def paged_reserve(cache, grow, workspace):
     """Makes room for grow[s] more positions of each sequence and adds them to lens;
     cache.status becomes 1, and nothing else changes, where there is none."""
-    dev = cache.device
+    dev = cache.gpu
     _launch(dev, lib.rgd_paged_reserve, cache.ref, _tensor(dev, "grow", grow, torch.int32, (cache.max_seqs,)),
             _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
 
 def paged_compact(cache, live, workspace):
     """Moves the live pages to [0, live[0])."""
-    dev = cache.device
+    dev = cache.gpu
     _launch(dev, lib.rgd_paged_compact, cache.ref, _tensor(dev, "live", live, torch.int32, (1,)),
             _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
@@ -494,7 +495,7 @@ def paged_compact(cache, live, workspace):
 def paged_append(cache, layer, k, v, n, n_new=None):
     """K and V rows [S * n][Hkv][D] (rows may lie apart) of each sequence's last n_new[s]
     (None: n) positions into the pages of one layer."""
-    dev, S = cache.device, cache.max_seqs
+    dev, S = cache.gpu, cache.max_seqs
     shape = (S * n, cache.n_kv_heads, cache.head_dim)
     pk, ldk = _rows(dev, "k", k, cache.dtype, shape)
     pv, ldv = _rows(dev, "v", v, cache.dtype, shape)
@@ -509,7 +510,7 @@ def paged_attention_workspace_bytes(cache, n, n_heads):
 def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
     """Causal attention of each sequence's last n_new[s] (None: n) positions, q
     [S * n][heads][D] (rows may lie apart), into out [S * n][heads * D] and lse [S * n][heads]."""
-    dev, S, D = cache.device, cache.max_seqs, cache.head_dim
+    dev, S, D = cache.gpu, cache.max_seqs, cache.head_dim
     if q.dim() != 3:
         _refuse("q must have three dimensions")
     heads = q.shape[1]
@@ -535,7 +536,7 @@ def verify_drafts(target, draft, draft_tokens, n_draft, T, min_p, u, workspace, 
     if target.dim() != 3 or not target.is_cuda:
         _refuse("target must be a 3-dimensional tensor on a GPU")
     S, K1, V = target.shape
-    K, dev, f32, i32 = K1 - 1, target.device, torch.float32, torch.int32
+    K, dev, f32, i32 = K1 - 1, target.get_device(), torch.float32, torch.int32
     _launch(dev, lib.rgd_verify_drafts, _tensor(dev, "target", target, f32, None),
             _optional(dev, "draft", draft, f32, (S, K, V)), _tensor(dev, "draft_tokens", draft_tokens, i32, (S, K)),
             _optional(dev, "n_draft", n_draft, i32, (S,)), S, K, V, T, min_p, _tensor(dev, "u", u, f32, (S, K1)),
