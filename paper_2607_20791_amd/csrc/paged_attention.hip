@@ -775,9 +775,10 @@ int tiles_for(const PagedView& c, int vectors) {
   return vectors <= 16 ? 1 : vectors <= 32 || (c.esz == 4 && c.D == 128) ? 2 : 4;
 }
 
-int runs_for(const PagedView& c, int n, int Hq) {
-  const int nt = tiles_for(c, n * (Hq / c.Hkv)), cols = 16 * nt;
-  const double items = (double)c.S * c.Hkv * ((n * (Hq / c.Hkv) + cols - 1) / cols);
+// Runs of a call whose sequences have up to `vectors` query vectors per KV head.
+int runs_for(const PagedView& c, int vectors) {
+  const int nt = tiles_for(c, vectors), cols = 16 * nt;
+  const double items = (double)c.S * c.Hkv * ((vectors + cols - 1) / cols);
   const double steps = items * std::max(1.0, std::ceil((double)c.width * c.ps / kStep));
   const double most = two_per_cu(nt, c.esz * c.D) ? kMaxRuns : kMaxRuns / 2;
   return (int)std::min(most, std::ceil((steps + item_cost(nt) * items) / kMinSteps));
@@ -785,7 +786,7 @@ int runs_for(const PagedView& c, int n, int Hq) {
 
 template <typename T, int D, int NT>
 hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
-  const int runs = runs_for(a.c, a.n, a.Hq);
+  const int runs = runs_for(a.c, a.n * a.G);
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
   // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
@@ -828,9 +829,16 @@ bool paged_attention_fits(const PagedView& c, int n, int Hq) {
   return units < 274877906944.0;  // 2^38: a run's share of it is counted in ints
 }
 
+// Enough for every call of up to n tokens: fewer query vectors take fewer tiles, whose runs may be twice as many
+// (two workgroups per CU in place of one), so the most that one to tiles_for of them need.
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
-  const int nt = tiles_for(c, n * (Hq / c.Hkv)), runs = runs_for(c, n, Hq);
-  return cut_floats(runs) + (size_t)2 * runs * 16 * nt * (c.D + 2);
+  const int vectors = n * (Hq / c.Hkv);
+  size_t most = 0;
+  for (const int upto : {16, 32, vectors}) {
+    const int v = std::min(upto, vectors), runs = runs_for(c, v);
+    most = std::max(most, cut_floats(runs) + (size_t)2 * runs * 16 * tiles_for(c, v) * (c.D + 2));
+  }
+  return most;
 }
 
 hipError_t paged_attention(const PagedAttnArgs& a0, hipStream_t s) {

@@ -592,3 +592,19 @@ def test_another_stream_and_a_captured_turn(rgd):
         assert all(t.equal(a, b) for a, b in zip(snapshot(c, args), want))
         noise = noise @ noise.T / 1000
         t.cuda.synchronize()
+
+
+@pytest.mark.parametrize("bf16,d", [(True, 32), (False, 128)])
+def test_one_workspace_for_every_number_of_tokens(rgd, bf16, d):
+    """The workspace for up to n tokens at the most runs there are: smaller counts write nothing behind it."""
+    t = torch()
+    x = _filled(rgd, [40000, 39000], hk=1, d=d, layers=1, bf16=bf16, seed=2)
+    need = x.rgd.paged_attention_workspace_bytes(x.c, 8, 8)
+    room = t.full((need + 65536,), 90, dtype=t.uint8, device="cuda")
+    for n in (1, 2, 4, 8):
+        q = t.randn(2 * n, 8, d, device="cuda").to(_dt(bf16))
+        out = [t.zeros(2 * n, 8 * d, dtype=_dt(bf16), device="cuda") for _ in range(2)]
+        rgd.paged_attention(x.c, 0, q, n, None, room[:need], out[0])
+        rgd.paged_attention(x.c, 0, q, n, None, t.empty_like(room), out[1])
+        assert bool((room[need:] == 90).all()), n
+        assert t.equal(out[0], out[1]) and bool(t.isfinite(out[0]).all())

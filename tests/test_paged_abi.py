@@ -104,3 +104,15 @@ def test_verify_arguments(rgd):
                dict(S=0), dict(K=0), dict(V=1), dict(T=-1.0), dict(T=nan), dict(T=float("inf")), dict(min_p=1.5),
                dict(min_p=-0.1), dict(min_p=nan), dict(ws=C.c_void_p(0x10001))):
         assert call(**kw) == INVALID and lib.rgd_last_error(), kw
+
+
+@pytest.mark.parametrize("kw", [dict(dtype=0, head_dim=128, max_pages=100000), dict(head_dim=128, max_pages=100000),
+                                dict(head_dim=32, max_pages=100000), dict(dtype=0), dict(max_seqs=1, max_pages=1),
+                                dict(max_seqs=70, max_pages=40, n_kv_heads=1)])
+@pytest.mark.parametrize("group", [1, 3, 8, 20])
+def test_an_attention_workspace_serves_fewer_tokens_too(rgd, kw, group):
+    """The bytes for up to n tokens are enough for every smaller count."""
+    kw = {"max_seqs": 64, **kw}
+    d, heads = _desc(rgd, **kw), group * kw.get("n_kv_heads", GOOD["n_kv_heads"])
+    need = [rgd.lib.rgd_paged_attention_workspace_bytes(d, n, heads) for n in range(1, 130)]
+    assert need[0] > 0 and need == sorted(need)
