@@ -182,7 +182,12 @@ struct Dist {
   float top, thr;
   double per_z, scale;  // p = 2^((z - top) per_z) * scale
   RGD_DEV double weight(float x) const { return x >= thr ? exp2_f64(((double)x - (double)top) * per_z) : 0.0; }
-  RGD_DEV double p(float x) const { return weight(x) * scale; }
+  // Rounded by itself: a product that went into the difference p - q unrounded would leave noise where p = q, and
+  // the draw would come from that.
+  RGD_DEV double p(float x) const {
+#pragma clang fp contract(off)
+    return weight(x) * scale;
+  }
 };
 
 RGD_DEV bool finite_top(float t) { return t > -INFINITY && t < INFINITY; }
@@ -377,6 +382,7 @@ struct Draw {
   }
   // (the rest of p over q, p) of one id
   RGD_DEV double2 rest(float zp, float zq, int id) const {
+#pragma clang fp contract(off)
     const double x = p.p(zp);
     double r = x;
     if (minus_q) r = fmax(x - q.p(zq), 0.0);

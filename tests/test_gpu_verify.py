@@ -224,3 +224,19 @@ def test_binding_refuses_wrong_tensors(rgd):
         with pytest.raises(rgd.RGDError) as e:
             rgd.verify_drafts(*(good[:i] + [bad] + good[i + 1:]))
         assert e.value.code == 1
+
+
+@pytest.mark.parametrize("V", [1000, 20011])
+@pytest.mark.parametrize("T,min_p", [(1.0, 0.1), (1.0, 0.0), (0.7, 0.05), (2.5, 0.0)])
+def test_a_refused_draft_of_equal_rows_draws_from_the_target(rgd, V, T, min_p):
+    """p - q is 0 everywhere: a draft outside the vocabulary, or one that the truncation leaves out, is refused and
+    the token comes from p itself."""
+    S, K = 8, 2
+    target, _, tokens, u = _inputs(V, S, K, V, T)
+    draft = target[:, :K].copy()
+    tokens[:, 1] = [-1, V, -1, 2**31 - 1, -2**31, V + 5, -1, V]
+    if min_p > 0:
+        tokens[::2, 0] = target[::2, 0].argmin(-1)  # p = q = 0
+        tokens[1::2, 0] = target[1::2, 0].argmax(-1)
+    counts = _compare(rgd, target, draft, tokens, None, T, min_p, u)
+    assert counts.tolist() == ([0, 1] * 4 if min_p > 0 else [1] * 8)
