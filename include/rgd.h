@@ -442,6 +442,14 @@ int32_t rgd_paged_select(const rgd_paged_cache* cache, const int32_t* parent, co
  * and nothing else is changed.  Asynchronous. */
 int32_t rgd_paged_reserve(const rgd_paged_cache* cache, const int32_t* grow, void* workspace, rgd_stream stream);
 
+/* As rgd_paged_reserve; granted (dev int32 [S]; grow itself, or apart from it) receives how many positions
+ * each sequence got: max(grow[s], 0), or 0 for every sequence where there was no room.  What is queued
+ * behind a reserve without the host's look at status takes its counts from here: an append and an
+ * attention with n_new = granted, and a roll-back to lens - granted + kept, leave a cache that had no room
+ * as it is, where grow would have them write over and drop older positions. */
+int32_t rgd_paged_reserve_granted(const rgd_paged_cache* cache, const int32_t* grow, int32_t* granted,
+                                  void* workspace, rgd_stream stream);
+
 /* Moves pages so that the pages held by any sequence (refs > 0) are the pages
  * [0, n): those at or above n go, in order, to the free ones below it, in every
  * layer; tables and refs follow.  live dev int32 [1] receives n.  Asynchronous. */
@@ -449,9 +457,9 @@ int32_t rgd_paged_compact(const rgd_paged_cache* cache, int32_t* live, void* wor
 
 /* Writes the K and V of each sequence's last n_new[s] positions (dev int32 [S],
  * counts outside [0, n] as the nearest inside; NULL: n of each) of one layer:
- * token i of sequence s goes to position lens[s] - n_new[s] + i (rgd_paged_reserve
- * has made it, so that no other sequence holds its page; positions before 0 are
- * left out).  k, v dev in the cache's type:
+ * token i of sequence s goes to position lens[s] - n_new[s] + i, whatever is there (a reserve
+ * that had room has made it, so that no other sequence holds its page; behind one that may have had none,
+ * n_new is what rgd_paged_reserve_granted granted; positions before 0 are left out).  k, v dev in the cache's type:
  * row s * n + i at k + (s * n + i) * ldk elements, [Hkv][D] each; keys already
  * rotated.  ldk, ldv >= Hkv * D; k, v and their row strides 16-byte aligned.
  * Asynchronous. */

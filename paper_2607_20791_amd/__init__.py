@@ -26,7 +26,7 @@ EXPORTS = (
     "rgd_prefill_kv", "rgd_prefill_kv_scored", "rgd_probe", "rgd_probe_fixed", "rgd_probe_soft", "rgd_probe_adaptive", "rgd_gate", "rgd_sample_continuations", "rgd_sample_continuations_pless", "rgd_check_status",
     "rgd_kernel_attention", "rgd_kernel_lm_head", "rgd_sampler_workspace_bytes",
     "rgd_kernel_argmax", "rgd_kernel_sample", "rgd_kernel_sample_noalloc", "rgd_kernel_sample_pless", "rgd_kernel_probe_step", "rgd_timing_enable", "rgd_timing_read",
-    "rgd_paged_workspace_bytes", "rgd_paged_select", "rgd_paged_reserve", "rgd_paged_compact", "rgd_paged_append",
+    "rgd_paged_workspace_bytes", "rgd_paged_select", "rgd_paged_reserve", "rgd_paged_reserve_granted", "rgd_paged_compact", "rgd_paged_append",
     "rgd_paged_attention_workspace_bytes", "rgd_paged_attention", "rgd_verify_workspace_bytes", "rgd_verify_drafts",
 )
 
@@ -114,6 +114,7 @@ _CACHE = C.POINTER(PagedCacheDesc)
 _sig("rgd_paged_workspace_bytes", U64, _CACHE)
 _sig("rgd_paged_select", I32, _CACHE, VP, VP, VP, VP)
 _sig("rgd_paged_reserve", I32, _CACHE, VP, VP, VP)
+_sig("rgd_paged_reserve_granted", I32, _CACHE, VP, VP, VP, VP)
 _sig("rgd_paged_compact", I32, _CACHE, VP, VP, VP)
 _sig("rgd_paged_append", I32, _CACHE, I32, VP, VP, I64, I64, I32, VP, VP)
 _sig("rgd_paged_attention_workspace_bytes", U64, _CACHE, I32, I32)
@@ -477,12 +478,17 @@ def paged_select(cache, parent, keep, workspace):
             _optional(dev, "keep", keep, torch.int32, shape), _workspace(dev, workspace, paged_workspace_bytes(cache)))
 
 
-def paged_reserve(cache, grow, workspace):
+def paged_reserve(cache, grow, workspace, granted=None):
     """Makes room for grow[s] more positions of each sequence and adds them to lens;
-    cache.status becomes 1, and nothing else changes, where there is none."""
-    dev = cache.gpu
-    _launch(dev, lib.rgd_paged_reserve, cache.ref, _tensor(dev, "grow", grow, torch.int32, (cache.max_seqs,)),
-            _workspace(dev, workspace, paged_workspace_bytes(cache)))
+    cache.status becomes 1, and nothing else changes, where there is none.  granted (int32 [S], may be grow)
+    receives what each sequence got, 0 then: the n_new of what is queued without a look at the status."""
+    dev, shape = cache.gpu, (cache.max_seqs,)
+    pg = _tensor(dev, "grow", grow, torch.int32, shape)
+    ws = _workspace(dev, workspace, paged_workspace_bytes(cache))
+    if granted is None:
+        _launch(dev, lib.rgd_paged_reserve, cache.ref, pg, ws)
+    else:
+        _launch(dev, lib.rgd_paged_reserve_granted, cache.ref, pg, _tensor(dev, "granted", granted, torch.int32, shape), ws)
 
 
 def paged_compact(cache, live, workspace):

@@ -20,7 +20,7 @@ RGD_DEV bool page_ok(const PagedView& c, int p) { return (unsigned)p < (unsigned
 
 size_t paged_workspace_ints(const PagedView& c);
 hipError_t paged_select(const PagedView& c, const int* parent, const int* keep, int* ws, hipStream_t s);
-hipError_t paged_reserve(const PagedView& c, const int* grow, int* ws, hipStream_t s);
+hipError_t paged_reserve(const PagedView& c, const int* grow, int* granted, int* ws, hipStream_t s);
 hipError_t paged_compact(const PagedView& c, int* live, int* ws, hipStream_t s);
 // k, v: row s * n + i at k + (s * n + i) * ldk elements
 hipError_t paged_append(const PagedView& c, int layer, const void* k, const void* v, long long ldk, long long ldv,

@@ -148,8 +148,8 @@ RGD_DEV int list_pages(unsigned hits, int p0, int found, int most, int* list, Lo
 // (from, to) pairs [2 S], the sequences' first list entries [S], the page each
 // gives up for a copy of its own or -1 [S], the list.  288 sequences and 4000 pages:
 // 8.6 us, a chain of dependent reads (length, last page, its count, list entries) and seven
-// barriers.
-__global__ __launch_bounds__(kPlan) void reserve_plan_kernel(PagedView c, const int* grow, int* ws) {
+// barriers.  granted (or null) may be grow: a sequence's entries are read and written by one thread.
+__global__ __launch_bounds__(kPlan) void reserve_plan_kernel(PagedView c, const int* grow, int* granted, int* ws) {
   __shared__ int red[kPlan / 64];
   __shared__ LookCounts counts;
   __shared__ int over, ncopy;
@@ -205,10 +205,13 @@ __global__ __launch_bounds__(kPlan) void reserve_plan_kernel(PagedView c, const 
       ws[0] = 0;
       *c.status = 1;
     }
+    if (granted)
+      for (int s = threadIdx.x; s < c.S; s += kPlan) granted[s] = 0;
     return;
   }
   for (int s = threadIdx.x; s < c.S; s += kPlan) {  // the threads that wrote first and given
     const int g = max(grow[s], 0);
+    if (granted) granted[s] = g;
     if (!g) continue;
     const int len = paged_len(c, s), used = pages_of(c, len), after = pages_of(c, len + g), from = given[s];
     int* row = c.pages + (size_t)s * c.width;
@@ -400,8 +403,8 @@ hipError_t paged_select(const PagedView& c, const int* parent, const int* keep, 
   return hipGetLastError();
 }
 
-hipError_t paged_reserve(const PagedView& c, const int* grow, int* ws, hipStream_t s) {
-  hipLaunchKernelGGL(reserve_plan_kernel, dim3(1), dim3(kPlan), 0, s, c, grow, ws);
+hipError_t paged_reserve(const PagedView& c, const int* grow, int* granted, int* ws, hipStream_t s) {
+  hipLaunchKernelGGL(reserve_plan_kernel, dim3(1), dim3(kPlan), 0, s, c, grow, granted, ws);
   const int blocks = (int)std::min<long long>(4096, 2LL * c.L * c.S);
   hipLaunchKernelGGL(copy_pairs_kernel, dim3(blocks), dim3(256), 0, s, c, ws, c.page_elems() * c.esz);
   return hipGetLastError();

@@ -63,6 +63,18 @@ const char* heads_ok(const PagedView& v, int32_t n, int32_t n_heads) {
   return nullptr;
 }
 
+int32_t reserve(const rgd_paged_cache* cache, const int32_t* grow, int32_t* granted, void* workspace,
+                rgd_stream stream) {
+  clear_error();
+  PagedView v;
+  if (const char* why = view_of(cache, v)) return bad(why);
+  if (!grow || !workspace) return bad("null argument");
+  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+  const int64_t counts = (int64_t)v.S * 4;
+  if (granted != grow && overlap(granted, counts, grow, counts)) return bad("granted overlaps a part of grow");
+  return launched(paged_reserve(v, grow, granted, (int*)workspace, (hipStream_t)stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -88,12 +100,14 @@ int32_t rgd_paged_select(const rgd_paged_cache* cache, const int32_t* parent, co
 }
 
 int32_t rgd_paged_reserve(const rgd_paged_cache* cache, const int32_t* grow, void* workspace, rgd_stream stream) {
+  return reserve(cache, grow, nullptr, workspace, stream);
+}
+
+int32_t rgd_paged_reserve_granted(const rgd_paged_cache* cache, const int32_t* grow, int32_t* granted,
+                                  void* workspace, rgd_stream stream) {
   clear_error();
-  PagedView v;
-  if (const char* why = view_of(cache, v)) return bad(why);
-  if (!grow || !workspace) return bad("null argument");
-  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
-  return launched(paged_reserve(v, grow, (int*)workspace, (hipStream_t)stream));
+  if (!granted) return bad("null argument");
+  return reserve(cache, grow, granted, workspace, stream);
 }
 
 int32_t rgd_paged_compact(const rgd_paged_cache* cache, int32_t* live, void* workspace, rgd_stream stream) {

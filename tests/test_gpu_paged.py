@@ -608,3 +608,71 @@ def test_one_workspace_for_every_number_of_tokens(rgd, bf16, d):
         rgd.paged_attention(x.c, 0, q, n, None, t.empty_like(room), out[1])
         assert bool((room[need:] == 90).all()), n
         assert t.equal(out[0], out[1]) and bool(t.isfinite(out[0]).all())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_a_turn_without_room_leaves_the_cache_as_it_is(rgd, in_place):
+    """A captured turn (reserve, append, attention, roll-back by what was kept) whose pages run out, with a page
+    that two sequences share; later the same turn goes on from where it stood."""
+    t = torch()
+    x = Case(rgd, 4, 4, 9, layers=1, hk=2, d=64, seed=31)
+    assert x.reserve([20, 0, 0, 30])
+    x.append(0, 30, [20, 0, 0, 30])
+    x.select([0, 0, 2, 3], None)      # 1 shares both pages of 0; four pages held, five free
+    x.check()
+    c = x.c
+    want, grow, kept = _i32([3, 2, 40, 1]), _i32([0, 0, 0, 0]), _i32([2, 2, 39, 1])
+    granted = grow if in_place else _i32([7, 7, 7, 7])
+    kv, q = t.randn(2, 4 * 40, 2, 64, device="cuda").bfloat16(), t.randn(4 * 40, 4, 64, device="cuda").bfloat16()
+    out = t.full((160, 256), 7.0, dtype=t.bfloat16, device="cuda")
+    aws = t.empty(rgd.paged_attention_workspace_bytes(c, 40, 4), dtype=t.uint8, device="cuda")
+
+    def turn():
+        grow.copy_(want)
+        rgd.paged_reserve(c, grow, x.ws, granted)
+        rgd.paged_append(c, 0, kv[0], kv[1], 40, granted)
+        rgd.paged_attention(c, 0, q, 40, granted, aws, out)
+        rgd.paged_select(c, None, c.lens - granted + kept, x.ws)
+
+    t.cuda.synchronize()
+    graph = t.cuda.CUDAGraph()
+    with t.cuda.graph(graph):
+        turn()
+    want.copy_(_i32([3, 2, 48, 1]))   # 0 and 1 copy their shared page, 2 wants three pages, 3 has room: five
+    graph.replay()
+    assert granted.tolist() == [3, 2, 48, 1] and int(c.status[0]) == 0
+    assert c.lens.tolist() == [22, 22, 39, 31] and int((c.refs == 0).sum()) == 1
+    rgd.paged_select(c, _i32([0, 0, 2, 3]), None, x.ws)   # 0 and 1 share again; two pages are free
+    x2 = [y.clone() for y in (c.pages, c.lens, c.refs, c.pool_k, c.pool_v)]
+    out.fill_(7.0)
+    want.copy_(_i32([3, 2, 20, 1]))   # two copies and a page: three
+    for _ in range(3):
+        graph.replay()
+        assert granted.tolist() == [0] * 4 and int(c.status[0]) == 1
+        for a, b in zip((c.pages, c.lens, c.refs, c.pool_k, c.pool_v), x2):
+            assert t.equal(a, b)
+        assert bool((out == 7).all())
+        t.cuda.synchronize()
+    rgd.paged_select(c, _i32([0, 0, 2, 3]), _i32([-1, -1, 0, -1]), x.ws)  # 2 is freed
+    c.status.zero_()
+    want.copy_(_i32([0, 1, -5, 0]))
+    pools = c.pool_k.clone(), c.pool_v.clone()
+    n0 = int(c.lens[0])
+    graph.replay()
+    assert granted.tolist() == [0, 1, 0, 0] and int(c.status[0]) == 0
+    assert c.lens.tolist() == [n0, n0 + 1, 0, int(x2[1][3])]
+    held = int(c.pages[0, n0 // 16])
+    assert t.equal(c.pool_k[0, held], pools[0][0, held]) and int(c.pages[1, n0 // 16]) != held
+
+
+def test_granted_is_what_reserve_gave(rgd):
+    """1100 sequences, more than a turn of the planning workgroup."""
+    x = Case(rgd, 1100, 2, 1500, layers=1, hk=1, d=32, seed=3)
+    granted = _i32(np.full(1100, 9))
+    for grow in (x.r.integers(-3, 17, 1100), np.full(1100, 16), x.r.integers(-2, 2, 1100)):
+        ok = op.reserve(x.pages, x.lens, x.refs, 16, grow)[-1]
+        rgd.paged_reserve(x.c, _i32(grow), x.ws, granted)
+        x.pages, x.lens, x.refs = op.reserve(x.pages, x.lens, x.refs, 16, grow)[:3]
+        assert granted.tolist() == (np.maximum(grow, 0) * ok).tolist()
+        for a, b in ((x.c.pages, x.pages), (x.c.lens, x.lens), (x.c.refs, x.refs)):
+            assert np.array_equal(a.cpu().numpy(), b)

@@ -116,3 +116,14 @@ def test_an_attention_workspace_serves_fewer_tokens_too(rgd, kw, group):
     d, heads = _desc(rgd, **kw), group * kw.get("n_kv_heads", GOOD["n_kv_heads"])
     need = [rgd.lib.rgd_paged_attention_workspace_bytes(d, n, heads) for n in range(1, 130)]
     assert need[0] > 0 and need == sorted(need)
+
+
+def test_reserve_with_granted_arguments(rgd):
+    lib, d = rgd.lib, _desc(rgd)
+
+    def call(cache=d, grow=P, granted=OUT, ws=WS):
+        return lib.rgd_paged_reserve_granted(cache, grow, granted, ws, None)
+
+    for kw in (dict(cache=None), dict(cache=_desc(rgd, n_pages=0)), dict(grow=None), dict(granted=None), dict(ws=None),
+               dict(ws=C.c_void_p(0x10010)), dict(granted=C.c_void_p(0x40000 + 8)), dict(granted=C.c_void_p(0x40000 - 8))):
+        assert call(**kw) == INVALID and lib.rgd_last_error(), kw
