@@ -56,6 +56,7 @@ constexpr int kWaves = 4;      // per workgroup
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLazy = 8.f;       // the running maximum moves when a score passes it by this (log2 units)
+constexpr float kLift = 256.f;     // 2^kLazy: weights are held divided by it, so none is above 1 and no sum above that of |V|
 constexpr float kNoRef = -3.0e38f; // the maximum before any visible score: finite, so a masked one gives 0, never NaN
 
 RGD_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
@@ -408,7 +409,7 @@ struct Piece {
   }
 
   // Weights of tile t's scores (log2 units) against its running maximum, which moves
-  // with them; hi + lo: the weights in two bf16.
+  // with them, over kLift; hi + lo: the weights in two bf16.
   RGD_DEV void weights(int t, const float (&x)[E], float (&p)[E], u32x4& hi, u32x4& lo) {
     float top = x[0];
 #pragma unroll
@@ -425,7 +426,7 @@ struct Piece {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      p[j] = exp2_raw(x[j] - m[t]);
+      p[j] = exp2_raw(x[j] - m[t]) * (1.f / kLift);
       sum += p[j];
     }
     l[t] += sum;
@@ -590,7 +591,7 @@ struct Piece {
   }
 };
 
-RGD_DEV float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2; }
+RGD_DEV float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l * kLift)) * kLn2; }
 
 template <typename T>
 RGD_DEV void store_row4(T* p, f32x4 v) {

@@ -676,3 +676,38 @@ def test_granted_is_what_reserve_gave(rgd):
         assert granted.tolist() == (np.maximum(grow, 0) * ok).tolist()
         for a, b in ((x.c.pages, x.pages), (x.c.lens, x.lens), (x.c.refs, x.refs)):
             assert np.array_equal(a.cpu().numpy(), b)
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n,hk,G,d", [(1, 2, 4, 64), (5, 1, 4, 128), (16, 1, 4, 32)])
+def test_values_up_to_the_largest_sum(rgd, bf16, n, hk, G, d):
+    """Values whose sum over the positions is just below 2^128, the larger weights behind the smaller ones, by less
+    than what moves a running maximum: the output is finite wherever the formula is."""
+    t = torch()
+    big, lens = 1.6e38, [300, 3000]
+    x = _filled(rgd, lens, hk=hk, d=d, layers=1, bf16=bf16, seed=n)
+    # a third sequence over one page makes the runs so long that a wave takes several rounds
+    pages = np.full((3, 40000), int(x.pages[0, 0]))
+    pages[:2, :x.width] = x.pages
+    c = rgd.PagedCache(x.c.pool_k, x.c.pool_v, _i32(pages), _i32(lens + [640000]), x.c.refs, x.c.status)
+    x.c.pool_k.nan_to_num_(nan=0.0).zero_()
+    x.c.pool_v.nan_to_num_(nan=0.0).zero_()
+    q = t.zeros(3 * n, hk * G, d, device="cuda", dtype=_dt(bf16))
+    q[:, :, 0] = 1.0
+    for s, first in enumerate((0, 1500)):  # a wave takes every 64th or 128th position of an item's
+        for pos, score in ((first, 0.0), (first + 128, 5.375)):  # 5.375 / ln 2 = 7.75
+            p = int(x.pages[s, pos // 16])
+            x.c.pool_k[0, p, :, pos % 16, 0] = score * d ** 0.5
+            x.c.pool_v[0, p, :, :, pos % 16] = big
+    out, lse = t.zeros(3 * n, hk * G * d, dtype=_dt(bf16), device="cuda"), t.zeros(3 * n, hk * G, device="cuda")
+    ws = t.empty(rgd.paged_attention_workspace_bytes(c, n, hk * G), dtype=t.uint8, device="cuda")
+    rgd.paged_attention(c, 0, q, n, None, ws, out, lse)
+    pk, pv, o = _np(x.c.pool_k)[0], _np(x.c.pool_v)[0], _np(out).reshape(3, n, hk * G, d)
+    for s, N in enumerate(lens):
+        k, v, there = op.gather(pk, pv, x.pages[s], N, 16)
+        assert v.sum(0).max() < 2.0**128
+        ro, rl = op.attention(_np(q)[s * n:(s + 1) * n], k, v, there, N - n)
+        # as in _attention; nothing cancels, so relative to the output itself; one score of one product, at most 5.4
+        rel = 2.0**(-8 if bf16 else -24) + 4 * 5.4 * 2.0**-24 + 2.0**-15 * bf16 + 2.0**-21 + 2 * (N + 64) * 2.0**-24
+        assert np.isfinite(ro).all() and (np.abs(o[s] - ro) <= rel * ro).all(), (s, np.abs(o[s] / ro - 1).max(), rel)
+        assert (np.abs(_np(lse)[s * n:(s + 1) * n] - rl) <= 5.4 * 2.0**-22 + (N + 64) * 2.0**-24 + 2.0**-20 + 2.0**-22 * rl).all()
