@@ -408,12 +408,14 @@ struct Piece {
     return r;
   }
 
-  // Weights of tile t's scores (log2 units) against its running maximum, which moves
-  // with them, over kLift; hi + lo: the weights in two bf16.
-  RGD_DEV void weights(int t, const float (&x)[E], float (&p)[E], u32x4& hi, u32x4& lo) {
+  // Weights of tile t's products (times scale: scores in log2 units) against its running maximum, which moves
+  // with them, over kLift; hi + lo: the weights in two bf16.  A score's distance from the maximum is rounded once, at
+  // its own size: a score that is rounded first takes errors of the score's size into the weight.
+  RGD_DEV void weights(int t, const float (&x)[E], float scale, float (&p)[E], u32x4& hi, u32x4& lo) {
     float top = x[0];
 #pragma unroll
     for (int j = 1; j < E; ++j) top = fmaxf(top, x[j]);
+    top *= scale;
     if (__any(top > m[t] + kLazy)) {
       top = fmaxf(top, __shfl_xor(top, 16, 64));
       top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -426,7 +428,7 @@ struct Piece {
     float sum = 0.f;
 #pragma unroll
     for (int j = 0; j < E; ++j) {
-      p[j] = exp2_raw(x[j] - m[t]) * (1.f / kLift);
+      p[j] = exp2_raw(fmaf(x[j], scale, -m[t])) * (1.f / kLift);
       sum += p[j];
     }
     l[t] += sum;
@@ -509,9 +511,9 @@ struct Piece {
         for (int t = 0; t < NT; ++t) {
           float x[E], p[E];
 #pragma unroll
-          for (int j = 0; j < E; ++j) x[j] = s4[t][j / 4][j % 4] * scale;
+          for (int j = 0; j < E; ++j) x[j] = s4[t][j / 4][j % 4];
           u32x4 hi, lo;
-          weights(t, x, p, hi, lo);
+          weights(t, x, scale, p, hi, lo);
 #pragma unroll
           for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p, hi, lo, o[t][d]);
         }
@@ -550,8 +552,8 @@ struct Piece {
         const int seen = there ? lim[t] - pos : 0;
         float x[E];
 #pragma unroll
-        for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] * scale : -INFINITY;
-        weights(t, x, p[t], hi[t], lo[t]);
+        for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] : -INFINITY;
+        weights(t, x, scale, p[t], hi[t], lo[t]);
       }
       if (__any(odd)) {
         // 0 times a value that is not finite is not 0, so these leave the product: a

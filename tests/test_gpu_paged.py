@@ -711,3 +711,30 @@ def test_values_up_to_the_largest_sum(rgd, bf16, n, hk, G, d):
         rel = 2.0**(-8 if bf16 else -24) + 4 * 5.4 * 2.0**-24 + 2.0**-15 * bf16 + 2.0**-21 + 2 * (N + 64) * 2.0**-24
         assert np.isfinite(ro).all() and (np.abs(o[s] - ro) <= rel * ro).all(), (s, np.abs(o[s] / ro - 1).max(), rel)
         assert (np.abs(_np(lse)[s * n:(s + 1) * n] - rl) <= 5.4 * 2.0**-22 + (N + 64) * 2.0**-24 + 2.0**-20 + 2.0**-22 * rl).all()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n,hk,G,d", [(1, 2, 4, 64), (5, 1, 4, 128), (16, 1, 4, 32)])
+def test_weights_follow_the_differences_of_large_scores(rgd, bf16, n, hk, G, d):
+    """Products of 2^20 and a little, all exact: the weights keep the little."""
+    t = torch()
+    x = _filled(rgd, [300, 70, 900], hk=hk, d=d, layers=1, bf16=bf16, stale=0.0, seed=n)
+    g = t.Generator(device="cuda").manual_seed(n)
+    x.c.pool_k.zero_()
+    x.c.pool_k[..., 0] = 2.0**20
+    x.c.pool_k[..., 1] = t.randint(0, 16, x.c.pool_k.shape[:-1], generator=g, device="cuda").to(_dt(bf16))
+    q = t.zeros(3 * n, hk * G, d, device="cuda", dtype=_dt(bf16))
+    q[:, :, :2] = 1.0
+    out = t.zeros(3 * n, hk * G * d, dtype=_dt(bf16), device="cuda")
+    ws = t.empty(rgd.paged_attention_workspace_bytes(x.c, n, hk * G), dtype=t.uint8, device="cuda")
+    rgd.paged_attention(x.c, 0, q, n, None, ws, out)
+    pk, pv, o = _np(x.c.pool_k)[0], _np(x.c.pool_v)[0], _np(out).reshape(3, n, hk * G, d)
+    for s, N in enumerate(x.lens):
+        k, v, there = op.gather(pk, pv, x.pages[s], N, 16)
+        ro, _ = op.attention(_np(q)[s * n:(s + 1) * n], k, v, there, N - n)
+        # a difference is at most 15 / sqrt(d) log2(e) < 4 of the scale, which is rounded twice, and the reference, up
+        # to 8 off, so at most 12 rounded to 2^-21; the exponential 2^-22, weights as two bf16 2^-16; numerator and
+        # denominator, each with the roundings of its sums
+        weight = 12 * 2.0**-23 + 2.0**-21 + 2.0**-22 + 2.0**-16 * bf16
+        tol = 2.0**(-8 if bf16 else -24) * np.abs(ro) + (2 * weight + 2 * (N + 64) * 2.0**-24) * np.abs(v).max()
+        assert (np.abs(o[s] - ro) <= tol).all(), (s, np.abs(o[s] - ro).max(), tol.max())
