@@ -420,7 +420,8 @@ typedef struct rgd_paged_cache {
 
 /* Bytes of caller-provided device workspace (256-byte aligned) that
  * rgd_paged_select, rgd_paged_reserve and rgd_paged_compact need; 0 for a
- * description they refuse.  Calls that share a workspace must not overlap. */
+ * description they refuse.  Calls that share a workspace must not overlap; a
+ * workspace and what a call writes are apart from its inputs and from the cache. */
 uint64_t rgd_paged_workspace_bytes(const rgd_paged_cache* cache);
 
 /* Forks, reorders, rolls back and frees, all sequences at once: sequence s
@@ -477,9 +478,10 @@ uint64_t rgd_paged_attention_workspace_bytes(const rgd_paged_cache* cache, int32
  * cache's type, row s * n + i at q + (s * n + i) * ldq elements, [n_heads][D]
  * (16-byte aligned rows); query head h reads KV head h / (n_heads / Hkv), scores
  * are scaled by 1/sqrt(D).  out dev [S * n][n_heads * D] in the cache's type
- * (16-byte aligned, not overlapping q), lse dev fp32 [S * n][n_heads] or NULL:
+ * (16-byte aligned), lse dev fp32 [S * n][n_heads] or NULL:
  * the log of the sum of exponentiated scores, for joining with attention over
- * other positions.  A token that sees nothing gets 0 and -inf; rows at or behind
+ * other positions.  out, lse and the workspace overlap neither each other, nor q, n_new or the cache.  A token that
+ * sees nothing gets 0 and -inf; rows at or behind
  * n_new[s] are left as they were.  Slots behind a length and free pages may hold
  * anything.  A value of V that is not finite makes its dimension of the tokens
  * that see it inf or NaN and no other; sums are fp32, so a sequence's sum of |V|
@@ -511,7 +513,7 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * token is drawn from max(p_i - q_i, 0), after n_draft acceptances from p_i, by
  * u[K]: the smallest id whose running weight exceeds u[K] times the total.
  * out dev int32 [S][K+1]: the accepted drafts, the drawn token, then -1;
- * n_accepted dev int32 [S]; neither may overlap the other or an input.  A draft
+ * n_accepted dev int32 [S]; these and the workspace overlap neither each other nor an input.  A draft
  * outside [0, V) is refused.  NaN logits
  * count as -inf.  A target row whose maximum is not finite has no distribution:
  * its draft is refused and -1 stands for the drawn token; such a draft row has

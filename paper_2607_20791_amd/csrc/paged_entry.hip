@@ -1,5 +1,8 @@
 // C ABI of the paged sequences and of the draft verification: argument checks
 // (before any HIP call), then the launches.
+#include <algorithm>
+#include <initializer_list>
+
 #include "entry.hpp"
 #include "paged.hpp"
 #include "rgd.h"
@@ -42,8 +45,45 @@ const char* view_of(const rgd_paged_cache* c, PagedView& v) {
 
 int32_t bad(const char* why) { return set_error(RGD_E_INVALID_ARG, why); }
 
-bool overlap(const void* a, int64_t na, const void* b, int64_t nb) {
-  return a && b && (uintptr_t)a < (uintptr_t)b + (uintptr_t)nb && (uintptr_t)b < (uintptr_t)a + (uintptr_t)na;
+// A buffer of n bytes (0 at null).
+struct Range {
+  uintptr_t at;
+  uint64_t n;
+  Range(const void* p, uint64_t n) : at((uintptr_t)p), n(p ? n : 0) {}
+};
+// n rows of `row` bytes, `ld` bytes apart; past what an address can be: up to there
+Range rows_of(const void* p, int64_t n, int64_t ld, int64_t row) {
+  return Range(p, (uint64_t)std::min((__int128)(n - 1) * ld + row, (__int128)1 << 62));
+}
+bool overlap(const Range& a, const Range& b) { return a.n && b.n && a.at < b.at + b.n && b.at < a.at + a.n; }
+
+// Whether some output shares memory with an input or another output.
+bool outputs_shared(std::initializer_list<Range> outputs, std::initializer_list<Range> inputs) {
+  for (const Range* o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Range& in : inputs)
+      if (overlap(*o, in)) return true;
+    for (const Range* p = outputs.begin(); p != o; ++p)
+      if (overlap(*o, *p)) return true;
+  }
+  return false;
+}
+
+// Whether some of these buffers shares memory with the cache's.
+bool shares_cache(const PagedView& c, std::initializer_list<Range> buffers) {
+  const int64_t page = (int64_t)(c.page_elems() * c.esz), n = (int64_t)c.L * c.n_pages;
+  return outputs_shared(buffers, {rows_of(c.pool_k, n, page, page), rows_of(c.pool_v, n, page, page),
+                                  Range(c.pages, (uint64_t)c.S * c.width * 4), Range(c.lens, (uint64_t)c.S * 4),
+                                  Range(c.refs, (uint64_t)c.n_pages * 4), Range(c.status, 4)});
+}
+
+// Why the workspace of a page operator is refused, or what it writes besides (or null): each apart from the
+// other, from the cache and from the call's counts.
+const char* work_ok(const PagedView& c, void* ws, const Range& written, const Range& in0, const Range& in1) {
+  if (!aligned(ws, 256)) return "workspace must be 256-byte aligned";
+  const Range work(ws, paged_workspace_ints(c) * sizeof(int));
+  if (outputs_shared({work, written}, {in0, in1}) || shares_cache(c, {work, written}))
+    return "the workspace or an output overlaps an input, the cache or each other";
+  return nullptr;
 }
 
 int32_t launched(hipError_t e) { return e == hipSuccess ? (int32_t)RGD_OK : set_error(RGD_E_HIP, hipGetErrorString(e)); }
@@ -69,9 +109,8 @@ int32_t reserve(const rgd_paged_cache* cache, const int32_t* grow, int32_t* gran
   PagedView v;
   if (const char* why = view_of(cache, v)) return bad(why);
   if (!grow || !workspace) return bad("null argument");
-  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
-  const int64_t counts = (int64_t)v.S * 4;
-  if (granted != grow && overlap(granted, counts, grow, counts)) return bad("granted overlaps a part of grow");
+  const Range in(grow, (uint64_t)v.S * 4), out(granted, (uint64_t)v.S * 4), none(nullptr, 0);
+  if (const char* why = work_ok(v, workspace, out, granted == grow ? none : in, none)) return bad(why);
   return launched(paged_reserve(v, grow, granted, (int*)workspace, (hipStream_t)stream));
 }
 
@@ -95,7 +134,8 @@ int32_t rgd_paged_select(const rgd_paged_cache* cache, const int32_t* parent, co
   PagedView v;
   if (const char* why = view_of(cache, v)) return bad(why);
   if (parent && !workspace) return bad("null workspace");
-  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+  if (const char* why = work_ok(v, workspace, Range(nullptr, 0), Range(parent, (uint64_t)v.S * 4), Range(keep, (uint64_t)v.S * 4)))
+    return bad(why);
   return launched(paged_select(v, parent, keep, (int*)workspace, (hipStream_t)stream));
 }
 
@@ -115,7 +155,7 @@ int32_t rgd_paged_compact(const rgd_paged_cache* cache, int32_t* live, void* wor
   PagedView v;
   if (const char* why = view_of(cache, v)) return bad(why);
   if (!live || !workspace) return bad("null argument");
-  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+  if (const char* why = work_ok(v, workspace, Range(live, 4), Range(nullptr, 0), Range(nullptr, 0))) return bad(why);
   return launched(paged_compact(v, live, (int*)workspace, (hipStream_t)stream));
 }
 
@@ -156,7 +196,12 @@ int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const v
   const int64_t width = (int64_t)n_heads * a.c.D, rows = (int64_t)a.c.S * n;
   if (const char* why = rows_ok(a.c, q, ldq, width)) return bad(why);
   if (!aligned(out, 16) || !aligned(workspace, 256)) return bad("out must be 16-byte, the workspace 256-byte aligned");
-  if (overlap(q, ((rows - 1) * ldq + width) * a.c.esz, out, rows * width * a.c.esz)) return bad("out overlaps q");
+  const int64_t esz = (int64_t)a.c.esz;
+  const Range o(out, rows * width * esz), l(lse, rows * n_heads * 4),
+      w(workspace, paged_attention_workspace_floats(a.c, n, n_heads) * sizeof(float));
+  if (outputs_shared({o, l, w}, {rows_of(q, rows, ldq * esz, width * esz), Range(n_new, (uint64_t)a.c.S * 4)}) ||
+      shares_cache(a.c, {o, l, w}))
+    return bad("out, lse or the workspace overlaps an input, the cache or each other");
   const size_t layer0 = (size_t)layer * a.c.n_pages * a.c.page_elems() * a.c.esz;
   a.pool_k = a.c.pool_k + layer0;
   a.pool_v = a.c.pool_v + layer0;
@@ -186,14 +231,11 @@ int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t
   if (!(T >= 0.f && T < 3e38f)) return bad("T must be >= 0 and finite");
   if (!(min_p >= 0.f && min_p <= 1.f)) return bad("min_p must be in [0,1]");
   if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
-  const int64_t s = S, k = K, kept = s * (k + 1) * 4, counts = s * 4;  // bytes of out, of n_accepted
-  const struct {
-    const void* p;
-    int64_t n;
-  } inputs[] = {{target, kept * V}, {draft, s * k * 4 * V}, {draft_tokens, s * k * 4}, {n_draft, counts}, {u, kept}};
-  for (const auto& in : inputs)
-    if (overlap(out, kept, in.p, in.n) || overlap(n_accepted, counts, in.p, in.n)) return bad("an output overlaps an input");
-  if (overlap(out, kept, n_accepted, counts)) return bad("out overlaps n_accepted");
+  const uint64_t s = S, k = K, kept = s * (k + 1) * 4, counts = s * 4;  // bytes of out, of n_accepted
+  if (outputs_shared({Range(out, kept), Range(n_accepted, counts), Range(workspace, verify_workspace_bytes(S, K, V))},
+                     {Range(target, kept * V), Range(draft, s * k * 4 * V), Range(draft_tokens, s * k * 4),
+                      Range(n_draft, counts), Range(u, kept)}))
+    return bad("an output or the workspace overlaps an input or another output");
   VerifyArgs a{target, draft, draft_tokens, n_draft, S, K, V, T, min_p, u, out, n_accepted, (char*)workspace};
   return launched(verify_drafts(a, (hipStream_t)stream));
 }

@@ -127,3 +127,52 @@ def test_reserve_with_granted_arguments(rgd):
     for kw in (dict(cache=None), dict(cache=_desc(rgd, n_pages=0)), dict(grow=None), dict(granted=None), dict(ws=None),
                dict(ws=C.c_void_p(0x10010)), dict(granted=C.c_void_p(0x40000 + 8)), dict(granted=C.c_void_p(0x40000 - 8))):
         assert call(**kw) == INVALID and lib.rgd_last_error(), kw
+
+
+# buffers of a cache far apart from each other and from WS, P, OUT and W2
+APART = dict(pool_k=0x10000000, pool_v=0x20000000, pages=0x30000000, lens=0x31000000, refs=0x32000000, status=0x33000000)
+
+
+def _at(x):
+    return C.c_void_p(x)
+
+
+def test_attention_refuses_buffers_that_overlap(rgd):
+    lib, d = rgd.lib, _desc(rgd, **APART)
+    counts = _at(0x60000)
+
+    def call(q=P, out=OUT, ws=_at(0x1000000), lse=W2, ldq=256):
+        return lib.rgd_paged_attention(d, 0, q, ldq, 2, counts, 4, ws, out, lse, None)
+
+    need = lib.rgd_paged_attention_workspace_bytes(d, 2, 4)  # q: 6 rows of 512 bytes; lse: 96 bytes
+    cases = [dict(lse=OUT), dict(lse=_at(0x80000 + 3072 - 4)), dict(lse=P), dict(lse=_at(0x40000 + 3072 - 4)), dict(lse=counts),
+             dict(lse=_at(0x60000 - 92)), dict(out=counts), dict(ws=OUT), dict(ws=P), dict(ws=_at(0x80000 - need + 256)),
+             dict(ws=W2), dict(ldq=1 << 39, out=_at(0x40000 + (1 << 40)))]
+    cases += [{k: _at(a)} for k in ("out", "lse", "ws") for a in APART.values()]
+    cases += [dict(out=_at(0x10000000 + 65536 - 16)), dict(lse=_at(0x10000000 - 92)), dict(ws=_at(0x32000000 - 256))]
+    for kw in cases:
+        assert call(**kw) == INVALID and b"overlap" in lib.rgd_last_error(), kw
+
+
+def test_page_operators_refuse_buffers_that_overlap(rgd):
+    lib, d = rgd.lib, _desc(rgd, **APART)
+    for at in APART.values():
+        for rc in (lib.rgd_paged_select(d, P, None, _at(at), None), lib.rgd_paged_reserve(d, P, _at(at), None),
+                   lib.rgd_paged_reserve_granted(d, P, _at(at), WS, None), lib.rgd_paged_compact(d, OUT, _at(at), None),
+                   lib.rgd_paged_compact(d, _at(at), WS, None)):
+            assert rc == INVALID and b"overlap" in lib.rgd_last_error(), hex(at)
+    for rc in (lib.rgd_paged_select(d, P, None, P, None), lib.rgd_paged_select(d, W2, P, P, None),
+               lib.rgd_paged_reserve(d, P, P, None), lib.rgd_paged_reserve(d, _at(0x10000 + 4), WS, None),
+               lib.rgd_paged_reserve_granted(d, P, WS, WS, None), lib.rgd_paged_compact(d, WS, WS, None)):
+        assert rc == INVALID and b"overlap" in lib.rgd_last_error()
+
+
+def test_verify_refuses_a_workspace_that_overlaps(rgd):
+    lib = rgd.lib
+    need = lib.rgd_verify_workspace_bytes(2, 4, 101)
+    a = dict(target=0x1000000, draft=0x2000000, tokens=0x3000000, nd=0x3100000, u=0x3200000, out=0x3300000, count=0x3400000)
+    for at in list(a.values()) + [a["u"] - need + 256, a["target"] + 4096 - 256]:
+        p = {k: _at(v) for k, v in a.items()}
+        rc = lib.rgd_verify_drafts(p["target"], p["draft"], p["tokens"], p["nd"], 2, 4, 101, 1.0, 0.1, p["u"], _at(at // 256 * 256),
+                                   p["out"], p["count"], None)
+        assert rc == INVALID and b"overlap" in lib.rgd_last_error(), hex(at)
