@@ -470,12 +470,15 @@ def paged_workspace_bytes(cache):
     return cache.need("pages", lib.rgd_paged_workspace_bytes)
 
 
-def paged_select(cache, parent, keep, workspace):
+def paged_select(cache, parent, keep, workspace=None):
     """Sequence s becomes the first keep[s] positions (None or negative: all) of
-    sequence parent[s] (None or outside the cache: itself), all at once."""
+    sequence parent[s] (None or outside the cache: itself), all at once.  Without parent it needs no workspace."""
     dev, shape = cache.gpu, (cache.max_seqs,)
+    ws = None
+    if parent is not None or workspace is not None:
+        ws = _workspace(dev, workspace, paged_workspace_bytes(cache))
     _launch(dev, lib.rgd_paged_select, cache.ref, _optional(dev, "parent", parent, torch.int32, shape),
-            _optional(dev, "keep", keep, torch.int32, shape), _workspace(dev, workspace, paged_workspace_bytes(cache)))
+            _optional(dev, "keep", keep, torch.int32, shape), ws)
 
 
 def paged_reserve(cache, grow, workspace, granted=None):

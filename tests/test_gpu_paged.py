@@ -738,3 +738,17 @@ def test_weights_follow_the_differences_of_large_scores(rgd, bf16, n, hk, G, d):
         weight = 12 * 2.0**-23 + 2.0**-21 + 2.0**-22 + 2.0**-16 * bf16
         tol = 2.0**(-8 if bf16 else -24) * np.abs(ro) + (2 * weight + 2 * (N + 64) * 2.0**-24) * np.abs(v).max()
         assert (np.abs(o[s] - ro) <= tol).all(), (s, np.abs(o[s] - ro).max(), tol.max())
+
+
+def test_roll_back_needs_no_workspace(rgd):
+    x = Case(rgd, 3, 3, 9, seed=4)
+    assert x.reserve([20, 40, 5])
+    for keep in ([17, -1, 0], [16, 3, 9], None):
+        rgd.paged_select(x.c, None, None if keep is None else _i32(keep))
+        x.pages, x.lens, x.refs = op.select(x.pages, x.lens, x.refs, 16, None, keep)
+        x.check()
+    for bad in (None, x.ws[:8]):
+        with pytest.raises(rgd.RGDError) as e:
+            rgd.paged_select(x.c, _i32([0, 0, 0]), None, bad)
+        assert e.value.code == 1
+    x.check()
