@@ -752,3 +752,12 @@ def test_roll_back_needs_no_workspace(rgd):
             rgd.paged_select(x.c, _i32([0, 0, 0]), None, bad)
         assert e.value.code == 1
     x.check()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("n,hk,G,d,ps", [(64, 1, 4, 64, 16), (65, 2, 1, 128, 32), (150, 1, 2, 128, 64), (500, 1, 2, 32, 16),
+                                         (1024, 1, 1, 64, 16)])
+def test_attention_of_prompt_pieces(rgd, bf16, n, hk, G, d, ps):
+    """Many query tiles: whole prompts, pieces behind a prefix, pieces longer than what is there."""
+    x = _filled(rgd, [n + 70, n, 0, n // 2 + 1, 40], hk=hk, d=d, ps=ps, layers=1, bf16=bf16, seed=n)
+    _attention(x, 0, hk * G, n, [n, n, n, n - 1, 33])

@@ -145,7 +145,7 @@ def test_attention_refuses_buffers_that_overlap(rgd):
         return lib.rgd_paged_attention(d, 0, q, ldq, 2, counts, 4, ws, out, lse, None)
 
     need = lib.rgd_paged_attention_workspace_bytes(d, 2, 4)  # q: 6 rows of 512 bytes; lse: 96 bytes
-    cases = [dict(lse=OUT), dict(lse=_at(0x80000 + 3072 - 4)), dict(lse=P), dict(lse=_at(0x40000 + 3072 - 4)), dict(lse=counts),
+    cases = [dict(lse=OUT), dict(lse=_at(0x80000 + 6 * 512 - 4)), dict(lse=P), dict(lse=_at(0x40000 + 6 * 512 - 4)), dict(lse=counts),
              dict(lse=_at(0x60000 - 92)), dict(out=counts), dict(ws=OUT), dict(ws=P), dict(ws=_at(0x80000 - need + 256)),
              dict(ws=W2), dict(ldq=1 << 39, out=_at(0x40000 + (1 << 40)))]
     cases += [{k: _at(a)} for k in ("out", "lse", "ws") for a in APART.values()]
