@@ -438,7 +438,9 @@ int32_t rgd_paged_select(const rgd_paged_cache* cache, const int32_t* parent, co
  * behind each sequence and adds them to lens.  New pages are the lowest free
  * ones, in the order of the sequences.  A sequence that grows and whose last
  * page is partly filled and held by another table entry too gets a copy of that
- * page (every layer) in its place, so the new positions are its own.  If the
+ * page (every layer) in its place, so the new positions are its own.  That goes by
+ * refs before the call: where all N holders of a page grow, each gets a copy, which takes
+ * N free pages, and the original is free afterwards.  If the
  * pool has too few free pages or a table too few entries, status[0] is set to 1
  * and nothing else is changed.  Asynchronous. */
 int32_t rgd_paged_reserve(const rgd_paged_cache* cache, const int32_t* grow, void* workspace, rgd_stream stream);
@@ -486,8 +488,9 @@ uint64_t rgd_paged_attention_workspace_bytes(const rgd_paged_cache* cache, int32
  * anything.  A value of V that is not finite makes its dimension of the tokens
  * that see it inf or NaN and no other; sums are fp32, so a sequence's sum of |V|
  * in a dimension must stay below 2^128.  1 <= n <= 1024, S * n <= 2^24, n_heads <= 1024.  Meant for few tokens: every 64
- * query vectors (tokens x query heads per KV head) of a sequence read its K and
- * V once.  Asynchronous. */
+ * query vectors (tokens x query heads per KV head; 32 in fp32 with D = 128) of a sequence read its K and
+ * V once.  The same call gives the same bits; how a sequence's sums are associated also depends on the other
+ * sequences' lengths and on max_pages, so its last bits may differ in another batch.  Asynchronous. */
 int32_t rgd_paged_attention(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,
                             const int32_t* n_new, int32_t n_heads, void* workspace, void* out, float* lse,
                             rgd_stream stream);
@@ -512,6 +515,8 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * draft x_i is accepted while u[i] q_i(x_i) < p_i(x_i).  At the first refusal the next
  * token is drawn from max(p_i - q_i, 0), after n_draft acceptances from p_i, by
  * u[K]: the smallest id whose running weight exceeds u[K] times the total.
+ * Kept ids are those with z_i - max z >= T ln(min_p) in fp64; the sampler goes by the weight in fp32, so an id
+ * whose weight is within 1e-5 of itself of min_p may be kept by one of the two only.
  * out dev int32 [S][K+1]: the accepted drafts, the drawn token, then -1;
  * n_accepted dev int32 [S]; these and the workspace overlap neither each other nor an input.  A draft
  * outside [0, V) is refused.  NaN logits
@@ -520,7 +525,7 @@ uint64_t rgd_verify_workspace_bytes(int32_t S, int32_t K, int32_t V);
  * q = 0.  1 <= S <= 65536, 1 <= K <= 255, 2 <= V <= 1048576, S (2 K + 1)
  * ceil(V / 8192) <= 2^23, T >= 0, min_p in [0, 1].  Sums are taken in fp64, so
  * that the draw is the exact one unless u[K] meets the border of two tokens by
- * 1e-11 of the total.  Asynchronous. */
+ * 1e-11 of p's sum (not of the rest's, which is small where q is near p).  Asynchronous. */
 int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t* draft_tokens,
                           const int32_t* n_draft, int32_t S, int32_t K, int32_t V, float T, float min_p,
                           const float* u, void* workspace, int32_t* out, int32_t* n_accepted, rgd_stream stream);

@@ -266,8 +266,8 @@ RGD_DEV unsigned kept_bits(const f4 (&v)[kGroup], float thr, int spans_left) {
 
 // Whether some lane has so many kept logits of its 16 that all of them are weighed one after the other, in
 // place of one kept logit per lane and turn, of which few lanes have more than one or two.  72 rows of
-// 152064 ids that are all kept: pass 2 takes 24 us in place of 49, pass 3 20 in place of 27; a bound of 4 is
-// as fast as 6, 9 slower between few and all.
+// 152064 ids that are all kept: pass 2 takes 20 us in place of 39, pass 3 20 in place of 27 (of pass 2 the weights
+// alone take 16 and the loads alone 14); a bound of 4 is as fast as 6, 9 slower between few and all.
 RGD_DEV bool dense(unsigned bits) { return __builtin_expect(__any(__popc(bits) > 6), 0); }
 
 // v[i / 4][i % 4] by selects
