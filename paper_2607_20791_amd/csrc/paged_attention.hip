@@ -369,23 +369,28 @@ struct Piece {
       v[d] = PAST ? __builtin_nontemporal_load((const u32x4*)(at + d * step)) : *(const u32x4*)(at + d * step);
   }
 
+  // fp32: four sums of D / 4 products each, as every product is rounded where it is added (heads of 128: 2.8e-7 of the
+  // outputs with one sum, 2.0e-7 with two, 1.6e-7 with four, at the same times).
   RGD_DEV void scores(f32x4 (&s)[NT][NB]) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
       for (int e = 0; e < NB; ++e) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (BF) {
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < KL; ++c) {
-          if constexpr (BF) {
-            x = mfma_bf16(k[e][c], q_at(t, c), x);
-          } else {
+          for (int c = 0; c < KL; ++c) x = mfma_bf16(k[e][c], q_at(t, c), x);
+          s[t][e] = x;
+        } else {
+          f32x4 x[4] = {};
+#pragma unroll
+          for (int c = 0; c < KL; ++c) {
             const u32x4 qc = q_at(t, c);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x = mfma_f32(__uint_as_float(k[e][c][j]), __uint_as_float(qc[j]), x);
+            for (int j = 0; j < 4; ++j) x[j] = mfma_f32(__uint_as_float(k[e][c][j]), __uint_as_float(qc[j]), x[j]);
           }
+          s[t][e] = (x[0] + x[1]) + (x[2] + x[3]);
         }
-        s[t][e] = x;
       }
   }
 

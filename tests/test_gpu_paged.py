@@ -761,3 +761,29 @@ def test_attention_of_prompt_pieces(rgd, bf16, n, hk, G, d, ps):
     """Many query tiles: whole prompts, pieces behind a prefix, pieces longer than what is there."""
     x = _filled(rgd, [n + 70, n, 0, n // 2 + 1, 40], hk=hk, d=d, ps=ps, layers=1, bf16=bf16, seed=n)
     _attention(x, 0, hk * G, n, [n, n, n, n - 1, 33])
+
+
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("n,small", [(1, 1.0), (1, 0.3), (5, 1.0), (16, -0.9)])
+def test_small_products_beside_a_large_one(rgd, d, n, small):
+    """fp32: two positions, of which one has d - 1 small products beside the 2^24 that both have.  A product passes at most
+    d / 4 + 2 additions, each off by half a step of what is there."""
+    t = torch()
+    from paper_2607_20791_amd import session
+    c = session.alloc_paged(1, 1, 1, d, 1, 1, page_size=32, bf16=False)
+    c.pages.zero_()
+    c.lens.fill_(n + 1)  # every token sees positions 0 and 1; the others weigh nothing
+    c.pool_k[0, 0, 0, :, 0] = -2.0**24
+    c.pool_k[0, 0, 0, :2, 0] = 2.0**24
+    c.pool_k[0, 0, 0, 0, 1:] = small
+    c.pool_v[0, 0, 0, :, 0] = 1.0
+    ws = t.empty(rgd.paged_attention_workspace_bytes(c, n, 4), dtype=t.uint8, device="cuda")
+    out = t.zeros(n, 4 * d, device="cuda")
+    rgd.paged_attention(c, 0, t.ones(n, 4, d, device="cuda"), n, None, ws, out)
+    w = _np(out)
+    x = float(np.float32(small))
+    assert ((w > 0) & (w < 1)).all()
+    got = np.log(w / (1 - w)) * np.sqrt(d)  # the difference of the two products
+    # and four roundings around the weight, which count by its distance from 0 and 1
+    bound = (d / 4 + 2) * 2.0**-24 * (2.0**24 + abs(x) * d) + 4 * 2.0**-24 / np.minimum(w, 1 - w) * np.sqrt(d)
+    assert (np.abs(got - x * (d - 1)) <= bound).all(), (got.min(), got.max(), x * (d - 1), bound.max())
