@@ -395,6 +395,12 @@ def _tensor(device, name, t, dtype, shape):
     return t.data_ptr()
 
 
+def _int32(*numbers):
+    """Refuses what ctypes would pass on as its lowest 32 bits."""
+    if max(numbers) > 0x7FFFFFFF or min(numbers) < -0x80000000:
+        _refuse(f"{max(numbers, key=abs)} is out of range")
+
+
 def _optional(device, name, t, dtype, shape):
     return None if t is None else _tensor(device, name, t, dtype, shape)
 
@@ -441,6 +447,7 @@ class PagedCache:
             _refuse("pages must have two dimensions")
         S, width = pages.shape
         dev, i32 = pool_k.get_device(), torch.int32
+        _int32(*pool_k.shape, *pages.shape)
         self.desc = PagedCacheDesc(L, P, H, ps, D, types[pool_k.dtype], S, width,
                                    _tensor(dev, "pool_k", pool_k, pool_k.dtype, None),
                                    _tensor(dev, "pool_v", pool_v, pool_k.dtype, (L, P, H, D, ps)),
@@ -456,6 +463,7 @@ class PagedCache:
     def need(self, what, fn, *args):
         n = self._needs.get(what)
         if n is None:
+            _int32(0, *args)
             n = self._needs[what] = _bytes(fn(self.ref, *args))
         return n
 
@@ -504,6 +512,7 @@ def paged_compact(cache, live, workspace):
 def paged_append(cache, layer, k, v, n, n_new=None):
     """K and V rows [S * n][Hkv][D] (rows may lie apart) of each sequence's last n_new[s]
     (None: n) positions into the pages of one layer."""
+    _int32(layer, n)
     dev, S = cache.gpu, cache.max_seqs
     shape = (S * n, cache.n_kv_heads, cache.head_dim)
     pk, ldk = _rows(dev, "k", k, cache.dtype, shape)
@@ -519,6 +528,7 @@ def paged_attention_workspace_bytes(cache, n, n_heads):
 def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
     """Causal attention of each sequence's last n_new[s] (None: n) positions, q
     [S * n][heads][D] (rows may lie apart), into out [S * n][heads * D] and lse [S * n][heads]."""
+    _int32(layer, n)
     dev, S, D = cache.gpu, cache.max_seqs, cache.head_dim
     if q.dim() != 3:
         _refuse("q must have three dimensions")
@@ -533,6 +543,7 @@ def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
 
 # ------------------------------------------------------- verification of drafts --
 def verify_workspace_bytes(S, K, V):
+    _int32(S, K, V)
     n = lib.rgd_verify_workspace_bytes(S, K, V)
     if n == 0:
         _refuse("S, K or V out of range")

@@ -787,3 +787,22 @@ def test_small_products_beside_a_large_one(rgd, d, n, small):
     # and four roundings around the weight, which count by its distance from 0 and 1
     bound = (d / 4 + 2) * 2.0**-24 * (2.0**24 + abs(x) * d) + 4 * 2.0**-24 / np.minimum(w, 1 - w) * np.sqrt(d)
     assert (np.abs(got - x * (d - 1)) <= bound).all(), (got.min(), got.max(), x * (d - 1), bound.max())
+
+
+def test_numbers_beyond_31_bits_are_refused(rgd):
+    """They would reach the library as their lowest 32 bits."""
+    t = torch()
+    x = Case(rgd, 2, 2, 4)
+    k = t.zeros(2, 2, 64, dtype=t.bfloat16, device="cuda")
+    out = t.zeros(2, 128, dtype=t.bfloat16, device="cuda")
+    ws = t.empty(rgd.paged_attention_workspace_bytes(x.c, 1, 2), dtype=t.uint8, device="cuda")
+    before = x.c.pool_k.clone()
+    for layer in (1 << 32, -(1 << 32), 1 << 31):
+        for call in (lambda: rgd.paged_append(x.c, layer, k, k, 1), lambda: rgd.paged_attention(x.c, layer, k, 1, None, ws, out)):
+            with pytest.raises(rgd.RGDError) as e:
+                call()
+            assert e.value.code == 1
+    for n, heads in (((1 << 32) + 1, 2), (1, (1 << 32) + 2)):
+        with pytest.raises(rgd.RGDError):
+            rgd.paged_attention_workspace_bytes(x.c, n, heads)
+    assert t.equal(before, x.c.pool_k)

@@ -176,3 +176,10 @@ def test_verify_refuses_a_workspace_that_overlaps(rgd):
         rc = lib.rgd_verify_drafts(p["target"], p["draft"], p["tokens"], p["nd"], 2, 4, 101, 1.0, 0.1, p["u"], _at(at // 256 * 256),
                                    p["out"], p["count"], None)
         assert rc == INVALID and b"overlap" in lib.rgd_last_error(), hex(at)
+
+
+def test_verify_sizes_beyond_31_bits_are_refused(rgd):
+    for args in (((1 << 32) + 2, 4, 101), (2, (1 << 32) + 4, 101), (2, 4, (1 << 32) + 101)):
+        with pytest.raises(rgd.RGDError):
+            rgd.verify_workspace_bytes(*args)
+    assert rgd.verify_workspace_bytes(2, 4, 101) > 0
