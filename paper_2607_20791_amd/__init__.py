@@ -414,6 +414,8 @@ def _workspace(device, ws, need):
 
 def _rows(device, name, t, dtype, shape):
     """Address and row stride of a tensor [rows][heads][D] whose rows may lie apart (a slice of a fused projection)."""
+    if t is None:
+        _refuse(f"{name} is None")
     if t.dtype is not dtype or t.get_device() != device or t.shape != shape:
         _refuse(f"{name} must be a {dtype} tensor {tuple(shape)} on GPU {device}, got {t.dtype} {tuple(t.shape)} on "
                 f"{t.device}")
@@ -530,8 +532,8 @@ def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
     [S * n][heads][D] (rows may lie apart), into out [S * n][heads * D] and lse [S * n][heads]."""
     _int32(layer, n)
     dev, S, D = cache.gpu, cache.max_seqs, cache.head_dim
-    if q.dim() != 3:
-        _refuse("q must have three dimensions")
+    if q is None or q.dim() != 3:
+        _refuse("q must be a tensor of three dimensions")
     heads = q.shape[1]
     pq, ldq = _rows(dev, "q", q, cache.dtype, (S * n, heads, D))
     _launch(dev, lib.rgd_paged_attention, cache.ref, layer, pq, ldq, n,
@@ -553,7 +555,7 @@ def verify_workspace_bytes(S, K, V):
 def verify_drafts(target, draft, draft_tokens, n_draft, T, min_p, u, workspace, out, n_accepted):
     """Accepts a prefix of each sequence's drafts and draws the token after it, from target
     logits [S][K+1][V], the drafts' logits [S][K][V] (None: certain drafts) and uniforms u [S][K+1]."""
-    if target.dim() != 3 or not target.is_cuda:
+    if target is None or target.dim() != 3 or not target.is_cuda:
         _refuse("target must be a 3-dimensional tensor on a GPU")
     S, K1, V = target.shape
     K, dev, f32, i32 = K1 - 1, target.get_device(), torch.float32, torch.int32

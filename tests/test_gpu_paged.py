@@ -806,3 +806,19 @@ def test_numbers_beyond_31_bits_are_refused(rgd):
         with pytest.raises(rgd.RGDError):
             rgd.paged_attention_workspace_bytes(x.c, n, heads)
     assert t.equal(before, x.c.pool_k)
+
+
+def test_missing_tensors_are_refused(rgd):
+    t = torch()
+    x = Case(rgd, 2, 2, 4)
+    k = t.zeros(2, 2, 64, dtype=t.bfloat16, device="cuda")
+    out = t.zeros(2, 128, dtype=t.bfloat16, device="cuda")
+    ws = t.empty(rgd.paged_attention_workspace_bytes(x.c, 1, 2), dtype=t.uint8, device="cuda")
+    for call in (lambda: rgd.paged_append(x.c, 0, None, k, 1), lambda: rgd.paged_append(x.c, 0, k, None, 1),
+                 lambda: rgd.paged_attention(x.c, 0, None, 1, None, ws, out), lambda: rgd.paged_attention(x.c, 0, k, 1, None, ws, None),
+                 lambda: rgd.paged_attention(x.c, 0, k, 1, None, None, out), lambda: rgd.paged_reserve(x.c, None, x.ws),
+                 lambda: rgd.paged_compact(x.c, None, x.ws),
+                 lambda: rgd.verify_drafts(None, None, None, None, 1.0, 0.1, None, None, None, None)):
+        with pytest.raises(rgd.RGDError) as e:
+            call()
+        assert e.value.code == 1
