@@ -530,6 +530,112 @@ int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t
                           const int32_t* n_draft, int32_t S, int32_t K, int32_t V, float T, float min_p,
                           const float* u, void* workspace, int32_t* out, int32_t* n_accepted, rgd_stream stream);
 
+/* ---- rotary positions and head norms of a paged cache's new tokens ---- */
+
+/* How the frequencies theta^(-2j/dim) of a rotation are changed for contexts longer than the trained one
+ * (`context` positions) by `factor`. */
+enum rgd_rotary_kind {
+  RGD_ROTARY_LINEAR = 1,       /* each over factor */
+  RGD_ROTARY_BASE = 2,         /* theta times factor^(dim / (dim - 2)): the first kept, the last over factor */
+  RGD_ROTARY_BY_ROTATIONS = 3, /* by the turns r a pair makes over context: over factor for r <= low, kept for
+                                  r >= high, in between linear in r */
+  RGD_ROTARY_BY_INDEX = 4      /* linear in the pair's index between the pair (rounded down) that makes `high` turns
+                                  and the one (rounded up) that makes `low`; cosine and sine are scaled by
+                                  1 + ln(factor) / 10 */
+};
+
+typedef struct rgd_rotary_scaling {
+  int32_t kind;   /* rgd_rotary_kind */
+  double factor;  /* >= 1 */
+  double context; /* > 0 (the last two kinds) */
+  double low;     /* 0 < low < high (the last two kinds) */
+  double high;
+} rgd_rotary_scaling;
+
+/* The frequencies of a rotation of `dim` dimensions (even, 2 to 128): freq host fp64 [dim / 2] receives the radians per
+ * position of each pair, scale host [1] the factor of cosine and sine.  scaling NULL: theta^(-2j/dim) and 1.
+ * theta > 1; RGD_ROTARY_BASE needs dim > 2.  No HIP call. */
+int32_t rgd_rotary_frequencies(int32_t dim, double theta, const rgd_rotary_scaling* scaling, double* freq,
+                               float* scale);
+
+/* A rotation of the first dim dimensions of a head: pair j, of dimensions (j, j + dim / 2) or, interleaved,
+ * (2 j, 2 j + 1), turns by position * freq[j] radians: (a, b) -> scale (a cos - b sin, b cos + a sin).  Read during the
+ * call. */
+typedef struct rgd_rotary {
+  int32_t dim;         /* even, 0 (no rotation) to head_dim */
+  int32_t interleaved;
+  float scale;
+  const double* freq;  /* host [dim / 2], finite; of any source */
+} rgd_rotary;
+
+/* rgd_paged_append for rows as a fused projection leaves them, together with what attention needs of q: the heads of
+ * q and k are normed, x / sqrt(mean(x^2) + eps) times a gain for each dimension (q_norm, k_norm dev fp32 [D]; NULL:
+ * that one is left as it is), rotated by their token's position, and k and v are written to the pages of one layer as
+ * rgd_paged_append does, q to q_out.  Token i of sequence s has the position lens[s] - n_new[s] + i, or
+ * positions[s * n + i] (dev int32 [S * n], any value) where positions is given; the slot in the cache stays
+ * the former.  q, k, v dev in the cache's type, row s * n + i at q + (s * n + i) * ldq elements [n_heads][D],
+ * k and v [Hkv][D]; q_out alike, with ldo: q itself with its stride, or apart from every input.  Values are rounded
+ * once, to the cache's type; norms, angles' remainders (taken in fp64) and rotations are fp32.  Rows at or behind n_new[s]
+ * are left as they were; a token before position 0 or on a page outside the pool gets its q and no K and V.
+ * rotary NULL: no rotation.  ld* at least a row's elements; rows 16-byte aligned; eps >= 0 and finite; 1 <= n,
+ * S * n <= 2^24, n_heads a multiple of Hkv, at most 1024.  The inputs are apart from the cache.  Asynchronous. */
+int32_t rgd_paged_append_rotated(const rgd_paged_cache* cache, int32_t layer, const void* q, const void* k,
+                                 const void* v, int64_t ldq, int64_t ldk, int64_t ldv, int32_t n,
+                                 const int32_t* n_new, int32_t n_heads, const int32_t* positions,
+                                 const rgd_rotary* rotary, const float* q_norm, const float* k_norm, float eps,
+                                 void* q_out, int64_t ldo, rgd_stream stream);
+
+/* ---- attention of sequences that share leading pages ---- */
+
+/* Bytes of the plan (256-byte aligned device memory) that rgd_paged_share writes for up to n new tokens per sequence
+ * and n_heads query heads; 0 for arguments it refuses. */
+uint64_t rgd_paged_share_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads);
+
+/* Finds what the sequences of each group share, once for all layers of a turn: sequences with equal labels in
+ * group (dev int32 [S]; one outside [0, S): a sequence by itself; NULL: all are one group) that have new tokens (n_new
+ * dev int32 [S], counts outside [0, n] as the nearest inside; NULL: n of each) share the leading table entries that
+ * are the same in all of them, as far as whole pages in front of each one's new tokens go.  Labels are hints: a group
+ * that shares nothing costs nothing but the search, and one label for all finds what all share.  plan receives
+ * this for rgd_paged_attention_shared; it holds for these lens, tables and counts.  shared (dev int32 [S], or NULL)
+ * receives the positions that each sequence shares, 0 where it is its group's only one with new tokens.  Asynchronous. */
+int32_t rgd_paged_share(const rgd_paged_cache* cache, int32_t n, const int32_t* n_new, int32_t n_heads,
+                        const int32_t* group, void* plan, int32_t* shared, rgd_stream stream);
+
+/* Bytes of device workspace (256-byte aligned) for rgd_paged_attention_shared with these n and n_heads; 0 for
+ * arguments it refuses. */
+uint64_t rgd_paged_attention_shared_workspace_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads);
+
+/* rgd_paged_attention with the counts of a plan, whose shared positions are read once for all sequences of their group: the
+ * same outputs but for the rounding of their sums, the same rows, limits and handling of bad pages and of values that
+ * are not finite.  plan: written by rgd_paged_share for the same n, n_heads and sizes of the cache; where it was
+ * not, every row of out and lse is left as it was.  Asynchronous. */
+int32_t rgd_paged_attention_shared(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,
+                                   int32_t n_heads, const void* plan, void* workspace, void* out, float* lse,
+                                   rgd_stream stream);
+
+/* ---- sampling with limits for each row ---- */
+
+/* Bytes of device workspace (256-byte aligned) for rgd_sample_truncated; 0 for sizes it refuses. */
+uint64_t rgd_sample_truncated_workspace_bytes(int32_t R, int32_t V);
+
+/* Draws one id from each row of logits z (dev fp32, row r at z + r * ldz, V ids) under limits of its own.  The ids are
+ * ordered by logit, equal ones lower id first, and weighted w = exp((z - max z) / T).  Kept are, in this order,
+ *   the first top_k ids (dev int32 [R]; below 1, or NULL: no limit),
+ *   of these, every id with less than top_p of their weight in front of it (dev fp32 [R]; 1 and above, NaN, or
+ *   NULL: no limit; the first id is always kept),
+ *   of these, every id with z - max z >= T ln(min_p) (dev fp32 [R]; 0 and below, NaN, or NULL: no limit; above 1 as 1).
+ * The id drawn is the smallest one whose running kept weight, in the order of the ids, exceeds u (dev fp32 [R], uniform in
+ * [0, 1); outside as the nearest inside, NaN as 0) times the kept weight.  T dev fp32 [R] (NULL: 1); where it is 0,
+ * negative or NaN the first maximum is drawn.  out dev int32 [R]; logp dev fp32 [R] or NULL: the logarithm of the drawn id's share of the kept
+ * weight.  NaN logits count as -inf, which is never kept; a row whose maximum is not finite gives -1 and -inf.
+ * Weights are taken in 64 bits, to 2^-44 of the largest (less weighs nothing), and sums are of whole multiples of 2^-43, so that
+ * they do not depend on their order: the draw is the exact one unless u or a limit meets the border of two
+ * ids by about 2^-44 for each id.  The same row gives the same id in any batch.  1 <= R <= 65536, 1 <= V <= 2^20, ldz >= V.  out, logp and the workspace
+ * overlap neither each other nor an input.  Asynchronous. */
+int32_t rgd_sample_truncated(const float* z, int64_t ldz, int32_t R, int32_t V, const float* T, const int32_t* top_k,
+                             const float* top_p, const float* min_p, const float* u, void* workspace, int32_t* out,
+                             float* logp, rgd_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,6 +1,6 @@
 """Paged sequences in float64 / plain integers: page tables with shared pages,
-their forks, roll-backs, reservations and compaction, and causal attention of a
-sequence's last tokens over its pages.
+their forks, roll-backs, reservations and compaction, what groups of them share, and causal
+attention of a sequence's last tokens over its pages.
 
 Arrays as the library lays them out: pages [S][width], lens [S], refs [n_pages],
 pool_k [L][n_pages][Hkv][ps][D], pool_v [L][n_pages][Hkv][D][ps].
@@ -76,6 +76,22 @@ def compact(pages, lens, refs, ps):
     for m, h in to.items():
         refs[h], refs[m] = refs[m], 0
     return pages, refs, list(to.items()), live
+
+
+def share(pages, lens, ps, new, group=None):
+    """Positions that each sequence with new tokens has, in whole pages in front of them, in common with all others
+    of its group that have some; 0 where there is none."""
+    S, width = pages.shape
+    label = [0] * S if group is None else [int(g) if 0 <= g < S else -1 - s for s, g in enumerate(group)]
+    out = np.zeros(S, int)
+    for g in set(label):
+        members = [s for s in range(S) if label[s] == g and new[s] > 0]
+        if len(members) < 2:
+            continue
+        n = min(max(min(max(int(lens[s]), 0), width * ps) - int(new[s]), 0) // ps for s in members)
+        same = [all(pages[s, j] == pages[members[0], j] for s in members) for j in range(n)]
+        out[members] = ps * (same.index(False) if False in same else n)
+    return out
 
 
 def gather(pool_k, pool_v, pages_row, length, ps):

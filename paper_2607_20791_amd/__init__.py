@@ -15,7 +15,9 @@ __all__ = [
     "sample_continuations", "sample_continuations_pless", "check_status", "kernel_attention", "kernel_lm_head", "kernel_argmax",
     "kernel_sample", "kernel_sample_noalloc", "kernel_sample_pless", "sampler_workspace_bytes", "timing_enable", "timing_read", "TIMERS", "PagedCache", "paged_workspace_bytes", "paged_select",
     "paged_reserve", "paged_compact", "paged_append", "paged_attention_workspace_bytes", "paged_attention",
-    "verify_workspace_bytes", "verify_drafts", "EVENT_INCOMPAT", "EVENT_STOP", "EVENT_MAXLEN",
+    "RotaryScaling", "Rotary", "paged_append_rotated", "paged_share_bytes", "paged_share",
+    "paged_attention_shared_workspace_bytes", "paged_attention_shared",
+    "verify_workspace_bytes", "verify_drafts", "sample_truncated_workspace_bytes", "sample_truncated", "EVENT_INCOMPAT", "EVENT_STOP", "EVENT_MAXLEN",
     "DTYPE_F32", "DTYPE_BF16",
 ]
 
@@ -28,6 +30,9 @@ EXPORTS = (
     "rgd_kernel_argmax", "rgd_kernel_sample", "rgd_kernel_sample_noalloc", "rgd_kernel_sample_pless", "rgd_kernel_probe_step", "rgd_timing_enable", "rgd_timing_read",
     "rgd_paged_workspace_bytes", "rgd_paged_select", "rgd_paged_reserve", "rgd_paged_reserve_granted", "rgd_paged_compact", "rgd_paged_append",
     "rgd_paged_attention_workspace_bytes", "rgd_paged_attention", "rgd_verify_workspace_bytes", "rgd_verify_drafts",
+    "rgd_rotary_frequencies", "rgd_paged_append_rotated", "rgd_paged_share_bytes", "rgd_paged_share",
+    "rgd_paged_attention_shared_workspace_bytes", "rgd_paged_attention_shared",
+    "rgd_sample_truncated_workspace_bytes", "rgd_sample_truncated",
 )
 
 DTYPE_F32, DTYPE_BF16 = 0, 1
@@ -73,6 +78,14 @@ class PagedCacheDesc(C.Structure):
     _fields_ = [(n, I32) for n in ("n_layers", "n_pages", "n_kv_heads", "page_size", "head_dim", "dtype", "max_seqs",
                                    "max_pages")] + \
                [(n, VP) for n in ("pool_k", "pool_v", "pages", "lens", "refs", "status")]
+
+
+class RotaryScalingDesc(C.Structure):
+    _fields_ = [("kind", I32), ("factor", C.c_double), ("context", C.c_double), ("low", C.c_double), ("high", C.c_double)]
+
+
+class RotaryDesc(C.Structure):
+    _fields_ = [("dim", I32), ("interleaved", I32), ("scale", F32), ("freq", C.POINTER(C.c_double))]
 
 
 def _sig(name, res, *args):
@@ -121,6 +134,15 @@ _sig("rgd_paged_attention_workspace_bytes", U64, _CACHE, I32, I32)
 _sig("rgd_paged_attention", I32, _CACHE, I32, VP, I64, I32, VP, I32, VP, VP, VP, VP)
 _sig("rgd_verify_workspace_bytes", U64, I32, I32, I32)
 _sig("rgd_verify_drafts", I32, VP, VP, VP, VP, I32, I32, I32, F32, F32, VP, VP, VP, VP, VP)
+_sig("rgd_rotary_frequencies", I32, I32, C.c_double, C.POINTER(RotaryScalingDesc), C.POINTER(C.c_double), C.POINTER(F32))
+_sig("rgd_paged_append_rotated", I32, _CACHE, I32, VP, VP, VP, I64, I64, I64, I32, VP, I32, VP, C.POINTER(RotaryDesc), VP, VP,
+     F32, VP, I64, VP)
+_sig("rgd_paged_share_bytes", U64, _CACHE, I32, I32)
+_sig("rgd_paged_share", I32, _CACHE, I32, VP, I32, VP, VP, VP, VP)
+_sig("rgd_paged_attention_shared_workspace_bytes", U64, _CACHE, I32, I32)
+_sig("rgd_paged_attention_shared", I32, _CACHE, I32, VP, I64, I32, I32, VP, VP, VP, VP, VP)
+_sig("rgd_sample_truncated_workspace_bytes", U64, I32, I32)
+_sig("rgd_sample_truncated", I32, VP, I64, I32, I32, VP, VP, VP, VP, VP, VP, VP, VP, VP)
 _sig("rgd_timing_enable", I32, VP, I32)
 _sig("rgd_timing_read", I32, VP, C.POINTER(C.c_double), C.POINTER(C.c_int64))
 
@@ -405,11 +427,15 @@ def _optional(device, name, t, dtype, shape):
     return None if t is None else _tensor(device, name, t, dtype, shape)
 
 
-def _workspace(device, ws, need):
-    p = _tensor(device, "workspace", ws, torch.uint8, None)
-    if ws.numel() < need:
-        _refuse(f"workspace holds {ws.numel()} of {need} bytes")
+def _sized(device, name, t, need):
+    p = _tensor(device, name, t, torch.uint8, None)
+    if t.numel() < need:
+        _refuse(f"{name} holds {t.numel()} of {need} bytes")
     return p
+
+
+def _workspace(device, ws, need):
+    return _sized(device, "workspace", ws, need)
 
 
 def _rows(device, name, t, dtype, shape):
@@ -543,6 +569,101 @@ def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
             _optional(dev, "lse", lse, torch.float32, (S * n, heads)))
 
 
+# ------------------------------------------------- rotary positions, head norms --
+class RotaryScaling:
+    """How a rotation's frequencies are changed by `factor` for positions beyond the trained `context`: kind "linear",
+    "base", "by_rotations" or "by_index" (the last two between `low` and `high` turns over the context)."""
+
+    KINDS = ("linear", "base", "by_rotations", "by_index")
+
+    def __init__(self, kind, factor, context=0.0, low=1.0, high=4.0):
+        if kind not in self.KINDS:
+            _refuse(f"kind must be one of {', '.join(self.KINDS)}")
+        self.desc = RotaryScalingDesc(1 + self.KINDS.index(kind), factor, context, low, high)
+
+
+class Rotary:
+    """A rotation of the first `dim` dimensions of a head, in pairs (j, j + dim / 2) or, interleaved, (2 j, 2 j + 1), by
+    position * freq[j] radians, cosine and sine times `scale`.  Give theta (and scaling), or frequencies of your own."""
+
+    def __init__(self, dim, theta=None, interleaved=False, scaling=None, freq=None, scale=1.0):
+        _int32(dim)
+        if (theta is None) == (freq is None):
+            _refuse("one of theta and freq is wanted")
+        if freq is None:
+            factor = F32(1.0)
+            self.freq = (C.c_double * max(1, min(dim, 128) // 2))()
+            _check(lib.rgd_rotary_frequencies(dim, theta, C.byref(scaling.desc) if scaling else None, self.freq,
+                                              C.byref(factor)))
+            scale *= factor.value
+        else:
+            if scaling is not None:
+                _refuse("scaling goes with theta")
+            if len(freq) * 2 != dim:
+                _refuse(f"{dim} dimensions have {dim // 2} frequencies, got {len(freq)}")
+            self.freq = (C.c_double * max(1, len(freq)))(*freq)
+        self.dim, self.interleaved, self.scale = dim, bool(interleaved), scale
+        self.desc = RotaryDesc(dim, self.interleaved, scale, self.freq)
+        self.ref = C.byref(self.desc)
+
+
+def paged_append_rotated(cache, layer, q, k, v, n, rotary, q_out, n_new=None, positions=None, q_norm=None, k_norm=None,
+                         eps=1e-5):
+    """paged_append of q [S * n][heads][D], k and v [S * n][Hkv][D] (rows may lie apart) as a projection leaves them: the
+    heads of q and k are normed (gains q_norm, k_norm [D] fp32, None: not), rotated by their positions (positions int32 [S * n],
+    None: those in the cache; rotary None: not), k and v appended to the pages of one layer and q written to q_out (q itself, or apart)."""
+    _int32(layer, n)
+    dev, S, D, i32, f32 = cache.gpu, cache.max_seqs, cache.head_dim, torch.int32, torch.float32
+    if q is None or q.dim() != 3:
+        _refuse("q must be a tensor of three dimensions")
+    heads, kv = q.shape[1], (S * n, cache.n_kv_heads, D)
+    shape = (S * n, heads, D)
+    pq, ldq = _rows(dev, "q", q, cache.dtype, shape)
+    pk, ldk = _rows(dev, "k", k, cache.dtype, kv)
+    pv, ldv = _rows(dev, "v", v, cache.dtype, kv)
+    po, ldo = _rows(dev, "q_out", q_out, cache.dtype, shape)
+    _launch(dev, lib.rgd_paged_append_rotated, cache.ref, layer, pq, pk, pv, ldq, ldk, ldv, n,
+            _optional(dev, "n_new", n_new, i32, (S,)), heads, _optional(dev, "positions", positions, i32, (S * n,)),
+            None if rotary is None else rotary.ref, _optional(dev, "q_norm", q_norm, f32, (D,)),
+            _optional(dev, "k_norm", k_norm, f32, (D,)), eps, po, ldo)
+
+
+# ------------------------------------------- attention over pages that are shared --
+def paged_share_bytes(cache, n, n_heads):
+    return cache.need(("share", n, n_heads), lib.rgd_paged_share_bytes, n, n_heads)
+
+
+def paged_share(cache, n, n_new, n_heads, group, plan, shared=None):
+    """Finds which leading pages the sequences of each group (labels int32 [S]; None: all are one) share, for up to n new
+    tokens each (n_new int32 [S], None: n), once for all layers: plan (uint8, paged_share_bytes) receives it for
+    paged_attention_shared, shared (int32 [S]) the positions."""
+    _int32(n, n_heads)
+    dev, i32, shape = cache.gpu, torch.int32, (cache.max_seqs,)
+    _launch(dev, lib.rgd_paged_share, cache.ref, n, _optional(dev, "n_new", n_new, i32, shape), n_heads,
+            _optional(dev, "group", group, i32, shape), _sized(dev, "plan", plan, paged_share_bytes(cache, n, n_heads)),
+            _optional(dev, "shared", shared, i32, shape))
+
+
+def paged_attention_shared_workspace_bytes(cache, n, n_heads):
+    return cache.need(("shared", n, n_heads), lib.rgd_paged_attention_shared_workspace_bytes, n, n_heads)
+
+
+def paged_attention_shared(cache, layer, q, n, plan, workspace, out, lse=None):
+    """paged_attention with the counts of a plan, whose shared positions are read once for each group: q
+    [S * n][heads][D] (rows may lie apart) into out [S * n][heads * D] and lse [S * n][heads]."""
+    _int32(layer, n)
+    dev, S, D = cache.gpu, cache.max_seqs, cache.head_dim
+    if q is None or q.dim() != 3:
+        _refuse("q must be a tensor of three dimensions")
+    heads = q.shape[1]
+    pq, ldq = _rows(dev, "q", q, cache.dtype, (S * n, heads, D))
+    _launch(dev, lib.rgd_paged_attention_shared, cache.ref, layer, pq, ldq, n, heads,
+            _sized(dev, "plan", plan, paged_share_bytes(cache, n, heads)),
+            _workspace(dev, workspace, paged_attention_shared_workspace_bytes(cache, n, heads)),
+            _tensor(dev, "out", out, cache.dtype, (S * n, heads * D)),
+            _optional(dev, "lse", lse, torch.float32, (S * n, heads)))
+
+
 # ------------------------------------------------------- verification of drafts --
 def verify_workspace_bytes(S, K, V):
     _int32(S, K, V)
@@ -564,3 +685,28 @@ def verify_drafts(target, draft, draft_tokens, n_draft, T, min_p, u, workspace, 
             _optional(dev, "n_draft", n_draft, i32, (S,)), S, K, V, T, min_p, _tensor(dev, "u", u, f32, (S, K1)),
             _workspace(dev, workspace, verify_workspace_bytes(S, K, V)), _tensor(dev, "out", out, i32, (S, K1)),
             _tensor(dev, "n_accepted", n_accepted, i32, (S,)))
+
+
+# ------------------------------------------------- sampling with limits for each row --
+def sample_truncated_workspace_bytes(R, V):
+    _int32(R, V)
+    n = lib.rgd_sample_truncated_workspace_bytes(R, V)
+    if n == 0:
+        _refuse("R or V out of range")
+    return int(n)
+
+
+def sample_truncated(z, u, workspace, out, T=None, top_k=None, top_p=None, min_p=None, logp=None):
+    """Draws one id from each row of logits z [R][V] (rows may lie apart) by the uniforms u [R], under limits for each row:
+    temperature T, then top_k (int32), top_p and min_p (each [R]; None: without); logp [R] receives the id's log probability."""
+    if z is None or z.dim() != 2 or not z.is_cuda:
+        _refuse("z must be a 2-dimensional tensor on a GPU")
+    R, V = z.shape
+    dev, f32, i32, shape = z.get_device(), torch.float32, torch.int32, (R,)
+    if z.dtype is not f32 or (V > 1 and z.stride(1) != 1):
+        _refuse(f"z must be fp32 with contiguous rows, got {z.dtype} of strides {z.stride()}")
+    _launch(dev, lib.rgd_sample_truncated, z.data_ptr(), z.stride(0) if R > 1 else V, R, V, _optional(dev, "T", T, f32, shape),
+            _optional(dev, "top_k", top_k, i32, shape), _optional(dev, "top_p", top_p, f32, shape),
+            _optional(dev, "min_p", min_p, f32, shape), _tensor(dev, "u", u, f32, shape),
+            _workspace(dev, workspace, sample_truncated_workspace_bytes(R, V)), _tensor(dev, "out", out, i32, shape),
+            _optional(dev, "logp", logp, f32, shape))

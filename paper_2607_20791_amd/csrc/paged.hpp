@@ -1,5 +1,5 @@
 // Paged sequences (internal): the kernels' view of an rgd_paged_cache and the
-// launch interface of its operators and of the draft verification.
+// launch interface of its operators, of the draft verification and of the sampler with per-row limits.
 #pragma once
 #include "common.hpp"
 
@@ -39,6 +39,51 @@ struct PagedAttnArgs {
 bool paged_attention_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq);
 hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s);
+
+constexpr int kRotaryLinear = 1, kRotaryBase = 2, kRotaryByRotations = 3, kRotaryByIndex = 4;
+struct RotaryScaling {
+  int kind;
+  double factor, context, low, high;
+};
+void rotary_frequencies(int dim, double theta, const RotaryScaling* scaling, double* freq, float* scale);
+
+struct RotateArgs {
+  PagedView c;
+  void *pool_k, *pool_v;  // of the layer
+  const void *q, *k, *v; long long ldq, ldk, ldv;
+  void* out; long long ldo;
+  int n; const int *n_new, *positions;
+  const float *q_norm, *k_norm; float eps;
+  int dim, interleaved; float scale;
+  double turns[64];  // of each pair, per position
+  int G;       // query heads per KV head
+  int blocks;  // 16-position blocks per sequence
+};
+hipError_t paged_append_rotated(const RotateArgs& a, hipStream_t s);
+
+// What the sequences of a group share (see rgd_paged_share); ints in the caller's plan.
+struct ShareArgs {
+  PagedView c;
+  int n; const int *n_new, *group;
+  int Hq;
+  int* plan;
+  int* shared;
+};
+size_t paged_share_ints(const PagedView& c, int n);
+hipError_t paged_share(const ShareArgs& a, hipStream_t s);
+// a.n_new is taken from the plan
+hipError_t paged_attention_shared(const PagedAttnArgs& a, const int* plan, hipStream_t s);
+size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq);
+
+struct TruncateArgs {
+  const float* z; long long ldz;
+  int R, V;
+  const float* T; const int* top_k; const float *top_p, *min_p, *u;
+  int* out; float* logp;
+  char* ws;
+};
+size_t sample_truncated_workspace_bytes(int R, int V);
+hipError_t sample_truncated(const TruncateArgs& a, hipStream_t s);
 
 struct VerifyArgs {
   const float *target, *draft;  // [S][K+1][V], [S][K][V] or null

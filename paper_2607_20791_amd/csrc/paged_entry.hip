@@ -1,6 +1,7 @@
-// C ABI of the paged sequences and of the draft verification: argument checks
+// C ABI of the paged sequences, of the draft verification and of the sampler with per-row limits: argument checks
 // (before any HIP call), then the launches.
 #include <algorithm>
+#include <cmath>
 #include <initializer_list>
 
 #include "entry.hpp"
@@ -112,6 +113,34 @@ int32_t reserve(const rgd_paged_cache* cache, const int32_t* grow, int32_t* gran
   const Range in(grow, (uint64_t)v.S * 4), out(granted, (uint64_t)v.S * 4), none(nullptr, 0);
   if (const char* why = work_ok(v, workspace, out, granted == grow ? none : in, none)) return bad(why);
   return launched(paged_reserve(v, grow, granted, (int*)workspace, (hipStream_t)stream));
+}
+
+// Whether rows at `out` share memory with rows at `in`, each of so many bytes, n rows.  Rows of one stride, as those of
+// a fused projection, may lie between each other.
+bool rows_overlap(const void* out, int64_t ld_out, int64_t row_out, const void* in, int64_t ld_in, int64_t row_in,
+                  int64_t n) {
+  if (!overlap(rows_of(out, n, ld_out, row_out), rows_of(in, n, ld_in, row_in))) return false;
+  if (ld_out != ld_in || n == 1) return true;
+  // the distance from an output row to the next input row that starts at or behind it, and from that one on
+  const int64_t gap = (int64_t)((uintptr_t)in - (uintptr_t)out) % ld_out, ahead = gap < 0 ? gap + ld_out : gap;
+  return ahead < row_out || ahead + row_in > ld_out;
+}
+
+const char* rotary_ok(const rgd_rotary* r, int D) {
+  if (!r || r->dim == 0) return nullptr;
+  if (r->dim < 0 || r->dim > D || r->dim % 2) return "a rotation's dim must be even, at most head_dim";
+  if (!r->freq) return "null frequencies";
+  if (!std::isfinite(r->scale)) return "a rotation's scale must be finite";
+  for (int j = 0; j < r->dim / 2; ++j)
+    if (!std::isfinite(r->freq[j])) return "frequencies must be finite";
+  return nullptr;
+}
+
+// A plan's or a workspace's size is refused with the entry point's arguments.
+const char* shared_ok(const PagedView& v, int32_t n, int32_t n_heads) {
+  if (const char* why = heads_ok(v, n, n_heads)) return why;
+  if ((int64_t)v.S * n * n_heads > (1 << 22)) return "max_seqs * n * n_heads must be at most 2^22";
+  return nullptr;
 }
 
 }  // namespace
@@ -238,6 +267,186 @@ int32_t rgd_verify_drafts(const float* target, const float* draft, const int32_t
     return bad("an output or the workspace overlaps an input or another output");
   VerifyArgs a{target, draft, draft_tokens, n_draft, S, K, V, T, min_p, u, out, n_accepted, (char*)workspace};
   return launched(verify_drafts(a, (hipStream_t)stream));
+}
+
+int32_t rgd_rotary_frequencies(int32_t dim, double theta, const rgd_rotary_scaling* scaling, double* freq,
+                               float* scale) {
+  clear_error();
+  if (!freq || !scale) return bad("null argument");
+  if (dim < 2 || dim > 128 || dim % 2) return bad("dim must be even, 2 to 128");
+  if (!(theta > 1.0 && std::isfinite(theta))) return bad("theta must be above 1 and finite");
+  RotaryScaling how{};
+  if (scaling) {
+    how = RotaryScaling{scaling->kind, scaling->factor, scaling->context, scaling->low, scaling->high};
+    if (how.kind < kRotaryLinear || how.kind > kRotaryByIndex) return bad("unknown kind of scaling");
+    if (!(how.factor >= 1.0 && std::isfinite(how.factor))) return bad("factor must be at least 1 and finite");
+    if (how.kind == kRotaryBase && dim < 4) return bad("dim must be above 2 where theta is scaled");
+    if (how.kind >= kRotaryByRotations) {
+      if (!(how.context > 0.0 && std::isfinite(how.context))) return bad("context must be positive and finite");
+      if (!(how.low > 0.0 && how.low < how.high && std::isfinite(how.high))) return bad("0 < low < high is wanted");
+    }
+  }
+  rotary_frequencies(dim, theta, scaling ? &how : nullptr, freq, scale);
+  return RGD_OK;
+}
+
+int32_t rgd_paged_append_rotated(const rgd_paged_cache* cache, int32_t layer, const void* q, const void* k,
+                                 const void* v, int64_t ldq, int64_t ldk, int64_t ldv, int32_t n,
+                                 const int32_t* n_new, int32_t n_heads, const int32_t* positions,
+                                 const rgd_rotary* rotary, const float* q_norm, const float* k_norm, float eps,
+                                 void* q_out, int64_t ldo, rgd_stream stream) {
+  clear_error();
+  RotateArgs a{};
+  if (const char* why = view_of(cache, a.c)) return bad(why);
+  if (!q || !k || !v || !q_out) return bad("null argument");
+  if (layer < 0 || layer >= a.c.L) return bad("layer out of range");
+  if (n < 1 || (int64_t)a.c.S * n > (1 << 24)) return bad("n out of range");
+  if (n_heads < 1 || n_heads > 1024 || n_heads % a.c.Hkv) return bad("n_heads must be a multiple of n_kv_heads, at most 1024");
+  const int64_t rows = (int64_t)a.c.S * n, esz = (int64_t)a.c.esz, wq = (int64_t)n_heads * a.c.D, wk = (int64_t)a.c.Hkv * a.c.D;
+  if (const char* why = rows_ok(a.c, q, ldq, wq)) return bad(why);
+  if (const char* why = rows_ok(a.c, k, ldk, wk)) return bad(why);
+  if (const char* why = rows_ok(a.c, v, ldv, wk)) return bad(why);
+  if (const char* why = rows_ok(a.c, q_out, ldo, wq)) return bad(why);
+  if (const char* why = rotary_ok(rotary, a.c.D)) return bad(why);
+  if ((q_norm || k_norm) && !(eps >= 0.f && std::isfinite(eps))) return bad("eps must be at least 0 and finite");
+  const bool in_place = q_out == q && ldo == ldq;
+  const Range out = rows_of(q_out, rows, ldo * esz, wq * esz);
+  if ((!in_place && rows_overlap(q_out, ldo * esz, wq * esz, q, ldq * esz, wq * esz, rows)) ||
+      rows_overlap(q_out, ldo * esz, wq * esz, k, ldk * esz, wk * esz, rows) ||
+      rows_overlap(q_out, ldo * esz, wq * esz, v, ldv * esz, wk * esz, rows))
+    return bad("q_out overlaps q (other than in place), k or v");
+  const Range counts(n_new, (uint64_t)a.c.S * 4), at(positions, (uint64_t)rows * 4), gq(q_norm, (uint64_t)a.c.D * 4),
+      gk(k_norm, (uint64_t)a.c.D * 4);
+  if (outputs_shared({out}, {counts, at, gq, gk}) || shares_cache(a.c, {out}))
+    return bad("q_out overlaps an input or the cache");
+  // (ranges of the inputs against the cache's one by one: they may share memory with each other)
+  for (const Range& in : {rows_of(q, rows, ldq * esz, wq * esz), rows_of(k, rows, ldk * esz, wk * esz),
+                          rows_of(v, rows, ldv * esz, wk * esz), counts, at, gq, gk})
+    if (shares_cache(a.c, {in})) return bad("an input overlaps the cache");
+  const size_t layer0 = (size_t)layer * a.c.n_pages * a.c.page_elems() * a.c.esz;
+  a.pool_k = a.c.pool_k + layer0;
+  a.pool_v = a.c.pool_v + layer0;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.out = q_out;
+  a.ldo = ldo;
+  a.n = n;
+  a.n_new = n_new;
+  a.positions = positions;
+  a.q_norm = q_norm;
+  a.k_norm = k_norm;
+  a.eps = eps;
+  a.G = n_heads / a.c.Hkv;
+  if (rotary) {
+    a.dim = rotary->dim;
+    a.interleaved = rotary->interleaved != 0;
+    a.scale = rotary->scale;
+    for (int j = 0; j < a.dim / 2; ++j) a.turns[j] = rotary->freq[j] / 6.283185307179586;
+  }
+  return launched(paged_append_rotated(a, (hipStream_t)stream));
+}
+
+uint64_t rgd_paged_share_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads) {
+  clear_error();
+  PagedView v;
+  const char* why = view_of(cache, v);
+  if (!why) why = shared_ok(v, n, n_heads);
+  if (why) {
+    bad(why);
+    return 0;
+  }
+  return paged_share_ints(v, n) * sizeof(int);
+}
+
+int32_t rgd_paged_share(const rgd_paged_cache* cache, int32_t n, const int32_t* n_new, int32_t n_heads,
+                        const int32_t* group, void* plan, int32_t* shared, rgd_stream stream) {
+  clear_error();
+  ShareArgs a{};
+  if (const char* why = view_of(cache, a.c)) return bad(why);
+  if (!plan) return bad("null argument");
+  if (const char* why = shared_ok(a.c, n, n_heads)) return bad(why);
+  if (!aligned(plan, 256)) return bad("the plan must be 256-byte aligned");
+  const uint64_t counts = (uint64_t)a.c.S * 4;
+  const Range p(plan, paged_share_ints(a.c, n) * sizeof(int)), o(shared, counts);
+  if (outputs_shared({p, o}, {Range(n_new, counts), Range(group, counts)}) || shares_cache(a.c, {p, o}))
+    return bad("the plan or shared overlaps an input, the cache or each other");
+  a.n = n;
+  a.n_new = n_new;
+  a.group = group;
+  a.Hq = n_heads;
+  a.plan = (int*)plan;
+  a.shared = shared;
+  return launched(paged_share(a, (hipStream_t)stream));
+}
+
+uint64_t rgd_paged_attention_shared_workspace_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads) {
+  clear_error();
+  PagedView v;
+  const char* why = view_of(cache, v);
+  if (!why) why = shared_ok(v, n, n_heads);
+  if (why) {
+    bad(why);
+    return 0;
+  }
+  return paged_attention_shared_workspace_floats(v, n, n_heads) * sizeof(float);
+}
+
+int32_t rgd_paged_attention_shared(const rgd_paged_cache* cache, int32_t layer, const void* q, int64_t ldq, int32_t n,
+                                   int32_t n_heads, const void* plan, void* workspace, void* out, float* lse,
+                                   rgd_stream stream) {
+  clear_error();
+  PagedAttnArgs a{};
+  if (const char* why = view_of(cache, a.c)) return bad(why);
+  if (!q || !plan || !workspace || !out) return bad("null argument");
+  if (layer < 0 || layer >= a.c.L) return bad("layer out of range");
+  if (const char* why = shared_ok(a.c, n, n_heads)) return bad(why);
+  const int64_t width = (int64_t)n_heads * a.c.D, rows = (int64_t)a.c.S * n;
+  if (const char* why = rows_ok(a.c, q, ldq, width)) return bad(why);
+  if (!aligned(out, 16) || !aligned(workspace, 256) || !aligned(plan, 256))
+    return bad("out must be 16-byte, the plan and the workspace 256-byte aligned");
+  const int64_t esz = (int64_t)a.c.esz;
+  const Range o(out, rows * width * esz), l(lse, rows * n_heads * 4),
+      w(workspace, paged_attention_shared_workspace_floats(a.c, n, n_heads) * sizeof(float)),
+      p(plan, paged_share_ints(a.c, n) * sizeof(int));
+  if (outputs_shared({o, l, w}, {rows_of(q, rows, ldq * esz, width * esz), p}) || shares_cache(a.c, {o, l, w}))
+    return bad("out, lse or the workspace overlaps an input, the cache or each other");
+  const size_t layer0 = (size_t)layer * a.c.n_pages * a.c.page_elems() * a.c.esz;
+  a.pool_k = a.c.pool_k + layer0;
+  a.pool_v = a.c.pool_v + layer0;
+  a.q = q;
+  a.ldq = ldq;
+  a.n = n;
+  a.Hq = n_heads;
+  a.out = out;
+  a.lse = lse;
+  a.ws = (float*)workspace;
+  return launched(paged_attention_shared(a, (const int*)plan, (hipStream_t)stream));
+}
+
+uint64_t rgd_sample_truncated_workspace_bytes(int32_t R, int32_t V) {
+  if (R < 1 || R > 65536 || V < 1 || V > (1 << 20)) return 0;
+  return sample_truncated_workspace_bytes(R, V);
+}
+
+int32_t rgd_sample_truncated(const float* z, int64_t ldz, int32_t R, int32_t V, const float* T, const int32_t* top_k,
+                             const float* top_p, const float* min_p, const float* u, void* workspace, int32_t* out,
+                             float* logp, rgd_stream stream) {
+  clear_error();
+  if (!z || !u || !workspace || !out) return bad("null argument");
+  if (!rgd_sample_truncated_workspace_bytes(R, V)) return bad("R or V out of range");
+  if (ldz < V || ldz > ((int64_t)1 << 40)) return bad("row stride smaller than a row");
+  if (!aligned(workspace, 256)) return bad("workspace must be 256-byte aligned");
+  const uint64_t r4 = (uint64_t)R * 4;
+  if (outputs_shared({Range(out, r4), Range(logp, r4), Range(workspace, sample_truncated_workspace_bytes(R, V))},
+                     {rows_of(z, R, ldz * 4, (int64_t)V * 4), Range(T, r4), Range(top_k, r4), Range(top_p, r4),
+                      Range(min_p, r4), Range(u, r4)}))
+    return bad("an output or the workspace overlaps an input or another output");
+  TruncateArgs a{z, ldz, R, V, T, top_k, top_p, min_p, u, out, logp, (char*)workspace};
+  return launched(sample_truncated(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -22,6 +22,7 @@
 #include <cmath>
 
 #include "paged.hpp"
+#include "weights.hpp"
 
 namespace rgd {
 
@@ -37,25 +38,6 @@ constexpr int kMaxParts = 16;    // workgroups that share a row in pass 3
 constexpr int kResident = 5120;  // waves of pass 2 at a time: 20 per CU
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
-
-// 2^x to 1e-14 for x <= 0: the Taylor series of 2^f, |f| <= 1/2, to f^11.
-RGD_DEV double exp2_f64(double x) {
-  x = fmax(x, -1100.0);  // below: 0 either way (and -inf - rint(-inf) is not a number)
-  const double n = rint(x), g = (x - n) * 0.6931471805599453;
-  double s = 1.0 / 39916800.0;
-  s = fma(s, g, 1.0 / 3628800.0);
-  s = fma(s, g, 1.0 / 362880.0);
-  s = fma(s, g, 1.0 / 40320.0);
-  s = fma(s, g, 1.0 / 5040.0);
-  s = fma(s, g, 1.0 / 720.0);
-  s = fma(s, g, 1.0 / 120.0);
-  s = fma(s, g, 1.0 / 24.0);
-  s = fma(s, g, 1.0 / 6.0);
-  s = fma(s, g, 0.5);
-  s = fma(s, g, 1.0);
-  s = fma(s, g, 1.0);
-  return ldexp(s, (int)n);
-}
 
 RGD_DEV double wave_sum_f64(double v) {
 #pragma unroll
@@ -163,19 +145,6 @@ __global__ __launch_bounds__(256) void verify_max_kernel(Job j, int groups) {
   if (lane == 63) j.chunk_max[r * j.chunks + first * kSpan / kChunk] = mine;
 }
 
-// The lowest kept logit of a row of maximum `top`: the smallest float z with
-// (double)z - top >= low, so that one fp32 comparison decides as fp64 does.
-RGD_DEV float threshold(float top, double low) {
-  float f = (float)((double)top + low);
-  for (int i = 0; i < 4 && (double)f - (double)top < low; ++i) f = nextafterf(f, INFINITY);
-  for (int i = 0; i < 4; ++i) {
-    const float g = nextafterf(f, -INFINITY);
-    if (!((double)g - (double)top >= low)) break;
-    f = g;
-  }
-  return f;
-}
-
 // One row's distribution.
 struct Dist {
   const float* z;
@@ -189,8 +158,6 @@ struct Dist {
     return weight(x) * scale;
   }
 };
-
-RGD_DEV bool finite_top(float t) { return t > -INFINITY && t < INFINITY; }
 
 // Row r, of kept sum W.  A row without a finite maximum keeps nothing.
 RGD_DEV Dist dist_of(const Job& j, const float* logits, long long r, double W) {

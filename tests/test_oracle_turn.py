@@ -1,0 +1,134 @@
+"""Pins of the oracles of a paged decoder's turn: rotary frequencies and rotations, shared pages, and the truncated draw."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+
+from oracle import model, paged, rotary, sampler, truncate
+
+
+@pytest.mark.parametrize("dim", [4, 64, 128])
+def test_rotation_in_halves_is_the_models(dim):
+    r = np.random.default_rng(dim)
+    x = r.standard_normal((3, dim))
+    f, scale = rotary.frequencies(dim, 500000.0)
+    assert scale == 1.0
+    for pos in (0, 1, 77, 8191):
+        assert np.allclose(rotary.rotate(x, pos, f), model.rope(x, pos, 500000.0), rtol=0, atol=1e-12)
+
+
+def test_interleaved_pairs_are_complex_numbers():
+    r = np.random.default_rng(0)
+    x, f = r.standard_normal((2, 12)), np.array([1.0, 0.1, 0.01])
+    y = rotary.rotate(x, 5, f, 1.5, True)
+    z = (x[:, 0:6:2] + 1j * x[:, 1:6:2]) * 1.5 * np.exp(5j * f)
+    assert np.allclose(y[:, 0:6:2], z.real) and np.allclose(y[:, 1:6:2], z.imag) and (y[:, 6:] == x[:, 6:]).all()
+
+
+def test_scores_depend_on_the_distance_alone():
+    r = np.random.default_rng(1)
+    q, k = r.standard_normal((2, 1, 64))
+    f, _ = rotary.frequencies(64, 10000.0, "by_index", 8.0, 4096, 1.0, 32.0)
+    dots = [float((rotary.rotate(q, 40 + a, f, 1.0, i) * rotary.rotate(k, 7 + a, f, 1.0, i)).sum())
+            for i in (False, True) for a in (0, 1000)]
+    assert abs(dots[0] - dots[1]) < 1e-9 and abs(dots[2] - dots[3]) < 1e-9
+
+
+def test_scaled_frequencies_at_their_ends():
+    base, _ = rotary.frequencies(128, 500000.0)
+    for kind in ("linear", "base", "by_rotations", "by_index"):
+        one, scale = rotary.frequencies(128, 500000.0, kind, 1.0, 8192)
+        assert np.allclose(one, base, rtol=1e-14) and scale == 1.0
+    f, _ = rotary.frequencies(128, 500000.0, "linear", 4.0)
+    assert np.allclose(f, base / 4)
+    f, _ = rotary.frequencies(128, 500000.0, "base", 4.0)
+    assert f[0] == 1.0 and math.isclose(f[-1], base[-1] / 4, rel_tol=1e-12)
+    for kind in ("by_rotations", "by_index"):  # fast pairs as they are, slow ones over factor, falling in between
+        f, scale = rotary.frequencies(128, 500000.0, kind, 8.0, 8192, 1.0, 4.0)
+        turns = 8192 * base / (2 * math.pi)
+        assert np.allclose(f[turns > 5], base[turns > 5]) and np.allclose(f[turns < 0.8], base[turns < 0.8] / 8)
+        assert (np.diff(f) < 0).all() and scale == (1 + math.log(8) / 10 if kind == "by_index" else 1.0)
+
+
+@pytest.mark.parametrize("dim,theta", [(2, 10000.0), (4, 10000.0), (22, 500000.0), (64, 10000.0), (118, 1e6), (128, 500000.0)])
+@pytest.mark.parametrize("how", [None, ("linear", 4.0, 0.0, 1.0, 4.0), ("base", 2.5, 0.0, 1.0, 4.0),
+                                 ("by_rotations", 8.0, 8192, 1.0, 4.0), ("by_index", 16.0, 4096, 1.0, 32.0)])
+def test_the_library_gives_the_oracles_frequencies(dim, theta, how):
+    import paper_2607_20791_amd as rgd
+    if how and how[0] == "base" and dim == 2:
+        with pytest.raises(rgd.RGDError):
+            rgd.Rotary(dim, theta, scaling=rgd.RotaryScaling(*how))
+        return
+    r = rgd.Rotary(dim, theta, scaling=rgd.RotaryScaling(*how) if how else None)
+    f, scale = rotary.frequencies(dim, theta, *(how or ()))
+    # a dozen fp64 operations; the scale is rounded to fp32
+    assert np.allclose(np.array(r.freq[:dim // 2]), f, rtol=1e-13, atol=0) and abs(r.scale - scale) <= 2.0**-24 * scale
+
+
+def test_shared_pages_by_hand():
+    pages = np.array([[0, 1, 2, -1], [0, 1, 3, 4], [0, 5, 6, -1], [9, 1, 2, -1], [0, 1, 2, -1]])
+    lens = np.array([40, 55, 40, 40, 33])
+    ones = np.ones(5, int)
+    assert list(paged.share(pages[:2], lens[:2], 16, ones[:2])) == [32, 32]
+    assert list(paged.share(pages[:3], lens[:3], 16, ones[:3])) == [16, 16, 16]
+    assert list(paged.share(pages, lens, 16, ones)) == [0] * 5                  # the fourth starts elsewhere
+    assert list(paged.share(pages, lens, 16, ones, [0, 0, 2, 3, 0])) == [32, 32, 0, 0, 32]
+    assert list(paged.share(pages, lens, 16, [1, 0, 1, 1, 1], [0, 0, 0, 9, -1])) == [16, 0, 16, 0, 0]
+    assert list(paged.share(pages, lens, 16, [9, 1, 0, 0, 1], [0] * 5)) == [16, 16, 0, 0, 16]  # 40 - 9 positions: one page
+    assert list(paged.share(pages, lens, 16, [1, 0, 0, 0, 0])) == [0] * 5
+    assert list(paged.share(pages[[0, 0]], lens[[0, 0]], 16, [1, 1])) == [32, 32]  # 39 positions in front: two pages
+
+
+def test_truncated_draw_by_hand():
+    z = np.log(np.array([0.1, 0.4, 0.2, 0.25, 0.05]))
+    assert list(truncate.draw(z, 0.0, top_k=2).kept) == [1, 3]
+    assert list(truncate.draw(z, 0.0, top_p=0.7).kept) == [1, 2, 3]      # 0.4 + 0.25 is less
+    assert list(truncate.draw(z, 0.0, top_p=0.6).kept) == [1, 3]
+    assert list(truncate.draw(z, 0.0, top_p=0.0).kept) == [1]
+    assert list(truncate.draw(z, 0.0, min_p=0.45).kept) == [1, 2, 3]
+    assert list(truncate.draw(z, 0.0, top_k=3, top_p=0.75).kept) == [1, 3]  # of 0.85: 0.6375 and less in front of the third
+    d = truncate.draw(z, 0.5, top_k=3)                                   # runs 0.4, 0.6, 0.85; 0.425 is passed at id 2
+    assert d.token == 2 and math.isclose(d.logp, math.log(0.2 / 0.85), rel_tol=1e-12)
+    assert truncate.draw(z, 0.9, T=0.0).token == 1 and truncate.draw(z, 0.9, top_k=1).token == 1
+    ties = np.zeros(4)
+    assert list(truncate.draw(ties, 0.0, top_k=3).kept) == [0, 1, 2] and list(truncate.draw(ties, 0.0, top_p=0.5).kept) == [0, 1]
+    assert truncate.draw([-np.inf, np.nan], 0.5).token == -1 and truncate.draw([-np.inf, np.inf], 0.5).token == -1
+    assert list(truncate.draw([0.0, -np.inf, np.nan], 0.9, top_k=3).kept) == [0]
+
+
+def test_without_top_k_and_top_p_it_is_the_samplers_draw():
+    r = np.random.default_rng(3)
+    for T, p in ((1.0, 0.1), (2.0, 0.02), (0.7, 0.3)):
+        for _ in range(50):
+            z, u = r.standard_normal(400) * 3, r.random()
+            assert truncate.draw(z, u, T, min_p=p).token == sampler.sample_minp(z, T, p, u).token
+
+
+def test_draws_follow_the_kept_distribution():
+    z = np.array([0.3, 1.2, -0.5, 2.0, 0.9, -2.0])
+    ids, w, _ = truncate.kept_ids(z, 1.3, 5, 0.9, 0.05)
+    p = dict(zip(ids, w / w.sum()))
+    us = (np.arange(20000) + 0.5) / 20000
+    got = np.bincount([truncate.draw(z, u, 1.3, 5, 0.9, 0.05).token for u in us], minlength=6) / 20000
+    assert all(abs(got[i] - p.get(i, 0.0)) < 1e-4 for i in range(6))
+
+
+def test_refusals_of_rotations():
+    import paper_2607_20791_amd as rgd
+    lib, f, s = rgd.lib, (C.c_double * 64)(), C.c_float()
+    ok = lambda dim, theta, sc=None: lib.rgd_rotary_frequencies(dim, theta, sc and C.byref(sc), f, C.byref(s))  # noqa: E731
+    D = rgd.RotaryScalingDesc
+    assert ok(64, 10000.0) == 0 and ok(64, 10000.0, D(3, 2.0, 100.0, 1.0, 2.0)) == 0
+    for bad in ((0, 1e4), (3, 1e4), (130, 1e4), (-2, 1e4), (64, 1.0), (64, float("nan")), (64, float("inf"))):
+        assert ok(*bad) == 1 and lib.rgd_last_error()
+    for bad in (D(0, 2.0, 1.0, 1.0, 2.0), D(5, 2.0, 1.0, 1.0, 2.0), D(1, 0.5, 1.0, 1.0, 2.0), D(1, float("nan"), 1.0, 1.0, 2.0),
+                D(3, 2.0, 0.0, 1.0, 2.0), D(3, 2.0, 1.0, 2.0, 2.0), D(4, 2.0, 1.0, 0.0, 2.0), D(4, 2.0, 1.0, 1.0, float("inf"))):
+        assert ok(64, 10000.0, bad) == 1
+    assert ok(2, 1e4, D(2, 2.0, 1.0, 1.0, 2.0)) == 1
+    assert lib.rgd_rotary_frequencies(64, 1e4, None, None, C.byref(s)) == 1
+    for kw in (dict(theta=None), dict(theta=1e4, freq=[1.0] * 32), dict(freq=[1.0] * 31), dict(freq=[1.0] * 32, scaling=1)):
+        with pytest.raises(rgd.RGDError):
+            rgd.Rotary(64, **kw)
+    with pytest.raises(rgd.RGDError):
+        rgd.RotaryScaling("cubic", 2.0)
