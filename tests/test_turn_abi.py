@@ -120,6 +120,12 @@ def test_sampler_arguments(rgd):
         assert draw(**kw) == INVALID and lib.rgd_last_error(), kw
 
 
+@pytest.mark.parametrize("V", [1, 700, 5000, 20000, 50257, 152064, 1 << 20])
+def test_a_samplers_workspace_serves_fewer_rows_too(rgd, V):
+    sizes = [rgd.sample_truncated_workspace_bytes(R, V) for R in list(range(1, 1100)) + [4096, 65536]]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
 def test_binding_numbers_beyond_31_bits_are_refused(rgd):
     for fn in (lambda: rgd.sample_truncated_workspace_bytes(1 << 32, 8), lambda: rgd.sample_truncated_workspace_bytes(1, 1 << 33),
                lambda: rgd.Rotary((1 << 32) + 64, 1e4)):
