@@ -35,6 +35,12 @@ struct PagedAttnArgs {
   float* ws;
   int G;           // query heads per KV head
   unsigned inv_G;  // ceil(2^31 / G)
+  // by a plan: the groups' parts
+  int* plan;
+  void* at;                   // [S + 1]: where a group's units and items begin; units of a run
+  float* slots;               // of run r and item i: r + i
+  int s_cols, s_cost, s_step; // query vectors of a slot, units of an item besides its steps, positions of a step
+  int most;                   // tokens of a sequence: n, or 0 where the plan is not this call's
 };
 bool paged_attention_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq);
@@ -73,6 +79,7 @@ size_t paged_share_ints(const PagedView& c, int n);
 hipError_t paged_share(const ShareArgs& a, hipStream_t s);
 // a.n_new is taken from the plan
 hipError_t paged_attention_shared(const PagedAttnArgs& a, const int* plan, hipStream_t s);
+bool paged_attention_shared_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq);
 
 struct TruncateArgs {

@@ -38,6 +38,8 @@
 #include <type_traits>
 
 #include "paged.hpp"
+#include "paged_tiles.hpp"
+#include "share.hpp"
 
 namespace rgd {
 
@@ -55,13 +57,9 @@ constexpr int item_cost(int nt) { return 4 * nt; }
 // 131072 takes 162 us in place of 109.
 constexpr int kMaxRuns = 512;
 constexpr int kWaves = 4;      // per workgroup
-constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLazy = 8.f;       // the running maximum moves when a score passes it by this (log2 units)
-constexpr float kLift = 256.f;     // 2^kLazy: weights are held divided by it, so none is above 1 and no sum above that of |V|
-constexpr float kNoRef = -3.0e38f; // the maximum before any visible score: finite, so a masked one gives 0, never NaN
-
-RGD_DEV int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+// What a kernel attends to: whole sequences; by a plan, what groups of sequences share, each group a sequence of the
+// tokens of all its members; or what is left of the sequences behind that, whose parts are joined with the shared ones.
+enum Mode { WHOLE, SHARED, OWN };
 
 // New tokens of sequence s.
 RGD_DEV int new_tokens(const PagedAttnArgs& a, int s) { return a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n; }
@@ -72,62 +70,62 @@ RGD_DEV int token_of(const PagedAttnArgs& a, int col) { return (int)__umulhi((un
 
 struct Seq {
   int len, m;   // positions, new tokens
+  int from;     // first position of the steps: a multiple of 16
   int steps;    // per item; at least one, so that tokens that see nothing get their zeros
   int tiles;    // query tiles; 0 without new tokens.  Items: KV heads x query tiles
 };
 
 template <int COLS>
-RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m) {
+RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m, int from) {
   Seq q;
   q.len = len;
   q.m = m;
-  q.steps = max(1, (len + kStep - 1) / kStep);
+  q.from = from;
+  q.steps = max(1, (len - from + kStep - 1) / kStep);
   q.tiles = (m * a.G + COLS - 1) / COLS;
   return q;
 }
-template <int COLS>
+template <int COLS, int MODE>
 RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
-  return seq_of<COLS>(a, paged_len(a.c, s), new_tokens(a, s));
+  if constexpr (MODE == WHOLE) {
+    return seq_of<COLS>(a, paged_len(a.c, s), new_tokens(a, s), 0);
+  } else {
+    const Plan p(a.plan, a.c.S);
+    if constexpr (MODE == SHARED) {
+      const PlanGroup g = p.group[s];
+      return seq_of<COLS>(a, g.shared, a.most ? g.tokens : 0, 0);
+    } else {
+      const int len = paged_len(a.c, s);
+      return seq_of<COLS>(a, len, min(p.tokens[s], a.most), min(p.shared[s], len / 16 * 16));
+    }
+  }
 }
 // The same for an s that the whole wave shares, by scalar loads: a vector load's wait would be one
 // for the K and V on their way, too.
-template <int COLS>
+template <int COLS, int MODE>
 RGD_DEV Seq uniform_seq(const PagedAttnArgs& a, int s) {
   typedef const int __attribute__((address_space(4))) * Scalar;
-  const int len = ((Scalar)a.c.lens)[s], m = a.n_new ? ((Scalar)a.n_new)[s] : a.n;
-  return seq_of<COLS>(a, min(max(len, 0), a.c.width * a.c.ps), min(max(m, 0), a.n));
-}
-
-// Sum over the lanes up to this one (64-bit: long tables times many sequences).
-template <int CTRL, int ROWS>
-RGD_DEV long long scan_step(long long v) {
-  const int lo = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
-  const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
-  return v + (((long long)hi << 32) | (unsigned)lo);
-}
-RGD_DEV long long wave_scan(long long v) {
-  v = scan_step<0x111, 0xf>(v);  // row_shr:1
-  v = scan_step<0x112, 0xf>(v);
-  v = scan_step<0x114, 0xf>(v);
-  v = scan_step<0x118, 0xf>(v);
-  v = scan_step<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
-  return scan_step<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
-}
-RGD_DEV long long lane_value(long long v, int lane) {
-  const int lo = __builtin_amdgcn_readlane((int)v, lane), hi = __builtin_amdgcn_readlane((int)(v >> 32), lane);
-  return ((long long)hi << 32) | (unsigned)lo;
+  if constexpr (MODE == WHOLE) {
+    const int len = ((Scalar)a.c.lens)[s], m = a.n_new ? ((Scalar)a.n_new)[s] : a.n;
+    return seq_of<COLS>(a, min(max(len, 0), a.c.width * a.c.ps), min(max(m, 0), a.n), 0);
+  } else {
+    const Plan p(a.plan, a.c.S);
+    if constexpr (MODE == SHARED) {
+      Scalar g = (Scalar)p.group + 4 * s;
+      return seq_of<COLS>(a, g[0], a.most ? g[1] : 0, 0);
+    } else {
+      const int len = min(max(((Scalar)a.c.lens)[s], 0), a.c.width * a.c.ps);
+      return seq_of<COLS>(a, len, min(((Scalar)p.tokens)[s], a.most), min(((Scalar)p.shared)[s], len / 16 * 16));
+    }
+  }
 }
 
 // Units of the plan that this lane's sequence takes (none behind the last).
-template <int COLS>
+template <int COLS, int MODE>
 RGD_DEV long long units_of(const PagedAttnArgs& a, int s, Seq& q) {
-  q = seq_of<COLS>(a, min(s, a.c.S - 1));
+  q = seq_of<COLS, MODE>(a, min(s, a.c.S - 1));
   return s < a.c.S ? (long long)(q.steps + item_cost(COLS / 16)) * (a.c.Hkv * q.tiles) : 0;
 }
-
-// Floor of x / y for 0 <= x < 2^52, 0 < y.  Exact: a quotient that is no whole number
-// is at least 1 / y, more than 2^-52 of itself, away from the next one.
-RGD_DEV long long quotient(long long x, long long y) { return (long long)((double)x / (double)y); }
 
 struct Runs {
   long long total, length;  // units of the plan, units per run
@@ -135,13 +133,13 @@ struct Runs {
 
 // Finds the run of workgroup r (of `runs`): the sequence it starts in and the units
 // before that one.  False: there is none.
-template <int COLS>
+template <int COLS, int MODE>
 RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& s, Seq& sq, long long& before) {
   const int lane = threadIdx.x & 63, per = (a.c.S + 63) / 64;  // sequences a lane: one, or neighbouring ones
   Seq q;
   long long u = 0;
 #pragma unroll 8
-  for (int k = 0; k < per; ++k) u += units_of<COLS>(a, lane * per + k, q);
+  for (int k = 0; k < per; ++k) u += units_of<COLS, MODE>(a, lane * per + k, q);
   long long incl = wave_scan(u);
   plan.total = lane_value(incl, 63);
   plan.length = max((long long)kMinSteps, quotient(plan.total + runs - 1, runs));
@@ -152,7 +150,7 @@ RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& 
   s = l * per;
   if (per > 1)
     for (;; s += 64) {
-      u = units_of<COLS>(a, s + lane, q);
+      u = units_of<COLS, MODE>(a, s + lane, q);
       incl = wave_scan(u);
       if (const unsigned long long hit = __ballot(before + incl > start)) {
         l = __builtin_ctzll(hit);
@@ -162,16 +160,10 @@ RGD_DEV bool find_run(const PagedAttnArgs& a, int r, int runs, Runs& plan, int& 
       }
       before += lane_value(incl, 63);
     }
-  sq = seq_of<COLS>(a, __builtin_amdgcn_readlane(q.len, l), __builtin_amdgcn_readlane(q.m, l));
+  sq = seq_of<COLS>(a, __builtin_amdgcn_readlane(q.len, l), __builtin_amdgcn_readlane(q.m, l),
+                    MODE == OWN ? __builtin_amdgcn_readlane(q.from, l) : 0);
   return true;
 }
-
-RGD_DEV f32x4 mfma_bf16(const u32x4& x, const u32x4& y, f32x4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
-}
-RGD_DEV f32x4 mfma_f32(float x, float y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0); }
-
-RGD_DEV float exp2_raw(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // The first n of the values packed in v (bf16 pairs or floats), zeros behind.
 template <typename T>
@@ -230,62 +222,43 @@ RGD_DEV bool any_nonfinite(u32x4 v) {
   return bad;
 }
 
-// Looks up a sequence's table by 16-position blocks in rising order, two times 64
-// entries in registers.
-struct TableWalk {
-  const int* row;
-  int width, bpp;  // 16-position blocks per page
-  unsigned long long inv;
-  int jb, cur, nxt, lane;
-  RGD_DEV int page_index(int block) const { return (int)(((unsigned long long)block * inv) >> 36); }
-  RGD_DEV void start(const PagedView& c, int s, int block) {
-    row = c.pages + (size_t)s * c.width;
-    width = c.width;
-    bpp = c.ps >> 4;
-    inv = ((1ull << 36) + bpp - 1) / bpp;  // blocks are below 2^26, bpp at most 2^8: exact
-    lane = threadIdx.x & 63;
-    jb = page_index(block);
-    cur = row[min(jb + lane, width - 1)];
-    nxt = row[min(jb + 64 + lane, width - 1)];
-  }
-  // the page of a block (behind the table: any value) and the block's place in it
-  RGD_DEV int find(int block, int& place) {
-    const int j = page_index(block);
-    place = block - j * bpp;
-    while (j - jb >= 64) {
-      cur = nxt;
-      jb += 64;
-      nxt = row[min(jb + 64 + lane, width - 1)];
-    }
-    return __builtin_amdgcn_readlane(cur, j - jb);
-  }
-};
-
 // One item of a run: steps [t0, t1) of query tile qb of KV head g of sequence s.
 struct Item {
   Seq sq;
   int s, g, qb, t0, t1;
+  int row;     // SHARED: of its tokens in the plan's list
+  int number;  // SHARED: among all items
   bool valid;
   long long at;  // its first unit in the plan
-  RGD_DEV int end() const { return min(t1 * kStep, max(sq.len, 1)); }
-  RGD_DEV int begin(int wave, int per) const { return t0 * kStep + wave * per; }
+  RGD_DEV int end() const { return min(sq.from + t1 * kStep, max(sq.len, sq.from + 1)); }
+  RGD_DEV int begin(int wave, int per) const { return sq.from + t0 * kStep + wave * per; }
 };
 
-RGD_DEV Seq uniform(const Seq& q) { return Seq{uniform(q.len), uniform(q.m), uniform(q.steps), uniform(q.tiles)}; }
+RGD_DEV Seq same_for_all(const Seq& q) {
+  return Seq{uniform(q.len), uniform(q.m), uniform(q.from), uniform(q.steps), uniform(q.tiles)};
+}
+
+// The token row of an item's token i: its q, and its outputs.
+template <int MODE>
+RGD_DEV size_t row_of(const PagedAttnArgs& a, const Item& it, int i) {
+  if constexpr (MODE == SHARED) return Plan(a.plan, a.c.S).rows[it.row + i];
+  else return (size_t)it.s * a.n + i;
+}
 
 // The items of a run, one after the other.
-template <int COLS>
+template <int COLS, int MODE>
 struct Walk {
   static constexpr int COST = item_cost(COLS / 16);
   Seq sq;
   int s, g, qb, u0, left;
+  int number;
   long long at;
   RGD_DEV Item next(const PagedAttnArgs& a) {
     Item it{};
     if (left <= 0) return it;
     if (g == a.c.Hkv) {  // steps are left, so a sequence with new tokens follows
       g = 0;
-      do sq = uniform_seq<COLS>(a, ++s);
+      do sq = uniform_seq<COLS, MODE>(a, ++s);
       while (sq.tiles == 0);
     }
     // an item's first COST units of the plan are its fixed cost, in front of its steps
@@ -297,6 +270,11 @@ struct Walk {
     it.t0 = max(0, u0 - COST);
     it.t1 = u1 - COST;
     it.valid = it.t1 > it.t0;  // else the next run has the item's first step
+    if constexpr (MODE == SHARED) {
+      typedef const int __attribute__((address_space(4))) * Scalar;
+      it.row = ((Scalar)Plan(a.plan, a.c.S).group)[4 * s + 2];
+      it.number = number++;
+    }
     it.at = at;
     at += sq.steps + COST;
     left -= u1 - u0;
@@ -310,7 +288,7 @@ struct Walk {
 };
 
 // D dimensions, NT tiles of 16 query vectors; PAST: V is loaded past the caches.
-template <typename T, int D, int NT, bool PAST>
+template <typename T, int D, int NT, bool PAST, int MODE>
 struct Piece {
   static constexpr bool BF = sizeof(T) == 2;
   static constexpr int NB = BF ? 2 : 1;             // 16-position blocks per round
@@ -460,7 +438,7 @@ struct Piece {
   RGD_DEV void stage_q(const PagedAttnArgs& a, const Item& it, u32x4* dst, int wave) const {
     const int G = a.G, cols = it.sq.m * G;
     const int col = min(it.qb * COLS + wave * 16 + row, cols - 1), i = token_of(a, col);
-    const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
+    const T* src = (const T*)a.q + row_of<MODE>(a, it, i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
     for (int c = 0; c < KL; ++c) dst[(wave * KL + c) * 64 + lane] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
   }
@@ -471,7 +449,7 @@ struct Piece {
 #pragma unroll
     for (int t = 0; t < (QS ? 0 : NT); ++t) {
       const int col = min(it.qb * COLS + t * 16 + row, cols - 1), i = token_of(a, col);  // columns behind the last one repeat it
-      const T* src = (const T*)a.q + ((size_t)it.s * a.n + i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
+      const T* src = (const T*)a.q + row_of<MODE>(a, it, i) * a.ldq + (size_t)(it.g * G + col - i * G) * D;
 #pragma unroll
       for (int c = 0; c < KL; ++c) q[t][c] = *(const u32x4*)((const char*)src + c * 64 + grp * 16);
     }
@@ -496,13 +474,13 @@ struct Piece {
     int lim[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      lim[t] = sq.len - sq.m + token_of(a, min(qb * COLS + t * 16 + row, cols - 1)) + 1;
+      lim[t] = MODE == SHARED ? sq.len : sq.len - sq.m + token_of(a, min(qb * COLS + t * 16 + row, cols - 1)) + 1;
       m[t] = kNoRef;
       l[t] = 0.f;
 #pragma unroll
       for (int d = 0; d < VL; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = sq.len - sq.m + token_of(a, qb * COLS) + 1;  // all of the tile's tokens see that much
+    const int least = MODE == SHARED ? sq.len : sq.len - sq.m + token_of(a, qb * COLS) + 1;  // all of the tile's tokens see that much
     const float scale = kLog2e / sqrtf((float)D);
     if (p0 >= p1) {
       start(a, next, walk_next, wave);
@@ -600,8 +578,6 @@ struct Piece {
   }
 };
 
-RGD_DEV float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l * kLift)) * kLn2; }
-
 template <typename T>
 RGD_DEV void store_row4(T* p, f32x4 v) {
   if constexpr (sizeof(T) == 2) *(u32x2*)p = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -625,9 +601,74 @@ constexpr size_t slot_floats() {
 // Whether a CU holds two workgroups (row: bytes of a row of K).
 constexpr bool two_per_cu(int nt, size_t row) { return nt == 1 || (nt == 2 && row < 512); }
 
-template <typename T, int D, int NT, bool PAST>
+// The parts of a sequence's shared positions, as the kernel before left them, joined with (top, sum, o) of a query vector of
+// token i; four dimensions from d on.
+struct SharedParts {
+  const float* slots;
+  long long length, unit;  // of a run; the group's first
+  int col, tiles, steps, item, cols, cost, D;
+  RGD_DEV SharedParts(const PagedAttnArgs& a, int s) {
+    const Plan p(a.plan, a.c.S);
+    const int leader = p.leader[s], shared = leader < 0 ? 0 : p.shared[s];
+    steps = (shared + a.s_step - 1) / a.s_step;
+    if (!steps) return;
+    const PlanGroup g = p.group[leader];
+    const GroupAt at = ((const GroupAt*)a.at)[leader];
+    length = ((const GroupAt*)a.at)[a.c.S].unit;
+    unit = at.unit;
+    item = at.item;
+    col = (p.row[s] - g.row) * a.G;
+    cols = a.s_cols;
+    cost = a.s_cost;
+    tiles = (g.tokens * a.G + cols - 1) / cols;
+    slots = a.slots;
+    D = a.c.D;
+  }
+  // the query vector of KV head g that is `v` (token * G + head) among the sequence's
+  RGD_DEV void join(int g, int v, int d, float& top, float& sum, f32x4& o) const {
+    if (!steps) return;
+    const int qb = (col + v) / cols, c = col + v - qb * cols, k = g * tiles + qb;
+    const long long u = unit + (long long)k * (steps + cost) + cost;
+    const int r0 = (int)quotient(u, length), r1 = (int)quotient(u + steps - 1, length);
+    const size_t size = (size_t)cols * (D + 2);
+    const float* slot = slots + (size_t)(r0 + item + k) * size;
+#pragma unroll 4
+    for (int r = r0; r <= r1; ++r, slot += size) {
+      const float2 ml = *(const float2*)(slot + cols * D + 2 * c);
+      const f32x4 x = *(const f32x4*)(slot + c * D + d);
+      const float nt = fmaxf(top, ml.x), down = exp2_raw(top - nt), f = exp2_raw(ml.x - nt);
+      o = o * down + f * x;
+      sum = sum * down + f * ml.y;
+      top = nt;
+    }
+  }
+};
+
+// Where each group's units and items begin, for the kernels that join; one wave.
+template <int COLS>
+RGD_DEV void list_groups(const PagedAttnArgs& a, long long length) {
+  const int lane = threadIdx.x & 63;
+  GroupAt* at = (GroupAt*)a.at;
+  long long units = 0, items = 0;
+  for (int s0 = 0; s0 < a.c.S; s0 += 64) {
+    Seq q;
+    const long long u = units_of<COLS, SHARED>(a, s0 + lane, q), n = s0 + lane < a.c.S ? a.c.Hkv * q.tiles : 0;
+    const long long ui = wave_scan(u), ni = wave_scan(n);
+    if (s0 + lane < a.c.S) at[s0 + lane] = GroupAt{units + ui - u, (int)(items + ni - n), 0};
+    units += lane_value(ui, 63);
+    items += lane_value(ni, 63);
+  }
+  if (lane == 0) at[a.c.S] = GroupAt{length, 0, 0};
+}
+
+template <int MODE>
+RGD_DEV void check_plan(PagedAttnArgs& a) {
+  if constexpr (MODE != WHOLE) a.most = *Plan(a.plan, a.c.S).head == PlanHead::of(a.c, a.n, a.Hq) ? a.n : 0;
+}
+
+template <typename T, int D, int NT, bool PAST, int MODE>
 __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
-  using P = Piece<T, D, NT, PAST>;
+  using P = Piece<T, D, NT, PAST, MODE>;
   constexpr int COLS = P::COLS, LD = D + 4, COST = item_cost(NT);
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
@@ -637,19 +678,34 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
   Runs plan;
   int s;
   long long before;
-  Walk<COLS> walk;
+  Walk<COLS, MODE> walk;
   Cut* cut = (Cut*)a.ws + r;
-  if (threadIdx.x == 0) *cut = Cut{-1, 0, 0, 0};
-  if (!find_run<COLS>(a, r, runs, plan, s, walk.sq, before)) return;
+  check_plan<MODE>(a);
+  if (MODE != SHARED && threadIdx.x == 0) *cut = Cut{-1, 0, 0, 0};
+  const bool found = find_run<COLS, MODE>(a, min(r, runs - 1), runs, plan, s, walk.sq, before);
+  if constexpr (MODE == SHARED)
+    if (r == runs) {  // a workgroup beside the runs'
+      if (wave == 0) list_groups<COLS>(a, plan.length);
+      return;
+    }
+  if (!found) return;
   const long long start = r * plan.length;
   walk.s = uniform(s);
   walk.left = uniform((int)min(plan.length, plan.total - start));
-  walk.sq = uniform(walk.sq);
+  walk.sq = same_for_all(walk.sq);
   const int item = uniform((int)quotient(start - before, walk.sq.steps + COST));
   walk.g = item / walk.sq.tiles;
   walk.qb = item - walk.g * walk.sq.tiles;
   walk.at = before + (long long)item * (walk.sq.steps + COST);
   walk.u0 = uniform((int)(start - walk.at));
+  if constexpr (MODE == SHARED) {
+    long long ahead = 0;
+    for (int s0 = 0; s0 < walk.s; s0 += 64) {
+      const Seq q = seq_of<COLS, MODE>(a, min(s0 + lane, a.c.S - 1));
+      ahead += lane_value(wave_scan(s0 + lane < walk.s ? a.c.Hkv * q.tiles : 0), 63);
+    }
+    walk.number = uniform((int)ahead + item);
+  }
   const int G = a.G;
   P x;
   x.lane = lane;
@@ -679,10 +735,11 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
         if (grp == 0) ml[wave][t * 16 + row] = float2{x.m[t], x.l[t]};
       }
     __syncthreads();
-    const bool done = t0 == 0 && t1 == sq.steps;
-    if (t0 == 0 && !done && threadIdx.x == 0)
+    const bool done = MODE != SHARED && t0 == 0 && t1 == sq.steps;
+    if (MODE != SHARED && t0 == 0 && !done && threadIdx.x == 0)
       *cut = Cut{s, g, qb, (short)quotient(it.at + COST + sq.steps - 1, plan.length), (short)cols};
     float* slot = a.ws + cut_floats(runs) + (size_t)(2 * r + (t0 == 0)) * slot_floats<D, NT>();
+    if constexpr (MODE == SHARED) slot = a.slots + (size_t)(r + it.number) * slot_floats<D, NT>();
     for (int i = threadIdx.x; i < cols * (D / 4); i += 256) {
       const int c = i / (D / 4), d = i % (D / 4) * 4, col = qb * COLS + c;
       float top = ml[0][c].x, sum = 0.f;
@@ -698,6 +755,7 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
           o += f * *(const f32x4*)&part[w][c][d];
         }
       if (done) {
+        if constexpr (MODE == OWN) SharedParts(a, s).join(g, col, d, top, sum, o);
         const int i = token_of(a, col), h = g * G + col - i * G;
         const size_t row_out = (size_t)s * a.n + i;
         store_row4((T*)a.out + (row_out * a.Hq + h) * D + d, o * (sum == 0.f ? 0.f : 1.f / sum));
@@ -720,7 +778,7 @@ constexpr int join_cols(int nt) { return nt == 1 ? 1 : 8; }
 // The outputs of the items that several runs share, by the run that an item starts
 // in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.  2.8 to 5.7 us: a launch and
 // one round trip, two where an item has more pieces than fit the threads (1 to 5 MB, which lie in the caches).
-template <typename T, int D, int NT>
+template <typename T, int D, int NT, int MODE>
 __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
   constexpr int COLS = 16 * NT, W = D / 4, CB = join_cols(NT), PARTS = 256 / W / CB;
   __shared__ f32x4 acc_s[CB][PARTS][W];
@@ -770,6 +828,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int run
       sum += f * ml_s[k][i].y;
     }
   }
+  if constexpr (MODE == OWN) SharedParts(a, cut.s).join(cut.g, col, 4 * d, top, sum, acc);
   const int i = token_of(a, col);
   const size_t at = ((size_t)cut.s * a.n + i) * a.Hq + cut.g * G + col - i * G;
   store_row4((T*)a.out + at * D + 4 * d, acc * (sum == 0.f ? 0.f : 1.f / sum));
@@ -794,41 +853,64 @@ int runs_for(const PagedView& c, int vectors) {
   return (int)std::min(most, std::ceil((steps + item_cost(nt) * items) / kMinSteps));
 }
 
-template <typename T, int D, int NT>
-hipError_t launch(const PagedAttnArgs& a, hipStream_t s) {
-  const int runs = runs_for(a.c, a.n * a.G);
+template <typename T, int D, int NT, int MODE>
+hipError_t launch(const PagedAttnArgs& a, int vectors, hipStream_t s) {
+  const int runs = runs_for(a.c, vectors), extra = MODE == SHARED;
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
   // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
-  if (a.c.ps <= Piece<T, D, NT, true>::PER)
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true>), dim3(runs), dim3(256), 0, s, a, runs);
+  if (MODE != SHARED && a.c.ps <= Piece<T, D, NT, true, MODE>::PER)
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs), dim3(256), 0, s, a, runs);
   else
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false>), dim3(runs), dim3(256), 0, s, a, runs);
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false, MODE>), dim3(runs + extra), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
+  if (MODE == SHARED) return hipSuccess;
   const int cols = std::min(16 * NT, a.n * a.G);
   const dim3 grid(runs, (cols + join_cols(NT) - 1) / join_cols(NT));
-  hipLaunchKernelGGL((attn_join_kernel<T, D, NT>), grid, dim3(256), 0, s, a, runs);
+  hipLaunchKernelGGL((attn_join_kernel<T, D, NT, MODE>), grid, dim3(256), 0, s, a, runs);
   return hipGetLastError();
 }
 
-template <typename T, int D>
-hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
-  switch (tiles_for(a.c, a.n * a.G)) {
-    case 1: return launch<T, D, 1>(a, s);
-    case 2: return launch<T, D, 2>(a, s);
+template <int MODE, typename T, int D>
+hipError_t launch_tiles(const PagedAttnArgs& a, int vectors, hipStream_t s) {
+  switch (tiles_for(a.c, vectors)) {
+    case 1: return launch<T, D, 1, MODE>(a, vectors, s);
+    case 2: return launch<T, D, 2, MODE>(a, vectors, s);
   }
-  if constexpr (sizeof(T) == 2 || D < 128) return launch<T, D, 4>(a, s);
+  if constexpr (sizeof(T) == 2 || D < 128) return launch<T, D, 4, MODE>(a, vectors, s);
   return hipErrorInvalidValue;
 }
 
-template <typename T>
-hipError_t launch_dim(const PagedAttnArgs& a, hipStream_t s) {
+template <int MODE, typename T>
+hipError_t launch_dim(const PagedAttnArgs& a, int vectors, hipStream_t s) {
   switch (a.c.D) {
-    case 32: return launch_tiles<T, 32>(a, s);
-    case 64: return launch_tiles<T, 64>(a, s);
-    default: return launch_tiles<T, 128>(a, s);
+    case 32: return launch_tiles<MODE, T, 32>(a, vectors, s);
+    case 64: return launch_tiles<MODE, T, 64>(a, vectors, s);
+    default: return launch_tiles<MODE, T, 128>(a, vectors, s);
   }
 }
+
+template <int MODE>
+hipError_t launch_type(const PagedAttnArgs& a, int vectors, hipStream_t s) {
+  return a.c.esz == 2 ? launch_dim<MODE, bf16_t>(a, vectors, s) : launch_dim<MODE, float>(a, vectors, s);
+}
+
+PagedAttnArgs with_groups(const PagedAttnArgs& a0) {
+  PagedAttnArgs a = a0;
+  a.G = a.Hq / a.c.Hkv;
+  a.inv_G = (unsigned)(((1ull << 31) + a.G - 1) / a.G);
+  return a;
+}
+
+// Most query vectors per KV head of a call's groups.
+int group_vectors(const PagedView& c, int n, int Hq) { return c.S * n * (Hq / c.Hkv); }  // at most 2^22
+
+// Items of the groups at most: full tiles, and one more for each group (of two sequences or more).
+size_t group_items(const PagedView& c, int vectors, int cols) {
+  return (size_t)c.Hkv * ((size_t)vectors / cols + (c.S + 1) / 2 + 1);
+}
+
+size_t at_floats(const PagedView& c) { return ((size_t)(c.S + 1) * 4 + 63) / 64 * 64; }
 
 }  // namespace
 
@@ -851,11 +933,34 @@ size_t paged_attention_workspace_floats(const PagedView& c, int n, int Hq) {
   return most;
 }
 
-hipError_t paged_attention(const PagedAttnArgs& a0, hipStream_t s) {
-  PagedAttnArgs a = a0;
-  a.G = a.Hq / a.c.Hkv;
-  a.inv_G = (unsigned)(((1ull << 31) + a.G - 1) / a.G);
-  return a.c.esz == 2 ? launch_dim<bf16_t>(a, s) : launch_dim<float>(a, s);
+hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s) {
+  return launch_type<WHOLE>(with_groups(a), a.n * (a.Hq / a.c.Hkv), s);
+}
+
+bool paged_attention_shared_fits(const PagedView& c, int n, int Hq) {
+  const int vectors = group_vectors(c, n, Hq), nt = tiles_for(c, vectors);
+  const double units = (double)group_items(c, vectors, 16 * nt) * (std::ceil((double)c.width * c.ps / kStep) + item_cost(nt));
+  return paged_attention_fits(c, n, Hq) && units < 274877906944.0;
+}
+
+size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq) {
+  const int vectors = group_vectors(c, n, Hq), cols = 16 * tiles_for(c, vectors);
+  return at_floats(c) + (runs_for(c, vectors) + group_items(c, vectors, cols)) * cols * (c.D + 2) +
+         paged_attention_workspace_floats(c, n, Hq);
+}
+
+hipError_t paged_attention_shared(const PagedAttnArgs& a0, const int* plan, hipStream_t s) {
+  PagedAttnArgs a = with_groups(a0);
+  const int vectors = group_vectors(a.c, a.n, a.Hq), nt = tiles_for(a.c, vectors);
+  a.plan = (int*)plan;
+  a.at = a.ws;
+  a.slots = a.ws + at_floats(a.c);
+  a.s_cols = 16 * nt;
+  a.s_cost = item_cost(nt);
+  a.s_step = kStep;
+  a.ws = a.slots + (runs_for(a.c, vectors) + group_items(a.c, vectors, a.s_cols)) * a.s_cols * (a.c.D + 2);
+  if (hipError_t e = launch_type<SHARED>(a, vectors, s)) return e;
+  return launch_type<OWN>(a, a.n * a.G, s);
 }
 
 }  // namespace rgd

@@ -109,14 +109,6 @@ __global__ __launch_bounds__(256) void share_groups_kernel(ShareArgs a, Plan p) 
       }
 }
 
-// The plan's counts; none where it was made for something else.
-__global__ __launch_bounds__(256) void share_counts_kernel(PagedAttnArgs a, Plan p, int* counts) {
-  const int s = blockIdx.x * 256 + threadIdx.x;
-  if (s < a.c.S) counts[s] = *p.head == PlanHead::of(a.c, a.n, a.Hq) ? p.tokens[s] : 0;
-}
-
-size_t counts_floats(const PagedView& c) { return ((size_t)c.S + 63) / 64 * 64; }
-
 }  // namespace
 
 size_t paged_share_ints(const PagedView& c, int n) { return Plan::ints(c.S, n); }
@@ -126,19 +118,6 @@ hipError_t paged_share(const ShareArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(share_find_kernel, dim3(a.c.S), dim3(256), 0, s, a, p);
   hipLaunchKernelGGL(share_groups_kernel, dim3(a.c.S), dim3(256), 0, s, a, p);
   return hipGetLastError();
-}
-
-size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq) {
-  return counts_floats(c) + paged_attention_workspace_floats(c, n, Hq);
-}
-
-hipError_t paged_attention_shared(const PagedAttnArgs& a0, const int* plan, hipStream_t s) {
-  PagedAttnArgs a = a0;
-  int* counts = (int*)a.ws;
-  hipLaunchKernelGGL(share_counts_kernel, dim3((a.c.S + 255) / 256), dim3(256), 0, s, a, Plan((int*)plan, a.c.S), counts);
-  a.n_new = counts;
-  a.ws += counts_floats(a.c);
-  return paged_attention(a, s);
 }
 
 }  // namespace rgd

@@ -24,6 +24,11 @@ struct PlanGroup {
   int unused;
 };
 
+struct GroupAt {
+  long long unit;
+  int item, unused;
+};
+
 struct Plan {
   PlanHead* head;
   PlanGroup* group;  // [S]
