@@ -24,6 +24,7 @@
 // were no faster.
 #include <algorithm>
 
+#include "dma.hpp"
 #include "gemm_common.hpp"
 #include "kernels.hpp"
 
@@ -34,19 +35,6 @@ namespace {
 constexpr int kBM = 256, kBN = 128;  // rows and columns of a workgroup's tile
 constexpr int kXBytes = kBM * kStep * 2;  // X of one 64-k step in LDS
 
-// 1 KiB from global memory to LDS, 16 bytes a lane: base + off (per lane) +
-// OFF to lds + DST + OFF + 16 * lane.  No register is written; the compiler does not count it.
-// (m0 is reserved: the compiler never holds a value there across statements, which
-// its warning is about, but orders its own uses of m0 by the clobber.)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-template <int DST, int OFF>
-RGD_DEV void dma16(const char* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 offset:%4" ::"v"(off), "s"(base),
-               "s"(lds), "n"(DST), "n"(OFF)
-               : "m0", "scc");
-}
-#pragma clang diagnostic pop
 template <int A, int B, typename F>
 RGD_DEV void static_for(F&& f) {
   if constexpr (A < B) {
@@ -54,11 +42,6 @@ RGD_DEV void static_for(F&& f) {
     static_for<A + 1, B>(f);
   }
 }
-template <int N>
-RGD_DEV void dma_wait_barrier() {
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
-}
-
 RGD_DEV f32x16 mfma32x32x16(const u32x4& a, const u32x4& b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }

@@ -79,6 +79,12 @@ size_t paged_share_ints(const PagedView& c, int n);
 hipError_t paged_share(const ShareArgs& a, hipStream_t s);
 // a.n_new is taken from the plan
 hipError_t paged_attention_shared(const PagedAttnArgs& a, const int* plan, hipStream_t s);
+// How the groups' part is cut: query vectors of an item, units of one besides its steps, positions of a step, runs.
+struct GroupShape {
+  int cols, cost, step, runs;
+};
+GroupShape group_shape(const PagedView& c, int vectors);
+hipError_t paged_group(const PagedAttnArgs& a, int runs, hipStream_t s);  // bf16
 bool paged_attention_shared_fits(const PagedView& c, int n, int Hq);
 size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq);
 

@@ -910,6 +910,11 @@ size_t group_items(const PagedView& c, int vectors, int cols) {
   return (size_t)c.Hkv * ((size_t)vectors / cols + (c.S + 1) / 2 + 1);
 }
 
+// One slot for each run that enters or leaves an item (of run r and item i: r + i).
+size_t slots_floats(const PagedView& c, int vectors, const GroupShape& g) {
+  return (g.runs + group_items(c, vectors, g.cols)) * g.cols * (c.D + 2);
+}
+
 size_t at_floats(const PagedView& c) { return ((size_t)(c.S + 1) * 4 + 63) / 64 * 64; }
 
 }  // namespace
@@ -937,29 +942,37 @@ hipError_t paged_attention(const PagedAttnArgs& a, hipStream_t s) {
   return launch_type<WHOLE>(with_groups(a), a.n * (a.Hq / a.c.Hkv), s);
 }
 
+static GroupShape shape_of(const PagedView& c, int vectors) {
+  if (c.esz == 2) return group_shape(c, vectors);
+  const int nt = tiles_for(c, vectors);
+  return GroupShape{16 * nt, item_cost(nt), kStep, runs_for(c, vectors)};
+}
+
 bool paged_attention_shared_fits(const PagedView& c, int n, int Hq) {
-  const int vectors = group_vectors(c, n, Hq), nt = tiles_for(c, vectors);
-  const double units = (double)group_items(c, vectors, 16 * nt) * (std::ceil((double)c.width * c.ps / kStep) + item_cost(nt));
+  const int vectors = group_vectors(c, n, Hq);
+  const GroupShape g = shape_of(c, vectors);
+  const double units = (double)group_items(c, vectors, g.cols) * (std::ceil((double)c.width * c.ps / g.step) + g.cost);
   return paged_attention_fits(c, n, Hq) && units < 274877906944.0;
 }
 
 size_t paged_attention_shared_workspace_floats(const PagedView& c, int n, int Hq) {
-  const int vectors = group_vectors(c, n, Hq), cols = 16 * tiles_for(c, vectors);
-  return at_floats(c) + (runs_for(c, vectors) + group_items(c, vectors, cols)) * cols * (c.D + 2) +
-         paged_attention_workspace_floats(c, n, Hq);
+  const int vectors = group_vectors(c, n, Hq);
+  const GroupShape g = shape_of(c, vectors);
+  return at_floats(c) + slots_floats(c, vectors, g) + paged_attention_workspace_floats(c, n, Hq);
 }
 
 hipError_t paged_attention_shared(const PagedAttnArgs& a0, const int* plan, hipStream_t s) {
   PagedAttnArgs a = with_groups(a0);
-  const int vectors = group_vectors(a.c, a.n, a.Hq), nt = tiles_for(a.c, vectors);
+  const int vectors = group_vectors(a.c, a.n, a.Hq);
+  const GroupShape g = shape_of(a.c, vectors);
   a.plan = (int*)plan;
   a.at = a.ws;
   a.slots = a.ws + at_floats(a.c);
-  a.s_cols = 16 * nt;
-  a.s_cost = item_cost(nt);
-  a.s_step = kStep;
-  a.ws = a.slots + (runs_for(a.c, vectors) + group_items(a.c, vectors, a.s_cols)) * a.s_cols * (a.c.D + 2);
-  if (hipError_t e = launch_type<SHARED>(a, vectors, s)) return e;
+  a.s_cols = g.cols;
+  a.s_cost = g.cost;
+  a.s_step = g.step;
+  a.ws = a.slots + slots_floats(a.c, vectors, g);
+  if (hipError_t e = a.c.esz == 2 ? paged_group(a, g.runs, s) : launch_dim<SHARED, float>(a, vectors, s)) return e;
   return launch_type<OWN>(a, a.n * a.G, s);
 }
 

@@ -140,6 +140,8 @@ const char* rotary_ok(const rgd_rotary* r, int D) {
 const char* shared_ok(const PagedView& v, int32_t n, int32_t n_heads) {
   if (const char* why = heads_ok(v, n, n_heads)) return why;
   if ((int64_t)v.S * n * n_heads > (1 << 22)) return "max_seqs * n * n_heads must be at most 2^22";
+  if ((int64_t)v.S * n * (n_heads / v.Hkv) * (n_heads / v.Hkv) >= ((int64_t)1 << 31))  // what query vectors are divided with
+    return "max_seqs * n * (n_heads / n_kv_heads)^2 must be below 2^31";
   if (!paged_attention_shared_fits(v, n, n_heads)) return "tables too long for so many sequences and heads";
   return nullptr;
 }
