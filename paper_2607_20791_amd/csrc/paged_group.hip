@@ -216,6 +216,14 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
     }
   };
 
+  // the oldest step on its way is there (in each wave's order of copies)
+  auto arrive = [&] {
+    if (on_way >= 3) dma_wait_barrier<2 * LOADS>();
+    else if (on_way == 2) dma_wait_barrier<LOADS>();
+    else dma_wait_barrier<0>();
+    --on_way;
+  };
+
   Item it = walk.next(a);
   if (it.valid) {
     find_rows(it);
@@ -244,20 +252,11 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int c = 0; c < KL; ++c) asm volatile("" ::"v"(q[t][c]));
-    for (int step = it.t0; step < it.t1; ++step, buf = (buf + 1) % kRing) {
-      // the step is there (in each wave's order of copies), and every wave is done with the one before it
-      if (on_way >= 3) dma_wait_barrier<2 * LOADS>();
-      else if (on_way == 2) dma_wait_barrier<LOADS>();
-      else dma_wait_barrier<0>();
-      --on_way;
-      copy();
-      const int ok = uniform(ok_s[buf][2 * pg] | ok_s[buf][2 * pg + 1] << 1);  // this wave's two blocks
-      if (cg * 32 >= cols || !ok) continue;
-      const unsigned char* kt = lds + buf * BUF + pg * 2 * BLOCK;
-      const unsigned char* vt = kt + kBlocks * BLOCK;
-      // Products and weights of the two tiles take turns, so that the matrix units have the one's while the other's weights
-      // are worked out.
-      u32x4 k[2][KL], v[VL], hi[2], lo[2];
+    const bool works = cg * 32 < cols;
+    // the products of a step's keys with the wave's query vectors
+    auto scores = [&](int slot, f32x4 (&s)[2][2]) {
+      const unsigned char* kt = lds + slot * BUF + pg * 2 * BLOCK;
+      u32x4 k[2][KL];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         // row r of tile e: position (r >> 2) * 8 + e * 4 + (r & 3), so that a lane gets eight positions in a row
@@ -265,62 +264,99 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
 #pragma unroll
         for (int c = 0; c < KL; ++c) k[e][c] = *(const u32x4*)(kt + p * ROW + k_place<D>(p, c * 4 + grp) * 16);
       }
-      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) s[t][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < KL; ++c)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s[t][e] = mfma_bf16(k[e][c], q[t][c], s[t][e]);
+    };
+    f32x4 s[2][2];
+    arrive();
+    copy();
+    if (works) scores(buf, s);
+    for (int step = it.t0; step < it.t1; ++step) {
+      // The next step is there, and every wave is done with the one before this; the first step of an item has no place to give.
+      if (step + 1 < it.t1) arrive();
+      else if (step > it.t0) lds_barrier();
+      if (step > it.t0) copy();
+      const int here = buf;
+      buf = (buf + 1) % kRing;
+      if (!works) continue;
+      const int ok = uniform(ok_s[here][2 * pg] | ok_s[here][2 * pg + 1] << 1);  // this wave's two blocks
+      const bool there = ok >> (grp >> 1) & 1;
+      const unsigned char* vt = lds + here * BUF + pg * 2 * BLOCK + kBlocks * BLOCK;
+      u32x4 v[VL];
 #pragma unroll
       for (int d = 0; d < VL; ++d) {
         const int dim = d * 16 + row;
         v[d] = *(const u32x4*)(vt + (grp >> 1) * BLOCK + dim * 32 + v_place(dim, grp & 1) * 16);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      const bool there = ok >> (grp >> 1) & 1;
-      f32x4 s[2][2] = {};
+      float x[2][8];
+      bool moves = false;
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int c = 0; c < KL; ++c)
+        for (int j = 0; j < 8; ++j) x[t][j] = s[t][j / 4][j % 4];
+        if (ok != 3)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) s[t][e] = mfma_bf16(k[e][c], q[t][c], s[t][e]);
+          for (int j = 0; j < 8; ++j) x[t][j] = there ? x[t][j] : -INFINITY;
+      }
       if (ok != 3)  // what an earlier step left in place of a block may be NaN
 #pragma unroll
         for (int d = 0; d < VL; ++d) v[d] = there ? v[d] : u32x4{0, 0, 0, 0};
+      float top[2];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        float x[8], w[8];
+        const float* y = x[t];
+        top[t] = scale * fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
+        moves = moves || top[t] > m[t] + kLazy;
+      }
+      if (__any(moves))
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = s[t][j / 4][j % 4];
-        if (ok != 3)
-#pragma unroll
-          for (int j = 0; j < 8; ++j) x[j] = there ? x[j] : -INFINITY;
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        top *= scale;
-        if (__any(top > m[t] + kLazy)) {
-          top = fmaxf(top, __shfl_xor(top, 16, 64));
-          top = fmaxf(top, __shfl_xor(top, 32, 64));
-          const float nm = fmaxf(m[t], top), down = exp2_raw(m[t] - nm);
+        for (int t = 0; t < 2; ++t) {
+          top[t] = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
+          top[t] = fmaxf(top[t], __shfl_xor(top[t], 32, 64));
+          const float nm = fmaxf(m[t], top[t]), down = exp2_raw(m[t] - nm);
           m[t] = nm;
           l[t] *= down;
 #pragma unroll
           for (int d = 0; d < VL; ++d) o[t][d] *= down;
         }
+      // The next step's products (behind the last step: of whatever lies there, not used) and this one's weights, which keep
+      // the matrix and the vector units at work together.
+      f32x4 s_next[2][2];
+      scores(buf, s_next);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
         const float ref = m[t] + kLazy;  // weights are over kLift, 2^kLazy
-        float sum = 0.f;
+        float w[8], sum = 0.f;
+        u32x4 hi, lo;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          w[j] = exp2_raw(fmaf(x[j], scale, -ref));
+          w[j] = exp2_raw(fmaf(x[t][j], scale, -ref));
           sum += w[j];
         }
         l[t] += sum;
         // a weight is the sum of two bf16, which leaves out 2^-17 of it
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          hi[t][j] = pack_bf16x2(w[2 * j], w[2 * j + 1]);
-          lo[t][j] = pack_bf16x2(w[2 * j] - __uint_as_float(hi[t][j] << 16), w[2 * j + 1] - __uint_as_float(hi[t][j] & 0xFFFF0000u));
+          hi[j] = pack_bf16x2(w[2 * j], w[2 * j + 1]);
+          lo[j] = pack_bf16x2(w[2 * j] - __uint_as_float(hi[j] << 16), w[2 * j + 1] - __uint_as_float(hi[j] & 0xFFFF0000u));
         }
 #pragma unroll
-        for (int d = 0; d < VL; ++d) o[t][d] = mfma_bf16(v[d], hi[t], o[t][d]);
+        for (int d = 0; d < VL; ++d) o[t][d] = mfma_bf16(v[d], hi, o[t][d]);
 #pragma unroll
-        for (int d = 0; d < VL; ++d) o[t][d] = mfma_bf16(v[d], lo[t], o[t][d]);
+        for (int d = 0; d < VL; ++d) o[t][d] = mfma_bf16(v[d], lo, o[t][d]);
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) s[t][e] = s_next[t][e];
     }
     // The two halves of the positions meet in the step's place, which is free: of each pair of waves one takes the first
     // tile of query vectors, the other the second.
