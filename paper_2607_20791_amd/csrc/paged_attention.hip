@@ -58,8 +58,10 @@ constexpr int item_cost(int nt) { return 4 * nt; }
 constexpr int kMaxRuns = 512;
 constexpr int kWaves = 4;      // per workgroup
 // What a kernel attends to: whole sequences; by a plan, what groups of sequences share, each group a sequence of the
-// tokens of all its members; or what is left of the sequences behind that, whose parts are joined with the shared ones.
-enum Mode { WHOLE, SHARED, OWN };
+// tokens of all its members; or what is left of the sequences behind that, whose parts are joined with the shared ones:
+// long ones as WHOLE, the others, of up to kTailSteps, a wave each.
+enum Mode { WHOLE, SHARED, OWN, TAIL };
+constexpr int kTailSteps = 10;
 
 // New tokens of sequence s.
 RGD_DEV int new_tokens(const PagedAttnArgs& a, int s) { return a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n; }
@@ -85,6 +87,13 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m, int from) {
   q.tiles = (m * a.G + COLS - 1) / COLS;
   return q;
 }
+// What is left of a sequence of m tokens behind its shared positions; no tiles where that is the other mode's.
+template <int COLS, int MODE>
+RGD_DEV Seq rest_of(const PagedAttnArgs& a, int len, int m, int shared) {
+  Seq q = seq_of<COLS>(a, len, m, min(shared, len / 16 * 16));
+  if ((q.steps <= kTailSteps) != (MODE == TAIL)) q.tiles = 0;
+  return q;
+}
 template <int COLS, int MODE>
 RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
   if constexpr (MODE == WHOLE) {
@@ -95,8 +104,7 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
       const PlanGroup g = p.group[s];
       return seq_of<COLS>(a, g.shared, a.most ? g.tokens : 0, 0);
     } else {
-      const int len = paged_len(a.c, s);
-      return seq_of<COLS>(a, len, min(p.tokens[s], a.most), min(p.shared[s], len / 16 * 16));
+      return rest_of<COLS, MODE>(a, paged_len(a.c, s), min(p.tokens[s], a.most), p.shared[s]);
     }
   }
 }
@@ -115,7 +123,7 @@ RGD_DEV Seq uniform_seq(const PagedAttnArgs& a, int s) {
       return seq_of<COLS>(a, g[0], a.most ? g[1] : 0, 0);
     } else {
       const int len = min(max(((Scalar)a.c.lens)[s], 0), a.c.width * a.c.ps);
-      return seq_of<COLS>(a, len, min(((Scalar)p.tokens)[s], a.most), min(((Scalar)p.shared)[s], len / 16 * 16));
+      return rest_of<COLS, MODE>(a, len, min(((Scalar)p.tokens)[s], a.most), ((Scalar)p.shared)[s]);
     }
   }
 }
@@ -349,7 +357,8 @@ struct Piece {
 
   // fp32: four sums of D / 4 products each, as every product is rounded where it is added (heads of 128: 2.8e-7 of the
   // outputs with one sum, 2.0e-7 with two, 1.6e-7 with four, at the same times).
-  RGD_DEV void scores(f32x4 (&s)[NT][NB]) const {
+  RGD_DEV void scores(f32x4 (&s)[NT][NB]) const { scores(k, s); }
+  RGD_DEV void scores(const u32x4 (&k)[NB][KL], f32x4 (&s)[NT][NB]) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -465,6 +474,110 @@ struct Piece {
     load_v(a);
   }
 
+  // One round of positions from p0 on, whose K and V `from` holds; any of them may be masked.  lim: positions that a
+  // column sees, least of all.
+  RGD_DEV void take(Piece& from, const Seq& sq, const int (&lim)[NT], int least, int p0, float scale) {
+    f32x4 s4[NT][NB];
+    scores(from.k, s4);
+    const int here = from.ok, pos = p0 + grp * E;  // of this lane's first score
+    const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
+    bool odd = false;
+    if (here != (1 << NB) - 1 || p0 + PER > sq.len) {
+      const int held = there ? sq.len - pos : 0;
+#pragma unroll
+      for (int d = 0; d < VL; ++d) from.v[d] = keep_first<T>(from.v[d], held);
+    }
+    if (least < min(p0 + PER, sq.len)) {  // not every column sees every value
+#pragma unroll
+      for (int d = 0; d < VL; ++d) odd = odd || any_nonfinite<T>(from.v[d]);
+    }
+    float p[NT][E];
+    u32x4 hi[NT], lo[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int seen = there ? lim[t] - pos : 0;
+      float x[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] : -INFINITY;
+      weights(t, x, scale, p[t], hi[t], lo[t]);
+    }
+    if (__any(odd)) spread_nonfinite(from.v, lim, there, pos);
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int d = 0; d < VL; ++d) o[t][d] = weigh(from.v[d], p[t], hi[t], lo[t], o[t][d]);
+  }
+
+  // 0 times a value that is not finite is not 0, so these leave the product: a
+  // column gets them by whether it sees one, not by its weight
+  RGD_DEV void spread_nonfinite(u32x4 (&v)[VL], const int (&lim)[NT], bool there, int pos) {
+    u32x4 see[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) see[t] = ones<T>(there ? lim[t] - pos : 0);
+#pragma unroll
+    for (int d = 0; d < VL; ++d) {
+#pragma unroll
+      for (int kind = 0; kind < 3; ++kind) {
+        const u32x4 at = marks<T>(v[d], kind);
+        const float is = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const f32x4 r = count(at, see[t]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[t][d][e] += r[e] > 0.f ? is : 0.f;
+          __builtin_amdgcn_sched_barrier(0);  // one count's registers at a time
+        }
+      }
+      v[d] = finite<T>(v[d]);
+    }
+  }
+
+  // The whole item by one wave, two rounds' K and V on their way: a round lasts half of a memory round trip.
+  RGD_DEV void run_alone(const PagedAttnArgs& a, const Item& it, TableWalk& table) {
+    const Seq& sq = it.sq;
+    const int cols = sq.m * a.G, end = it.end();
+    int lim[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      lim[t] = sq.len - sq.m + token_of(a, min(it.qb * COLS + t * 16 + row, cols - 1)) + 1;
+      m[t] = kNoRef;
+      l[t] = 0.f;
+#pragma unroll
+      for (int d = 0; d < VL; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int least = sq.len - sq.m + token_of(a, it.qb * COLS) + 1;
+    const float scale = kLog2e / sqrtf((float)D);
+    Piece other;  // the second round's K and V
+    other.lane = lane;
+    other.row = row;
+    other.grp = grp;
+    auto load = [&](Piece& to, int p0) {
+      if (p0 >= end) return;
+      to.walk = table;
+      to.load_k(a, it.g, p0);
+      to.load_v(a);
+      table = to.walk;
+    };
+    int p0 = it.begin(0, PER);
+    load(*this, p0);
+    load_q(a, it);
+    load(other, p0 + PER);
+    while (p0 < end) {
+      take(*this, sq, lim, least, p0, scale);
+      load(*this, p0 + 2 * PER);
+      p0 += PER;
+      if (p0 >= end) break;
+      take(other, sq, lim, least, p0, scale);
+      load(other, p0 + 2 * PER);
+      p0 += PER;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      l[t] += __shfl_xor(l[t], 16, 64);
+      l[t] += __shfl_xor(l[t], 32, 64);
+    }
+  }
+
   // The wave's share of an item's steps, whose queries and first K and V are on their
   // way; leaves those of the next item on theirs (walk_next: its table's first entries).
   RGD_DEV void run(const PagedAttnArgs& a, const Item& it, const Item& next, const TableWalk& walk_next, int wave) {
@@ -540,29 +653,7 @@ struct Piece {
         for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] : -INFINITY;
         weights(t, x, scale, p[t], hi[t], lo[t]);
       }
-      if (__any(odd)) {
-        // 0 times a value that is not finite is not 0, so these leave the product: a
-        // column gets them by whether it sees one, not by its weight
-        u32x4 see[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) see[t] = ones<T>(there ? lim[t] - pos : 0);
-#pragma unroll
-        for (int d = 0; d < VL; ++d) {
-#pragma unroll
-          for (int kind = 0; kind < 3; ++kind) {
-            const u32x4 at = marks<T>(v[d], kind);
-            const float is = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              const f32x4 r = count(at, see[t]);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[t][d][e] += r[e] > 0.f ? is : 0.f;
-              __builtin_amdgcn_sched_barrier(0);  // one count's registers at a time
-            }
-          }
-          v[d] = finite<T>(v[d]);
-        }
-      }
+      if (__any(odd)) spread_nonfinite(v, lim, there, pos);
 #pragma unroll
       for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -577,12 +668,6 @@ struct Piece {
     }
   }
 };
-
-template <typename T>
-RGD_DEV void store_row4(T* p, f32x4 v) {
-  if constexpr (sizeof(T) == 2) *(u32x2*)p = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
-  else *(f32x4*)p = v;
-}
 
 // Workspace: per run a Cut, then the pieces: slot 2 r + 1 holds the start of the item
 // that run r ends in, slot 2 r the part of an item that an earlier run began.  Per slot
@@ -601,43 +686,78 @@ constexpr size_t slot_floats() {
 // Whether a CU holds two workgroups (row: bytes of a row of K).
 constexpr bool two_per_cu(int nt, size_t row) { return nt == 1 || (nt == 2 && row < 512); }
 
+template <typename T>
+RGD_DEV void store_row4(T* p, f32x4 v) {
+  if constexpr (sizeof(T) == 2) *(u32x2*)p = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+  else *(f32x4*)p = v;
+}
+
 // The parts of a sequence's shared positions, as the kernel before left them, joined with (top, sum, o) of a query vector of
 // token i; four dimensions from d on.
 struct SharedParts {
   const float* slots;
   long long length, unit;  // of a run; the group's first
   int col, tiles, steps, item, cols, cost, D;
+  // (scalar loads: s is the wave's, and these loads do not queue behind K and V)
   RGD_DEV SharedParts(const PagedAttnArgs& a, int s) {
+    typedef const int __attribute__((address_space(4))) * Scalar;
+    typedef const long long __attribute__((address_space(4))) * Scalar64;
     const Plan p(a.plan, a.c.S);
-    const int leader = p.leader[s], shared = leader < 0 ? 0 : p.shared[s];
+    const int leader = ((Scalar)p.leader)[s], shared = leader < 0 ? 0 : ((Scalar)p.shared)[s];
     steps = (shared + a.s_step - 1) / a.s_step;
     if (!steps) return;
-    const PlanGroup g = p.group[leader];
-    const GroupAt at = ((const GroupAt*)a.at)[leader];
-    length = ((const GroupAt*)a.at)[a.c.S].unit;
-    unit = at.unit;
-    item = at.item;
-    col = (p.row[s] - g.row) * a.G;
+    Scalar g = (Scalar)p.group + 4 * leader, at = (Scalar)a.at + 4 * leader;
+    length = *((Scalar64)a.at + 2 * a.c.S);
+    unit = *(Scalar64)at;
+    item = at[2];
+    col = (((Scalar)p.row)[s] - g[2]) * a.G;
     cols = a.s_cols;
     cost = a.s_cost;
-    tiles = (g.tokens * a.G + cols - 1) / cols;
+    tiles = (g[1] * a.G + cols - 1) / cols;
     slots = a.slots;
     D = a.c.D;
+  }
+  // the slots of query vector v of KV head g: [first, last], and its place there
+  RGD_DEV const float* find(int g, int v, int& parts, int& c) const {
+    const int qb = (col + v) / cols, k = g * tiles + qb;
+    c = col + v - qb * cols;
+    const long long u = unit + (long long)k * (steps + cost) + cost;
+    const int r0 = (int)quotient(u, length);
+    parts = (int)quotient(u + steps - 1, length) - r0 + 1;
+    return slots + (size_t)(r0 + item + k) * cols * (D + 2);
   }
   // the query vector of KV head g that is `v` (token * G + head) among the sequence's
   RGD_DEV void join(int g, int v, int d, float& top, float& sum, f32x4& o) const {
     if (!steps) return;
-    const int qb = (col + v) / cols, c = col + v - qb * cols, k = g * tiles + qb;
-    const long long u = unit + (long long)k * (steps + cost) + cost;
-    const int r0 = (int)quotient(u, length), r1 = (int)quotient(u + steps - 1, length);
-    const size_t size = (size_t)cols * (D + 2);
-    const float* slot = slots + (size_t)(r0 + item + k) * size;
+    int parts, c;
+    const float* slot = find(g, v, parts, c);
 #pragma unroll 4
-    for (int r = r0; r <= r1; ++r, slot += size) {
-      const float2 ml = *(const float2*)(slot + cols * D + 2 * c);
-      const f32x4 x = *(const f32x4*)(slot + c * D + d);
+    for (int r = 0; r < parts; ++r) {
+      const float* at = slot + (size_t)r * cols * (D + 2);
+      const float2 ml = *(const float2*)(at + cols * D + 2 * c);
+      const f32x4 x = *(const f32x4*)(at + c * D + d);
       const float nt = fmaxf(top, ml.x), down = exp2_raw(top - nt), f = exp2_raw(ml.x - nt);
       o = o * down + f * x;
+      sum = sum * down + f * ml.y;
+      top = nt;
+    }
+  }
+  // all of a lane's dimensions, d * 16 + off
+  template <int VL>
+  RGD_DEV void join_all(int g, int v, int off, float& top, float& sum, f32x4 (&o)[VL]) const {
+    if (!steps) return;
+    int parts, c;
+    const float* slot = find(g, v, parts, c);
+#pragma unroll 4
+    for (int r = 0; r < parts; ++r) {
+      const float* at = slot + (size_t)r * cols * (D + 2);
+      const float2 ml = *(const float2*)(at + cols * D + 2 * c);
+      f32x4 x[VL];
+#pragma unroll
+      for (int d = 0; d < VL; ++d) x[d] = *(const f32x4*)(at + c * D + d * 16 + off);
+      const float nt = fmaxf(top, ml.x), down = exp2_raw(top - nt), f = exp2_raw(ml.x - nt);
+#pragma unroll
+      for (int d = 0; d < VL; ++d) o[d] = o[d] * down + f * x[d];
       sum = sum * down + f * ml.y;
       top = nt;
     }
@@ -666,6 +786,42 @@ RGD_DEV void check_plan(PagedAttnArgs& a) {
   if constexpr (MODE != WHOLE) a.most = *Plan(a.plan, a.c.S).head == PlanHead::of(a.c, a.n, a.Hq) ? a.n : 0;
 }
 
+// What is left of a sequence behind its shared positions, where that is short: the wave's item is 16 query vectors of a
+// KV head, which one round trip after the other and the shared parts bound; there are enough of them to fill the chip.
+template <typename T, int D>
+RGD_DEV void attend_tail(PagedAttnArgs a, int index) {
+  using P = Piece<T, D, 1, false, TAIL>;
+  check_plan<TAIL>(a);
+  const int per = (a.n * a.G + 15) / 16, s = index / (a.c.Hkv * per), rest = index - s * a.c.Hkv * per;
+  if (s >= a.c.S) return;
+  Item it{};
+  it.sq = uniform_seq<16, TAIL>(a, s);
+  it.s = s;
+  it.g = rest / per;
+  it.qb = rest - it.g * per;
+  if (it.qb >= it.sq.tiles) return;
+  it.t1 = it.sq.steps;
+  it.valid = true;
+  const SharedParts shared(a, s);
+  P x;
+  x.lane = threadIdx.x & 63;
+  x.row = x.lane & 15;
+  x.grp = x.lane >> 4;
+  TableWalk table;
+  table.start(a.c, s, it.begin(0, P::PER) >> 4);
+  x.run_alone(a, it, table);
+  const int col = it.qb * 16 + x.row;
+  if (col >= it.sq.m * a.G) return;
+  float top = x.m[0], sum = x.l[0];
+  shared.join_all(it.g, col, x.grp * 4, top, sum, x.o[0]);
+  const int i = token_of(a, col);
+  const size_t at = ((size_t)s * a.n + i) * a.Hq + it.g * a.G + col - i * a.G;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int d = 0; d < P::VL; ++d) store_row4((T*)a.out + at * D + d * 16 + x.grp * 4, x.o[0][d] * inv);
+  if (a.lse && x.grp == 0) a.lse[at] = lse_of(top, sum);
+}
+
 template <typename T, int D, int NT, bool PAST, int MODE>
 __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
   using P = Piece<T, D, NT, PAST, MODE>;
@@ -673,7 +829,16 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
   __shared__ u32x4 q_s[P::QS ? NT * P::KL * 64 : 1];
-  const int r = blockIdx.x, wave = uniform(threadIdx.x >> 6);
+  const int wave = uniform(threadIdx.x >> 6);
+  int r = blockIdx.x;
+  if constexpr (MODE == OWN) {  // the tails' workgroups come before the runs'
+    const int tails = gridDim.x - runs;
+    if (r < tails) {
+      attend_tail<T, D>(a, uniform(r * kWaves + wave));
+      return;
+    }
+    r -= tails;
+  }
   const int lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
   Runs plan;
   int s;
@@ -828,7 +993,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int run
       sum += f * ml_s[k][i].y;
     }
   }
-  if constexpr (MODE == OWN) SharedParts(a, cut.s).join(cut.g, col, 4 * d, top, sum, acc);
+  if constexpr (MODE == OWN) SharedParts(a, uniform(cut.s)).join(cut.g, col, 4 * d, top, sum, acc);
   const int i = token_of(a, col);
   const size_t at = ((size_t)cut.s * a.n + i) * a.Hq + cut.g * G + col - i * G;
   store_row4((T*)a.out + at * D + 4 * d, acc * (sum == 0.f ? 0.f : 1.f / sum));
@@ -855,12 +1020,13 @@ int runs_for(const PagedView& c, int vectors) {
 
 template <typename T, int D, int NT, int MODE>
 hipError_t launch(const PagedAttnArgs& a, int vectors, hipStream_t s) {
-  const int runs = runs_for(a.c, vectors), extra = MODE == SHARED;
+  const int runs = runs_for(a.c, vectors);
+  const int extra = MODE == SHARED ? 1 : MODE == OWN ? (a.c.S * a.c.Hkv * ((a.n * a.G + 15) / 16) + kWaves - 1) / kWaves : 0;
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
   // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
   if (MODE != SHARED && a.c.ps <= Piece<T, D, NT, true, MODE>::PER)
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs), dim3(256), 0, s, a, runs);
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs + extra), dim3(256), 0, s, a, runs);
   else
     hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false, MODE>), dim3(runs + extra), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
