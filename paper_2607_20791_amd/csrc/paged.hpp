@@ -64,6 +64,7 @@ struct RotateArgs {
   double turns[64];  // of each pair, per position
   int G;       // query heads per KV head
   int blocks;  // 16-position blocks per sequence
+  int heads;   // KV heads per workgroup
 };
 hipError_t paged_append_rotated(const RotateArgs& a, hipStream_t s);
 
