@@ -588,7 +588,9 @@ int32_t rgd_paged_append_rotated(const rgd_paged_cache* cache, int32_t layer, co
 /* ---- attention of sequences that share leading pages ---- */
 
 /* Bytes of the plan (256-byte aligned device memory) that rgd_paged_share writes for up to n new tokens per sequence
- * and n_heads query heads; 0 for arguments it refuses. */
+ * and n_heads query heads; 0 for arguments it refuses.  Besides rgd_paged_attention's limits, max_seqs * n * n_heads is at
+ * most 2^22, max_seqs * n * (n_heads / Hkv)^2 below 2^31, and the tables hold at most 2^38 units of the work of all groups,
+ * a unit a step of 32 or 64 positions of 16 to 128 query vectors of one KV head. */
 uint64_t rgd_paged_share_bytes(const rgd_paged_cache* cache, int32_t n, int32_t n_heads);
 
 /* Finds what the sequences of each group share, once for all layers of a turn: sequences with equal labels in
@@ -626,12 +628,12 @@ uint64_t rgd_sample_truncated_workspace_bytes(int32_t R, int32_t V);
  *   of these, every id with z - max z >= T ln(min_p) (dev fp32 [R]; 0 and below, NaN, or NULL: no limit; above 1 as 1).
  * The id drawn is the smallest one whose running kept weight, in the order of the ids, exceeds u (dev fp32 [R], uniform in
  * [0, 1); outside as the nearest inside, NaN as 0) times the kept weight.  T dev fp32 [R] (NULL: 1); where it is 0,
- * negative or NaN the first maximum is drawn.  out dev int32 [R]; logp dev fp32 [R] or NULL: the logarithm of the drawn id's share of the kept
- * weight.  NaN logits count as -inf, which is never kept; a row whose maximum is not finite gives -1 and -inf.
- * Weights are taken in 64 bits, to 2^-44 of the largest (less weighs nothing), and sums are of whole multiples of 2^-43, so that
- * they do not depend on their order: the draw is the exact one unless u or a limit meets the border of two
- * ids by about 2^-44 for each id.  The same row gives the same id in any batch.  1 <= R <= 65536, 1 <= V <= 2^20, ldz >= V.  out, logp and the workspace
- * overlap neither each other nor an input.  Asynchronous. */
+ * negative or NaN the first maximum is drawn.  out dev int32 [R]; logp dev fp32 [R] or NULL: the logarithm of the drawn
+ * id's share of the kept weight.  NaN logits count as -inf, which is never kept; a row whose maximum is not finite gives
+ * -1 and -inf.  Weights are taken in 64 bits, to 2^-44 of the largest (less weighs nothing), and sums are of whole
+ * multiples of 2^-43, so that they do not depend on their order: the draw is the exact one unless u or a limit meets the
+ * border of two ids by about 2^-44 for each id.  The same row gives the same id in any batch.  1 <= R <= 65536,
+ * 1 <= V <= 2^20, ldz >= V.  out, logp and the workspace overlap neither each other nor an input.  Asynchronous. */
 int32_t rgd_sample_truncated(const float* z, int64_t ldz, int32_t R, int32_t V, const float* T, const int32_t* top_k,
                              const float* top_p, const float* min_p, const float* u, void* workspace, int32_t* out,
                              float* logp, rgd_stream stream);

@@ -59,9 +59,10 @@ constexpr int kMaxRuns = 512;
 constexpr int kWaves = 4;      // per workgroup
 // What a kernel attends to: whole sequences; by a plan, what groups of sequences share, each group a sequence of the
 // tokens of all its members; or what is left of the sequences behind that, whose parts are joined with the shared ones:
-// long ones as WHOLE, the others, of up to kTailSteps, a wave each.
+// long ones as WHOLE, the others, of up to kTailSteps, a wave or a workgroup each.
 enum Mode { WHOLE, SHARED, OWN, TAIL };
-constexpr int kTailSteps = 10;
+constexpr int kTailSteps = 24, kAloneSteps = 2, kManyTails = 768;
+static_assert(2 * kTailSteps + 1 <= 64, "a tail's pages, of 16 positions at least, are looked up in one load");
 
 // New tokens of sequence s.
 RGD_DEV int new_tokens(const PagedAttnArgs& a, int s) { return a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n; }
@@ -322,7 +323,7 @@ struct Piece {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       int place;
-      int p = walk.find((p0 >> 4) + b, place);
+      int p = MODE == TAIL ? walk.find_near((p0 >> 4) + b, place) : walk.find((p0 >> 4) + b, place);
       if (page_ok(a.c, p)) ok |= 1 << b;
       else p = 0;
       const size_t head = ((size_t)p * a.c.Hkv + g) * a.c.ps * D;
@@ -357,8 +358,7 @@ struct Piece {
 
   // fp32: four sums of D / 4 products each, as every product is rounded where it is added (heads of 128: 2.8e-7 of the
   // outputs with one sum, 2.0e-7 with two, 1.6e-7 with four, at the same times).
-  RGD_DEV void scores(f32x4 (&s)[NT][NB]) const { scores(k, s); }
-  RGD_DEV void scores(const u32x4 (&k)[NB][KL], f32x4 (&s)[NT][NB]) const {
+  RGD_DEV void scores(f32x4 (&s)[NT][NB]) const {
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -474,22 +474,28 @@ struct Piece {
     load_v(a);
   }
 
-  // One round of positions from p0 on, whose K and V `from` holds; any of them may be masked.  lim: positions that a
-  // column sees, least of all.
-  RGD_DEV void take(Piece& from, const Seq& sq, const int (&lim)[NT], int least, int p0, float scale) {
+  // One round of positions from p0 on, any of which may be masked, whose K and V are on their way; leaves those of p1 on
+  // theirs.  lim: positions that a column sees, least of all.
+  template <class LoadK>
+  RGD_DEV void take(const PagedAttnArgs& a, const Seq& sq, const int (&lim)[NT], int least, int p0, float scale, LoadK&& next) {
     f32x4 s4[NT][NB];
-    scores(from.k, s4);
-    const int here = from.ok, pos = p0 + grp * E;  // of this lane's first score
+    scores(s4);
+    const int here = ok;
+    __builtin_amdgcn_sched_barrier(0);
+    next();
+    __builtin_amdgcn_sched_barrier(0);
+    const int pos = p0 + grp * E;  // of this lane's first score
+// of this lane's first score
     const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
     bool odd = false;
     if (here != (1 << NB) - 1 || p0 + PER > sq.len) {
       const int held = there ? sq.len - pos : 0;
 #pragma unroll
-      for (int d = 0; d < VL; ++d) from.v[d] = keep_first<T>(from.v[d], held);
+      for (int d = 0; d < VL; ++d) v[d] = keep_first<T>(v[d], held);
     }
     if (least < min(p0 + PER, sq.len)) {  // not every column sees every value
 #pragma unroll
-      for (int d = 0; d < VL; ++d) odd = odd || any_nonfinite<T>(from.v[d]);
+      for (int d = 0; d < VL; ++d) odd = odd || any_nonfinite<T>(v[d]);
     }
     float p[NT][E];
     u32x4 hi[NT], lo[NT];
@@ -501,11 +507,11 @@ struct Piece {
       for (int j = 0; j < E; ++j) x[j] = j < seen ? s4[t][j / 4][j % 4] : -INFINITY;
       weights(t, x, scale, p[t], hi[t], lo[t]);
     }
-    if (__any(odd)) spread_nonfinite(from.v, lim, there, pos);
+    if (__any(odd)) spread_nonfinite(v, lim, there, pos);
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-      for (int d = 0; d < VL; ++d) o[t][d] = weigh(from.v[d], p[t], hi[t], lo[t], o[t][d]);
+      for (int d = 0; d < VL; ++d) o[t][d] = weigh(v[d], p[t], hi[t], lo[t], o[t][d]);
   }
 
   // 0 times a value that is not finite is not 0, so these leave the product: a
@@ -532,10 +538,11 @@ struct Piece {
     }
   }
 
-  // The whole item by one wave, two rounds' K and V on their way: a round lasts half of a memory round trip.
-  RGD_DEV void run_alone(const PagedAttnArgs& a, const Item& it, TableWalk& table) {
+  // Every waves-th round of the item from the wave's own on.  The loads are the same on every path, so that a wait for some
+  // leaves those behind them on their way: behind the end every lane asks for the last round's first bytes.
+  RGD_DEV void run_alone(const PagedAttnArgs& a, const Item& it, const TableWalk& table, int wave, int waves) {
     const Seq& sq = it.sq;
-    const int cols = sq.m * a.G, end = it.end();
+    const int cols = sq.m * a.G, by = waves * PER, first = it.begin(wave, PER), end = it.end();
     int lim[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -545,31 +552,28 @@ struct Piece {
 #pragma unroll
       for (int d = 0; d < VL; ++d) o[t][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int least = sq.len - sq.m + token_of(a, it.qb * COLS) + 1;
+    if (first >= end) return;
+    const int least = sq.len - sq.m + token_of(a, it.qb * COLS) + 1, row0 = row, grp0 = grp;
     const float scale = kLog2e / sqrtf((float)D);
-    Piece other;  // the second round's K and V
-    other.lane = lane;
-    other.row = row;
-    other.grp = grp;
-    auto load = [&](Piece& to, int p0) {
-      if (p0 >= end) return;
-      to.walk = table;
-      to.load_k(a, it.g, p0);
-      to.load_v(a);
-      table = to.walk;
-    };
-    int p0 = it.begin(0, PER);
-    load(*this, p0);
+    walk = table;
     load_q(a, it);
-    load(other, p0 + PER);
-    while (p0 < end) {
-      take(*this, sq, lim, least, p0, scale);
-      load(*this, p0 + 2 * PER);
-      p0 += PER;
-      if (p0 >= end) break;
-      take(other, sq, lim, least, p0, scale);
-      load(other, p0 + 2 * PER);
-      p0 += PER;
+    load_k(a, it.g, first);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(a);
+    for (int p0 = first; p0 < end; p0 += by) {
+      const bool more = p0 + by < end;
+      take(a, sq, lim, least, p0, scale, [&] {
+        row = more ? row0 : 0;
+        grp = more ? grp0 : 0;
+        load_k(a, it.g, more ? p0 + by : p0);
+        row = row0;
+        grp = grp0;
+      });
+      row = more ? row0 : 0;
+      grp = more ? grp0 : 0;
+      load_v(a);
+      row = row0;
+      grp = grp0;
     }
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -631,8 +635,7 @@ struct Piece {
         load_q(a, next);
         load_k(a, next.g, first);
       }
-      const int pos = p0 + grp * E;  // of this lane's first score
-      const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
+      const int pos = p0 + grp * E;      const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
       bool odd = false;
       if (here != ALL || p0 + PER > sq.len) {
         const int held = there ? sq.len - pos : 0;
@@ -742,14 +745,14 @@ struct SharedParts {
       top = nt;
     }
   }
-  // all of a lane's dimensions, d * 16 + off
+  // all of a lane's dimensions, d * 16 + off; every `ways`-th part from `way` on
   template <int VL>
-  RGD_DEV void join_all(int g, int v, int off, float& top, float& sum, f32x4 (&o)[VL]) const {
+  RGD_DEV void join_all(int g, int v, int off, int way, int ways, float& top, float& sum, f32x4 (&o)[VL]) const {
     if (!steps) return;
     int parts, c;
     const float* slot = find(g, v, parts, c);
 #pragma unroll 4
-    for (int r = 0; r < parts; ++r) {
+    for (int r = way; r < parts; r += ways) {
       const float* at = slot + (size_t)r * cols * (D + 2);
       const float2 ml = *(const float2*)(at + cols * D + 2 * c);
       f32x4 x[VL];
@@ -786,42 +789,6 @@ RGD_DEV void check_plan(PagedAttnArgs& a) {
   if constexpr (MODE != WHOLE) a.most = *Plan(a.plan, a.c.S).head == PlanHead::of(a.c, a.n, a.Hq) ? a.n : 0;
 }
 
-// What is left of a sequence behind its shared positions, where that is short: the wave's item is 16 query vectors of a
-// KV head, which one round trip after the other and the shared parts bound; there are enough of them to fill the chip.
-template <typename T, int D>
-RGD_DEV void attend_tail(PagedAttnArgs a, int index) {
-  using P = Piece<T, D, 1, false, TAIL>;
-  check_plan<TAIL>(a);
-  const int per = (a.n * a.G + 15) / 16, s = index / (a.c.Hkv * per), rest = index - s * a.c.Hkv * per;
-  if (s >= a.c.S) return;
-  Item it{};
-  it.sq = uniform_seq<16, TAIL>(a, s);
-  it.s = s;
-  it.g = rest / per;
-  it.qb = rest - it.g * per;
-  if (it.qb >= it.sq.tiles) return;
-  it.t1 = it.sq.steps;
-  it.valid = true;
-  const SharedParts shared(a, s);
-  P x;
-  x.lane = threadIdx.x & 63;
-  x.row = x.lane & 15;
-  x.grp = x.lane >> 4;
-  TableWalk table;
-  table.start(a.c, s, it.begin(0, P::PER) >> 4);
-  x.run_alone(a, it, table);
-  const int col = it.qb * 16 + x.row;
-  if (col >= it.sq.m * a.G) return;
-  float top = x.m[0], sum = x.l[0];
-  shared.join_all(it.g, col, x.grp * 4, top, sum, x.o[0]);
-  const int i = token_of(a, col);
-  const size_t at = ((size_t)s * a.n + i) * a.Hq + it.g * a.G + col - i * a.G;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int d = 0; d < P::VL; ++d) store_row4((T*)a.out + at * D + d * 16 + x.grp * 4, x.o[0][d] * inv);
-  if (a.lse && x.grp == 0) a.lse[at] = lse_of(top, sum);
-}
-
 template <typename T, int D, int NT, bool PAST, int MODE>
 __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void attn_run_kernel(PagedAttnArgs a, int runs) {
   using P = Piece<T, D, NT, PAST, MODE>;
@@ -829,16 +796,7 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
   __shared__ float part[kWaves][COLS][LD];
   __shared__ float2 ml[kWaves][COLS];
   __shared__ u32x4 q_s[P::QS ? NT * P::KL * 64 : 1];
-  const int wave = uniform(threadIdx.x >> 6);
-  int r = blockIdx.x;
-  if constexpr (MODE == OWN) {  // the tails' workgroups come before the runs'
-    const int tails = gridDim.x - runs;
-    if (r < tails) {
-      attend_tail<T, D>(a, uniform(r * kWaves + wave));
-      return;
-    }
-    r -= tails;
-  }
+  const int r = blockIdx.x, wave = uniform(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, row = lane & 15, grp = lane >> 4;
   Runs plan;
   int s;
@@ -940,17 +898,121 @@ __global__ __launch_bounds__(256, two_per_cu(NT, sizeof(T) * D) ? 2 : 1) void at
 // 64 pieces a head: 5.7 us, 12.8 with eight; 16 tokens of 16 sequences of 4096: 5.2, 13.3 with one.
 constexpr int join_cols(int nt) { return nt == 1 ? 1 : 8; }
 
+// Workgroups of the tails, four for each four items.
+__host__ __device__ inline int tail_groups(const PagedAttnArgs& a) {
+  return kWaves * a.c.S * ((a.c.Hkv * ((a.n * a.G + 15) / 16) + kWaves - 1) / kWaves);
+}
+
+// What is left of a sequence behind its shared positions, where that is short: 16 query vectors of a KV head are a
+// workgroup's, whose waves take rounds and shared parts in turn, or, of up to kAloneSteps steps where there are more than
+// the chip holds workgroups, a wave's.  What bounds it is a chain of loads: lengths and plan, pages, K and V, parts (9 us of
+// the 15 that 64 branches of one prompt take; theirs a wave each, 17).  256 branches, 4 to 300 positions left, 8 KV
+// heads: 30 us, a wave for up to 0, 2, 3 and 6 steps 33, 31, 30 and 31; 64 x 5 tokens, 20 vectors: 16, 16, 19 and 21.
+// There are four workgroups for each four items, of which the first has work where waves do them; these come
+// before all others, so that they meet all parts of the chip.
+template <typename T, int D>
+RGD_DEV void attend_tail(PagedAttnArgs a, int index, float (&part)[kWaves][16][D + 4], float2 (&ml)[kWaves][16]) {
+  using P = Piece<T, D, 1, false, TAIL>;
+  check_plan<TAIL>(a);
+  const int wave = uniform(threadIdx.x >> 6);
+  const int per = (a.n * a.G + 15) / 16, all = a.c.Hkv * per, fours = (all + kWaves - 1) / kWaves;
+  const int nth = index / (a.c.S * fours), s = (index - nth * a.c.S * fours) / fours;
+  Item it{};
+  it.sq = uniform_seq<16, TAIL>(a, s);
+  const bool alone = a.c.S * all > kManyTails && it.sq.steps <= kAloneSteps;
+  if (alone && nth) return;
+  const int rest = index % fours * kWaves + (alone ? wave : nth);
+  if (rest >= all) return;
+  it.s = s;
+  it.g = rest / per;
+  it.qb = rest - it.g * per;
+  if (it.qb >= it.sq.tiles) return;
+  it.t1 = it.sq.steps;
+  it.valid = true;
+  const SharedParts shared(a, s);
+  P x;
+  x.lane = threadIdx.x & 63;
+  x.row = x.lane & 15;
+  x.grp = x.lane >> 4;
+  TableWalk table;
+  table.start(a.c, s, it.begin(0, P::PER) >> 4);
+  const int w0 = alone ? 0 : wave, waves = alone ? 1 : kWaves;
+  x.run_alone(a, it, table, w0, waves);
+  // where there are fewer than 16 columns, the lanes of the others take part of a column's shared parts
+  const int here = min(it.sq.m * a.G - it.qb * 16, 16), width = here > 8 ? 16 : here > 4 ? 8 : here > 2 ? 4 : here;
+  const int way = x.row / width, ways = 16 / width, col = it.qb * 16 + min(x.row % width, here - 1);
+  float top = way ? kNoRef : x.m[0], sum = way ? 0.f : x.l[0];
+#pragma unroll
+  for (int d = 0; d < P::VL; ++d) x.o[0][d] = way ? f32x4{0.f, 0.f, 0.f, 0.f} : x.o[0][d];
+  shared.join_all(it.g, col, x.grp * 4, way + ways * w0, ways * waves, top, sum, x.o[0]);
+  for (int w = width; w < 16; w *= 2) {
+    const float t2 = __shfl_xor(top, w, 64), s2 = __shfl_xor(sum, w, 64);
+    const float nt = fmaxf(top, t2), down = exp2_raw(top - nt), f = exp2_raw(t2 - nt);
+    sum = sum * down + f * s2;
+    top = nt;
+#pragma unroll
+    for (int d = 0; d < P::VL; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x.o[0][d][e] = x.o[0][d][e] * down + f * __shfl_xor(x.o[0][d][e], w, 64);
+  }
+  const int i = token_of(a, col);
+  const size_t at = ((size_t)s * a.n + i) * a.Hq + it.g * a.G + col - i * a.G;
+  if (alone) {
+    if (x.row >= here) return;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int d = 0; d < P::VL; ++d) store_row4((T*)a.out + at * D + d * 16 + x.grp * 4, x.o[0][d] * inv);
+    if (a.lse && x.grp == 0) a.lse[at] = lse_of(top, sum);
+    return;
+  }
+#pragma unroll
+  for (int d = 0; d < P::VL; ++d) *(f32x4*)&part[wave][x.row][d * 16 + x.grp * 4] = x.o[0][d];
+  if (x.grp == 0) ml[wave][x.row] = float2{top, sum};
+  __syncthreads();
+  if (x.row >= here) return;
+  top = kNoRef;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, ml[w][x.row].x);
+  float f[kWaves];
+  sum = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    f[w] = exp2_raw(ml[w][x.row].x - top);
+    sum += f[w] * ml[w][x.row].y;
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  for (int d = wave; d < P::VL; d += kWaves) {
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) o += f[w] * *(const f32x4*)&part[w][x.row][d * 16 + x.grp * 4];
+    store_row4((T*)a.out + at * D + d * 16 + x.grp * 4, o * inv);
+  }
+  if (a.lse && x.grp == 0 && wave == 0) a.lse[at] = lse_of(top, sum);
+}
+
 // The outputs of the items that several runs share, by the run that an item starts
 // in: one workgroup per (run, join_cols columns), D / 4 threads to a piece.  2.8 to 5.7 us: a launch and
 // one round trip, two where an item has more pieces than fit the threads (1 to 5 MB, which lie in the caches).
 template <typename T, int D, int NT, int MODE>
-__global__ __launch_bounds__(256) void attn_join_kernel(PagedAttnArgs a, int runs) {
+__global__ __launch_bounds__(256, MODE != OWN ? 1 : D == 32 || sizeof(T) * D == 512 ? 2 : 3) void attn_join_kernel(PagedAttnArgs a, int runs) {
   constexpr int COLS = 16 * NT, W = D / 4, CB = join_cols(NT), PARTS = 256 / W / CB;
   __shared__ f32x4 acc_s[CB][PARTS][W];
   __shared__ float2 ml_s[CB][PARTS];
-  const int r = blockIdx.x, t = threadIdx.x;
+  const int t = threadIdx.x;
+  int block = blockIdx.x;
+  if constexpr (MODE == OWN) {  // the tails' workgroups come first
+    __shared__ float part_s[kWaves][16][D + 4];
+    __shared__ float2 ml_w[kWaves][16];
+    const int tails = tail_groups(a);
+    if (block < tails) {
+      attend_tail<T, D>(a, block, part_s, ml_w);
+      return;
+    }
+    block -= tails;
+  }
+  const int r = block % runs, by = block / runs;
   const Cut cut = ((const Cut*)a.ws)[r];
-  const int d = t % W, k = t / W / PARTS, part = t / W % PARTS, c = blockIdx.y * CB + k;
+  const int d = t % W, k = t / W / PARTS, part = t / W % PARTS, c = by * CB + k;
   const float* slots = a.ws + cut_floats(runs);
   auto slot = [&](int w) { return slots + (size_t)(2 * w + (w == r)) * slot_floats<D, NT>(); };
   // the first piece is asked for together with the cut; where there is none, it is not used
@@ -1021,18 +1083,17 @@ int runs_for(const PagedView& c, int vectors) {
 template <typename T, int D, int NT, int MODE>
 hipError_t launch(const PagedAttnArgs& a, int vectors, hipStream_t s) {
   const int runs = runs_for(a.c, vectors);
-  const int extra = MODE == SHARED ? 1 : MODE == OWN ? (a.c.S * a.c.Hkv * ((a.n * a.G + 15) / 16) + kWaves - 1) / kWaves : 0;
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
   // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
   if (MODE != SHARED && a.c.ps <= Piece<T, D, NT, true, MODE>::PER)
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs + extra), dim3(256), 0, s, a, runs);
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs), dim3(256), 0, s, a, runs);
   else
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false, MODE>), dim3(runs + extra), dim3(256), 0, s, a, runs);
+    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false, MODE>), dim3(runs + (MODE == SHARED)), dim3(256), 0, s, a, runs);
   if (hipError_t e = hipGetLastError()) return e;
   if (MODE == SHARED) return hipSuccess;
   const int cols = std::min(16 * NT, a.n * a.G);
-  const dim3 grid(runs, (cols + join_cols(NT) - 1) / join_cols(NT));
+  const dim3 grid(runs * ((cols + join_cols(NT) - 1) / join_cols(NT)) + (MODE == OWN ? tail_groups(a) : 0));
   hipLaunchKernelGGL((attn_join_kernel<T, D, NT, MODE>), grid, dim3(256), 0, s, a, runs);
   return hipGetLastError();
 }

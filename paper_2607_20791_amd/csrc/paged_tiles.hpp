@@ -73,6 +73,12 @@ struct TableWalk {
     }
     return __builtin_amdgcn_readlane(cur, j - jb);
   }
+  // of the first 64 pages: no load, for which those on their way would be waited for
+  RGD_DEV int find_near(int block, int& place) const {
+    const int j = page_index(block);
+    place = block - j * bpp;
+    return __builtin_amdgcn_readlane(cur, j - jb);
+  }
 };
 
 RGD_DEV float lse_of(float m, float l) { return l == 0.f ? -INFINITY : (m + __log2f(l * kLift)) * kLn2; }

@@ -368,3 +368,15 @@ def test_binding_refuses_wrong_tensors(rgd):
                dict(out=q), dict(lse=out), dict(q=q[:, :5])):
         with pytest.raises(rgd.RGDError):
             rgd.paged_attention_shared(x.c, **{**good, **kw})
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("bf16,n,d", [(True, 1, 128), (True, 5, 64), (False, 1, 32), (False, 3, 128)])
+def test_own_parts_around_every_length(rgd, bf16, n, d, many):
+    """Own parts of whole steps of 32 positions and one more or less, where a wave, a workgroup and the runs take turns; few
+    sequences, and as many as do not fit the chip at once."""
+    steps = [1, 31, 32, 33, 63, 64, 65, 96, 97, 128, 129, 319, 321, 767, 768, 769, 800]
+    hk = 8 if many else 2
+    x, group = _forks(rgd, [32 if bf16 else 48] * (7 if many else 1), len(steps), [n + t for t in steps], [n, 1], hk=hk, d=d, bf16=bf16, layers=1,
+                      seed=n + d)
+    _attend(x, 0, hk * 3, n, x.new, group)
