@@ -33,6 +33,10 @@
 // of 1024 sequences of up to 500 (354 MB): 115 us, as an item is a step or two of one to three waves.
 // Pieces of prompts, 4 sequences of 4096: 16 tokens 26 us, 64 59, 256 222, 1000 783 (300 TFLOP/s): each
 // 64 query vectors read the keys and values again, from the caches.
+//
+// By a plan of what sequences share the same kernels take only what is left of each one behind its shared positions, and
+// join that with the parts that the groups' kernel left (fp32: the run kernel with a group's tokens as one sequence's; bf16:
+// a kernel of its own).  Most of what is left is short, and is done in the joining launch.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -11,6 +11,13 @@
 // for every fragment that is read from LDS), and two the positions, 32 each; they meet in LDS at an item's end.  Both
 // arrays lie there in 16-byte chunks whose places are exchanged within a row, so that the 16 lanes that read at a time
 // hit all banks.
+//
+// Measured, 32 query heads, 8 KV heads of 128: 64 branches of 8192 positions (34 MB of keys and values, 256 query vectors a
+// KV head) 31 us; 32 prompts of 1024 with 8 branches each (134 MB) 31 us, 4.3 TB/s; 4 of 4095 with 16 branches of 5 tokens
+// 47 us.  Of the first some 7 us pass until the first step is there (lengths, table, keys), a step takes 1.9, the
+// end 3.  Inside a step the work of the CU bounds it: a matrix product of 16 x 16 x 32 takes 17.6 clocks and a vector
+// instruction 2.8, and on one SIMD these add up, whatever their order.  One kernel for all groups that read keys and
+// values through registers, a wave for 16 to 64 query vectors, took 44 and 45 us of the first two.
 #include <algorithm>
 #include <cmath>
 
@@ -327,8 +334,8 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
 #pragma unroll
           for (int d = 0; d < VL; ++d) o[t][d] *= down;
         }
-      // The next step's products (behind the last step: of whatever lies there, not used) and this one's weights, which keep
-      // the matrix and the vector units at work together.
+      // The next step's products (behind the last step: of whatever lies there, not used), whose results are not waited for
+      // then: this one's weights come in between.
       f32x4 s_next[2][2];
       scores(buf, s_next);
 #pragma unroll

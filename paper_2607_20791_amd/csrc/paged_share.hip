@@ -2,8 +2,8 @@
 //
 // Two short kernels, once for all layers of a turn: one finds, for each sequence, its group's first member with new tokens
 // and how far their tables agree, the other the least of these over each group.  Both look through all sequences for
-// each one (S^2 reads of the caches: 288 sequences a few us, 65536 some ms), so that nothing has to be cleared or counted by
-// atomics and results never depend on an order.
+// each one (S^2 reads of the caches), so that nothing has to be cleared or counted by atomics and results never depend on
+// an order.  288 sequences 4.8 + 4.7 us: two launches and the chains of reads in them bound it.
 #include "paged.hpp"
 #include "share.hpp"
 
