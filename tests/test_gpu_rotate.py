@@ -218,3 +218,10 @@ def test_binding_refuses_wrong_tensors(rgd):
                dict(layer=5), dict(layer=1 << 33), dict(eps=-1.0), dict(rotary=rgd.Rotary(128, 1e4)), dict(q=good["q_out"][:, :, ::2])):
         with pytest.raises(rgd.RGDError):
             rgd.paged_append_rotated(x.c, **{**good, **kw})
+
+
+@pytest.mark.parametrize("bf16,D,hk,n", [(True, 32, 3, 190), (False, 128, 4, 100), (True, 64, 6, 150)])
+def test_more_tokens_than_the_chip_holds(rgd, bf16, D, hk, n):
+    """Enough blocks of positions that a workgroup takes several KV heads."""
+    x, new = _case(rgd, 64, n, D=D, hk=hk, bf16=bf16, seed=n)
+    _run(rgd, x, n, new, D, interleaved=hk == 6, in_place=hk == 4, stride=8, G=1)

@@ -380,3 +380,41 @@ def test_own_parts_around_every_length(rgd, bf16, n, d, many):
     x, group = _forks(rgd, [32 if bf16 else 48] * (7 if many else 1), len(steps), [n + t for t in steps], [n, 1], hk=hk, d=d, bf16=bf16, layers=1,
                       seed=n + d)
     _attend(x, 0, hk * 3, n, x.new, group)
+
+
+@pytest.mark.parametrize("bf16,n,hk,G,d", [(True, 300, 1, 4, 64), (False, 260, 1, 2, 32), (True, 1024, 1, 1, 32)])
+def test_pieces_of_prompts(rgd, bf16, n, hk, G, d):
+    x, group = _forks(rgd, [50, 33], 2, [n, n + 9], [n, n - 7, 1, n], hk=hk, d=d, bf16=bf16, layers=1, seed=n)
+    _attend(x, 0, hk * G, n, x.new, group)
+
+
+def test_two_captured_turns_share_plan_and_workspace(rgd):
+    """Graphs of one token and of three, of one cache, over the same plan and workspace, replayed in turn."""
+    t = torch()
+    x, group = _forks(rgd, [200, 90], 4, [3, 30, 400], [1], hk=2, d=64, seed=13)
+    g = _i32(group)
+    size = lambda f: max(f(x.c, n, 8) for n in (1, 3))  # noqa: E731
+    plan = t.empty(size(rgd.paged_share_bytes), dtype=t.uint8, device="cuda")
+    ws = t.empty(size(rgd.paged_attention_shared_workspace_bytes), dtype=t.uint8, device="cuda")
+    turns = []
+    for n in (1, 3):
+        q = t.randn(x.S * n, 8, 64, device="cuda").bfloat16()
+        out = t.zeros(x.S * n, 512, device="cuda").bfloat16()
+
+        def turn(n=n, q=q, out=out):
+            rgd.paged_share(x.c, n, None, 8, g, plan)
+            rgd.paged_attention_shared(x.c, 0, q, n, plan, ws, out)
+
+        turn()
+        t.cuda.synchronize()
+        want = out.clone()
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph):
+            turn()
+        turns.append((graph, out, want, q))  # q: the graph reads it
+    for i in (0, 1, 1, 0, 1, 0):
+        turns[0][1].zero_(), turns[1][1].zero_()
+        plan.fill_(255), ws.fill_(255)
+        turns[i][0].replay()
+        t.cuda.synchronize()
+        assert t.equal(turns[i][1], turns[i][2]) and not turns[1 - i][1].any()

@@ -244,3 +244,37 @@ def test_binding_refuses_wrong_tensors(rgd):
                dict(logp=out), dict(logp=u), dict(z=z[:1].expand(3, 100))):
         with pytest.raises(rgd.RGDError):
             rgd.sample_truncated(**{**good, **kw})
+
+
+@pytest.mark.parametrize("R,V", [(1024, 300), (1025, 300), (2500, 77)])
+def test_more_rows_than_are_taken_at_a_time(rgd, R, V):
+    z, u, r = _rows(R, R, V)
+    pick = lambda *a: r.choice(a, R)  # noqa: E731
+    _compare(rgd, z, u, T=pick(0.0, 0.5, 1.0), k=pick(0, 1, 10, 60), p=pick(1.0, 0.5, 0.9), m=pick(0.0, 0.05))
+
+
+def test_two_captured_calls_share_a_workspace(rgd):
+    """Graphs of different sizes over one workspace, replayed in turn with eager calls between."""
+    t = torch()
+    calls = []
+    for R, V in ((3, 5000), (70, 900)):
+        z, u, r = _rows(R, R, V)
+        calls.append((_gpu(z), _gpu(u), t.empty(R, dtype=t.int32, device="cuda"), _gpu(r.choice([0.5, 0.9], R))))
+    ws = t.empty(max(rgd.sample_truncated_workspace_bytes(*c[0].shape) for c in calls), dtype=t.uint8, device="cuda")
+    want, graphs = [], []
+    for z, u, out, p in calls:
+        rgd.sample_truncated(z, u, ws, out, top_p=p)
+        t.cuda.synchronize()
+        want.append(out.clone())
+        graph = t.cuda.CUDAGraph()
+        with t.cuda.graph(graph):
+            rgd.sample_truncated(z, u, ws, out, top_p=p)
+        graphs.append(graph)
+    for i in (0, 1, 1, 0, 1, 0):
+        for c in calls:
+            c[2].fill_(-9)
+        ws.fill_(255)
+        graphs[i].replay()
+        t.cuda.synchronize()
+        assert t.equal(calls[i][2], want[i])
+        assert (calls[1 - i][2] == -9).all()
