@@ -21,6 +21,15 @@ namespace {
 
 constexpr int kFill = 768;  // workgroups that the chip holds
 
+// Where the other value of a pair is: in the same lane; eight lanes on of sixteen, one place of it; in one other lane, in the
+// same place; or anywhere in the row.
+enum Partner { kSame, kAcross, kLane, kAny };
+template <typename T>
+Partner partner_of(int D, int dim, int interleaved) {
+  constexpr int E = 16 / sizeof(T);
+  return interleaved || dim == 0 ? kSame : dim == D && D == 16 * E ? kAcross : dim / 2 % E == 0 ? kLane : kAny;
+}
+
 // The sum of neighbouring lanes' values, in each of them.
 template <int LANES>
 RGD_DEV float sum_lanes(float v) {
@@ -41,12 +50,12 @@ RGD_DEV float sum_lanes(float v) {
 // reads that one's sines and cosines once, and takes every few of its rows, kAhead of which are on their way (the case
 // above: four 33 us, two 38, one 41; in 128 registers, some of them in memory, 38).  Angles are taken once for the heads
 // of a workgroup, so it takes as many as leave the chip full: one KV head per workgroup 44 us, two 41, four 33, eight 49.
-template <typename T, int D>
+template <typename T, int D, Partner P>
 __global__ __launch_bounds__(256, 3) void rotate_append_kernel(RotateArgs a) {
-  constexpr int E = 16 / sizeof(T), kLanes = D / E, kRows = 256 / kLanes, kAhead = 4, kV = (16 * kLanes + 255) / 256;
+  constexpr int E = 16 / sizeof(T), kLanes = D / E, kRows = 256 / kLanes, kAhead = 6, kV = (16 * kLanes + 255) / 256;
   __shared__ T vt[2][D][16 + E];
   __shared__ float2 turn[16][D / 2 + 1];  // (cos, sin) of a position and pair
-  __shared__ float rows[kRows][D];
+  __shared__ float rows[P == kAny ? kRows : 1][D];
   const PagedView& c = a.c;
   const int s = blockIdx.x / a.blocks, heads = a.heads, g0 = blockIdx.y * heads, G = a.G;
   const int m = a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n;
@@ -106,20 +115,19 @@ __global__ __launch_bounds__(256, 3) void rotate_append_kernel(RotateArgs a) {
   }
   __syncthreads();
 
-  const bool whole = half % E == 0;               // a lane's partners are one lane's
-  const bool across = kLanes == 16 && a.dim == D; // which is eight lanes on of sixteen
   const int partner = ((int)threadIdx.x & 63) + (d < half ? half / E : -(half / E));
-  float* mine = rows[threadIdx.x / kLanes];
+  float* mine = rows[P == kAny ? threadIdx.x / kLanes : 0];
+  const int dim = P == kAcross ? D : a.dim;
   for (int t = t0; t < count; t += abreast) {
     if (t != t0) fetch(t);
     float cs[E], sn[E];  // x' = x cos + partner sin
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      if (d + e >= a.dim) continue;
-      const int j = a.interleaved ? (d + e) / 2 : d + e < half ? d + e : d + e - half;
+      if (d + e >= dim) continue;
+      const int j = P == kSame ? (d + e) / 2 : d + e < half ? d + e : d + e - half;
       const float2 w = turn[t][j];
       cs[e] = w.x;
-      sn[e] = (a.interleaved ? e % 2 == 0 : d + e < half) ? -w.y : w.y;
+      sn[e] = (P == kSame ? e % 2 == 0 : d + e < half) ? -w.y : w.y;
     }
     for (int h1 = h0; h1 < all; h1 += kAhead * hs)
 #pragma unroll
@@ -138,39 +146,37 @@ __global__ __launch_bounds__(256, 3) void rotate_append_kernel(RotateArgs a) {
 #pragma unroll
           for (int e = 0; e < E; ++e) x[e] = x[e] * inv * (h < queries ? gain[0][e] : gain[1][e]);
         }
-        if (half) {
-          float other[E];
-          if (a.interleaved) {
+        float other[E];
+        if constexpr (P == kSame) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) other[e] = x[e ^ 1];
-          } else if (across) {
+          for (int e = 0; e < E; ++e) other[e] = x[e ^ 1];
+        } else if constexpr (P == kAcross) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-              const int i = __float_as_int(x[e]);
-              other[e] = __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x128, 0xf, 0xf, false));
-            }
-          } else if (whole) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) other[e] = __shfl(x[e], partner, 64);
-          } else {
-#pragma unroll
-            for (int e = 0; e < E; ++e) mine[d + e] = x[e];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a row's lanes read what its lanes wrote
-            __builtin_amdgcn_wave_barrier();
-#pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (d + e < a.dim) other[e] = mine[d + e < half ? d + e + half : d + e - half];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next row's
-            __builtin_amdgcn_wave_barrier();
+          for (int e = 0; e < E; ++e) {
+            const int i = __float_as_int(x[e]);
+            other[e] = __int_as_float(__builtin_amdgcn_update_dpp(i, i, 0x128, 0xf, 0xf, false));
           }
-          if (d + E <= a.dim) {
+        } else if constexpr (P == kLane) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) x[e] = x[e] * cs[e] + other[e] * sn[e];
-          } else {
+          for (int e = 0; e < E; ++e) other[e] = __shfl(x[e], partner, 64);
+        } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-              if (d + e < a.dim) x[e] = x[e] * cs[e] + other[e] * sn[e];
-          }
+          for (int e = 0; e < E; ++e) mine[d + e] = x[e];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // a row's lanes read what its lanes wrote
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (d + e < dim) other[e] = mine[d + e < half ? d + e + half : d + e - half];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // before the next row's
+          __builtin_amdgcn_wave_barrier();
+        }
+        if (d + E <= dim) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = x[e] * cs[e] + other[e] * sn[e];
+        } else if constexpr (P == kSame || P == kAny) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (d + e < dim) x[e] = x[e] * cs[e] + other[e] * sn[e];
         }
         u32x4 res;
         if constexpr (E == 8) res = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
@@ -206,13 +212,24 @@ __global__ __launch_bounds__(256, 3) void rotate_append_kernel(RotateArgs a) {
   }
 }
 
-template <typename T>
+template <typename T, int D>
 void rotate_append(const RotateArgs& a, hipStream_t s) {
   const dim3 grid(a.blocks * a.c.S, a.c.Hkv / a.heads);
+  switch (partner_of<T>(D, a.dim, a.interleaved)) {
+    case kSame: hipLaunchKernelGGL((rotate_append_kernel<T, D, kSame>), grid, dim3(256), 0, s, a); break;
+    case kAcross:
+      if constexpr (D * sizeof(T) == 256) hipLaunchKernelGGL((rotate_append_kernel<T, D, kAcross>), grid, dim3(256), 0, s, a);
+      break;
+    case kLane: hipLaunchKernelGGL((rotate_append_kernel<T, D, kLane>), grid, dim3(256), 0, s, a); break;
+    case kAny: hipLaunchKernelGGL((rotate_append_kernel<T, D, kAny>), grid, dim3(256), 0, s, a);
+  }
+}
+template <typename T>
+void rotate_append(const RotateArgs& a, hipStream_t s) {
   switch (a.c.D) {
-    case 32: hipLaunchKernelGGL((rotate_append_kernel<T, 32>), grid, dim3(256), 0, s, a); break;
-    case 64: hipLaunchKernelGGL((rotate_append_kernel<T, 64>), grid, dim3(256), 0, s, a); break;
-    default: hipLaunchKernelGGL((rotate_append_kernel<T, 128>), grid, dim3(256), 0, s, a);
+    case 32: return rotate_append<T, 32>(a, s);
+    case 64: return rotate_append<T, 64>(a, s);
+    default: return rotate_append<T, 128>(a, s);
   }
 }
 
