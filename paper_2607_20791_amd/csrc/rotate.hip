@@ -3,9 +3,9 @@
 //
 // y = x / sqrt(mean(x^2) + eps) * gain for each head of q and k; the pair (a, b) of the first `dim` dimensions becomes
 // scale (a cos - b sin, b cos + a sin) of the angle position * freq.  Reading the rows once and writing them once bounds
-// it from below, at 5.35 TB/s; the operations on a row, some 80 a lane, take two thirds of the time of that.  8 x 1000
-// tokens of 32 + 8 + 8 heads of 128 in bf16, 109 MB: 33 us, 3.3 TB/s.  One token: 7.3 us, of which the launch and three
-// loads that need one another's results are most.
+// it from below, at 5.35 TB/s; the operations on a row, some 110 a lane, are the greater part of the rest.  8 x 1000 tokens
+// of 32 + 8 + 8 heads of 128 in bf16, 109 MB: 26 us in the trace, 4.1 TB/s (32 a call).  One token: 5.9 us (7.6 a call), of
+// which the launch and three loads that need one another's results are most.
 //
 // An angle enters as a part of a turn: position * (freq / 2 pi) and its distance from the nearest whole number in fp64
 // (2^31 positions lose 2^-23 of a turn at most), the rest in fp32, where sine and cosine of a part in [-1/2, 1/2] are
@@ -19,7 +19,7 @@ namespace rgd {
 
 namespace {
 
-constexpr int kFill = 768;  // workgroups that the chip holds
+constexpr int kFill = 768;  // workgroups that the chip holds, three per CU
 
 // Where the other value of a pair is: in the same lane; eight lanes on of sixteen, one place of it; in one other lane, in the
 // same place; or anywhere in the row.
@@ -47,9 +47,9 @@ RGD_DEV float sum_lanes(float v) {
 
 // One workgroup per (16 positions that lie together in a page, `heads` KV heads, sequence): the KV heads' k and v and the
 // query heads that read them.  A row is D / E neighbouring lanes with 16 bytes each; a thread keeps to one position, so it
-// reads that one's sines and cosines once, and takes every few of its rows, kAhead of which are on their way (the case
-// above: four 33 us, two 38, one 41; in 128 registers, some of them in memory, 38).  Angles are taken once for the heads
-// of a workgroup, so it takes as many as leave the chip full: one KV head per workgroup 44 us, two 41, four 33, eight 49.
+// reads that one's sines and cosines once, and takes every few of its rows, kAhead of which are on their way (a call of
+// the case above: four 35 us, six 32, eight 33, ten 33.5).  Angles are taken once for the heads of a workgroup, so it
+// takes as many as leave the chip full: one KV head per workgroup 44 us, two 41, four 33, eight 49, all with four rows.
 template <typename T, int D, Partner P>
 __global__ __launch_bounds__(256, 3) void rotate_append_kernel(RotateArgs a) {
   constexpr int E = 16 / sizeof(T), kLanes = D / E, kRows = 256 / kLanes, kAhead = 6, kV = (16 * kLanes + 255) / 256;
