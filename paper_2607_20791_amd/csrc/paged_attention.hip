@@ -1086,14 +1086,16 @@ int runs_for(const PagedView& c, int vectors) {
 
 template <typename T, int D, int NT, int MODE>
 hipError_t launch(const PagedAttnArgs& a, int vectors, hipStream_t s) {
-  const int runs = runs_for(a.c, vectors);
+  // no runs where the table holds no own part that is too long for a tail (2 sequences, 100 shared positions: 22 -> 20 us)
+  const int runs = MODE == OWN && a.c.width * a.c.ps <= kTailSteps * kStep ? 0 : runs_for(a.c, vectors);
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,
   // pages of 64: 109 us, 96 without.  (K past the caches, too: 48 and 109; K alone: 50 and 99.)
-  if (MODE != SHARED && a.c.ps <= Piece<T, D, NT, true, MODE>::PER)
-    hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs), dim3(256), 0, s, a, runs);
-  else
+  if (MODE != SHARED && a.c.ps <= Piece<T, D, NT, true, MODE>::PER) {
+    if (runs > 0) hipLaunchKernelGGL((attn_run_kernel<T, D, NT, true, MODE>), dim3(runs), dim3(256), 0, s, a, runs);
+  } else if (runs > 0) {
     hipLaunchKernelGGL((attn_run_kernel<T, D, NT, false, MODE>), dim3(runs + (MODE == SHARED)), dim3(256), 0, s, a, runs);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   if (MODE == SHARED) return hipSuccess;
   const int cols = std::min(16 * NT, a.n * a.G);
