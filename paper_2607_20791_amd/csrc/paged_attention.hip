@@ -478,10 +478,10 @@ struct Piece {
     load_v(a);
   }
 
-  // One round of positions from p0 on, any of which may be masked, whose K and V are on their way; leaves those of p1 on
-  // theirs.  lim: positions that a column sees, least of all.
+  // One round of positions from p0 on, any of which may be masked, whose K and V are on their way; the next round's K is
+  // asked for in between.  lim: positions that a column sees, least of all.
   template <class LoadK>
-  RGD_DEV void take(const PagedAttnArgs& a, const Seq& sq, const int (&lim)[NT], int least, int p0, float scale, LoadK&& next) {
+  RGD_DEV void take(const Seq& sq, const int (&lim)[NT], int least, int p0, float scale, LoadK&& next) {
     f32x4 s4[NT][NB];
     scores(s4);
     const int here = ok;
@@ -489,7 +489,6 @@ struct Piece {
     next();
     __builtin_amdgcn_sched_barrier(0);
     const int pos = p0 + grp * E;  // of this lane's first score
-// of this lane's first score
     const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
     bool odd = false;
     if (here != (1 << NB) - 1 || p0 + PER > sq.len) {
@@ -499,7 +498,7 @@ struct Piece {
     }
     if (least < min(p0 + PER, sq.len)) {  // not every column sees every value
 #pragma unroll
-      for (int d = 0; d < VL; ++d) odd = odd || any_nonfinite<T>(v[d]);
+      for (int d = 0; d < VL; ++d) odd |= any_nonfinite<T>(v[d]);
     }
     float p[NT][E];
     u32x4 hi[NT], lo[NT];
@@ -566,7 +565,7 @@ struct Piece {
     load_v(a);
     for (int p0 = first; p0 < end; p0 += by) {
       const bool more = p0 + by < end;
-      take(a, sq, lim, least, p0, scale, [&] {
+      take(sq, lim, least, p0, scale, [&] {
         row = more ? row0 : 0;
         grp = more ? grp0 : 0;
         load_k(a, it.g, more ? p0 + by : p0);
