@@ -41,6 +41,7 @@ constexpr int kFine = 64;          // bins per octave
 constexpr int kBins = kOctaves * kFine;
 constexpr int kReach = kBins + kFine;  // bins below its maximum that a workgroup counts
 constexpr int kRing = 8192;        // bins are counted modulo this
+constexpr float kLowest = -3.402823466e38f;  // -inf is never an id that weighs something, however large T is
 constexpr float kFar = 524288.f;   // 2^19 bins from 0: up to there, three roundings of fp32 are within 1/8 of a bin
 constexpr int kNear = 4096;        // listed ids that the last pass holds in LDS
 constexpr int kList = 16384;       // of a row, about
@@ -111,7 +112,7 @@ struct Weigher {
 
 RGD_DEV Weigher weigher(float top, float T) {
   // ids below `low` weigh nothing: the float nearest to 46 octaves down has none beyond 45 above it, whatever T is
-  return Weigher{top, 1.4426950408889634 / (double)T, fmaxf(top - 46.f * 0.6931472f * T, -3.402823466e38f)};
+  return Weigher{top, 1.4426950408889634 / (double)T, fmaxf(top - 46.f * 0.6931472f * T, kLowest)};
 }
 
 // The sum over the wave, in its last lane (without LDS, which is short of time here).
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(kThreads, 8) void truncate_count_kernel(Job j) {
         if (lane == 0) red[0][wave] = most;
         __syncthreads();
         for (int i = 0; i < kWaves; ++i) first = fmaxf(first, red[0][i]);
-        low = first > -INFINITY ? first - kReach / per : INFINITY;
+        low = first > -INFINITY ? fmaxf(first - kReach / per, kLowest) : INFINITY;
       }
       if (c < j.chunks)
 #pragma unroll
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(kThreads, 8) void truncate_count_kernel(Job j) {
     for (int i = 0; i < kWaves; ++i) most = fmaxf(most, red[1][i]);
     if (!((most - first) * per > 2000.f)) break;  // (-inf - -inf: no)
     // what came first lies far below the rest: again, from the maximum
-    low = most - kReach / per;
+    low = fmaxf(most - kReach / per, kLowest);
     for (int i = t; i < kRing; i += kThreads) bins[i] = 0;
     __syncthreads();
   }

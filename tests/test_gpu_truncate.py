@@ -278,3 +278,18 @@ def test_two_captured_calls_share_a_workspace(rgd):
         t.cuda.synchronize()
         assert t.equal(calls[i][2], want[i])
         assert (calls[1 - i][2] == -9).all()
+
+
+@pytest.mark.parametrize("V", [300, 30000])
+def test_banned_ids_at_temperatures_near_the_largest(rgd, V):
+    """T of 2^124 and more, where the range of logits that weigh anything ends below what fp32 holds: -inf weighs nothing."""
+    r = np.random.default_rng(V)
+    T = np.array([2e37, 5e37, 1e38, 2e37, 5e37, 1e38])
+    z = r.standard_normal((6, V)) * T[:, None] / 2
+    z = np.where(r.random(z.shape) < 0.7, -np.inf, np.clip(z, -3e38, 3e38)).astype(np.float32)
+    least = np.exp((0.1 * T - z.max(1)) / T)  # min_p's border, a little above 0 and below top_p's
+    for u in (r.random(6), np.full(6, 0.995)):
+        for m in (None, least, np.array([0.2, 0.5, 0.3, 0.05, 0.6, 0.9])):
+            _compare(rgd, z, u, T=T, p=np.full(6, 0.2), m=m)
+            _compare(rgd, z, u, T=T, k=[3, V // 5, V // 4, 40, 7, 1], m=m)
+            _compare(rgd, z, u, T=T, k=[30, V // 5, V // 4, 40, 70, 10], p=[0.5, 0.6, 0.7, 0.8, 0.9, 0.3], m=m)
