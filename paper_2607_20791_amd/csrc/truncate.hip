@@ -57,7 +57,7 @@ struct RowInfo {
   float top, T;
   uint32_t least;      // key of the lowest logit that min_p keeps
   int mode;            // below
-  int by_k, by_p;      // whether these limits cut anything
+  int by_k, by_p;      // whether these limits cut anything; by_p of kBelow: only if what the others keep weighs too much
   float k_low, k_end;  // the ids from k_low up to below k_end are listed: top_k's border is among them
   float p_low, p_end;  // top_p's; infinite where there is no such limit, as top_k's
   float kept;          // ids from here on are kept for certain
@@ -65,6 +65,7 @@ struct RowInfo {
   float low;           // what is below concerns nothing
 };
 enum { kNone, kGreedy, kDraw };
+constexpr int kBelow = 2;
 
 struct Job {
   TruncateArgs a;
@@ -297,6 +298,7 @@ struct Found {
   unsigned count[kWaves];
   int k, p0, p1;
   float ahead;    // estimate of what top_p's border refers to
+  float most[kWaves];  // of what min_p keeps
 };
 
 // The bins of the borders, one workgroup a row, from the counts: a bin's weight is that of its middle, within half of 1/64
@@ -446,12 +448,33 @@ RGD_DEV RowInfo find_bins(const Job& j, int r, Found& sh) {
     if (sh.p0) in.p_end = logit(sh.p0, 1.2f);
   }
   if (!in.by_p && !in.by_k) return in;  // fewer than top_k weigh anything
-  if (least >= (in.by_p ? in.p_end : in.k_end)) {  // min_p's border is above the others
+  bool above = least >= (in.by_p ? in.p_end : in.k_end);  // min_p's border above the others
+  if (above && in.by_p) {
+    // For top_p that is an estimate, whose error equal logits share.  Certain is that an id weighs its bin's middle times 2^(1/128) at
+    // most, or a little more (a fifth of a bin) for the roundings of z * per, and as much less at least: within 1%
+    // with those of the sums.  Otherwise what min_p keeps is weighed and compared at the end.
+    float most = 0.f;
+    const float bin = (float)top_bin - (floorf(least * per) - 1.f);  // of the lowest id that it may keep
+#pragma unroll
+    for (int i = 0; i < PER; ++i) most += (float)(t * PER + i) <= bin ? count[i] * weight[i] : 0.f;
+    most = wave_sum(most);
+    if (lane == 0) sh.most[wave] = most;
+    __syncthreads();
+    most = 0.f;
+    for (int i = 0; i < kWaves; ++i) most += sh.most[i];
+    above = most * 1.01f < a.top_p[r] * (total * 0.99f) && (!in.by_k || least >= in.k_end);
+    if (!above) {
+      in.by_p = kBelow;
+      in.p_low = in.p_end = INFINITY;
+    }
+  }
+  if (above) {
     in.by_k = in.by_p = 0;
     in.k_low = in.k_end = in.p_low = in.p_end = INFINITY;
     return in;
   }
-  in.kept = fmaxf(in.kept, in.by_p ? in.p_end : in.k_end);
+  if (in.by_p != kBelow) in.kept = fmaxf(in.kept, in.by_p ? in.p_end : in.k_end);
+  else if (in.by_k) in.kept = fmaxf(in.kept, in.k_end);
   if (in.by_p) in.whole = in.by_k ? fmaxf(in.k_end, floor_z) : floor_z;
   in.low = fminf(fminf(in.kept, in.whole), fminf(in.p_low, in.k_low));
   return in;
@@ -876,7 +899,7 @@ __global__ __launch_bounds__(kThreads) void truncate_draw_kernel(Job j) {
     const u64 kept = sh.kept;
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {  // top_k, top_p
-      if (which ? !in.by_p : !k) continue;
+      if (which ? !in.by_p || in.by_p == kBelow : !k) continue;
       const float z0 = which ? in.p_low : in.k_low, z1 = which ? in.p_end : in.k_end;
       const u64 lo = z1 <= in.top ? order_of(key_of(z1), 0xFFFFF) + 1 : order_of(key_of(in.top), 0),
                 hi = order_of(key_of(z0), 0xFFFFF);
@@ -893,6 +916,13 @@ __global__ __launch_bounds__(kThreads) void truncate_draw_kernel(Job j) {
       for (int i = t; i < it.n; i += kThreads) {
         const u64 o = it.order_at(i);
         if (o <= border && (uint32_t)~(o >> 20) >= in.least) atomicAdd(&sh.chunk[(int)(o & 0xFFFFF) / kChunk], it.weight_at(i));
+      }
+      if (in.by_p == kBelow) {
+        // top_p keeps all of what the other limits keep where that weighs less than it may
+        __syncthreads();
+        u64 all = 0;
+        for (int c = t; c < j.chunks; c += kThreads) all += sh.chunk[c];
+        fine = (double)block_total(all, sh) < (double)top_p * (double)whole;
       }
     }
   }

@@ -293,3 +293,36 @@ def test_banned_ids_at_temperatures_near_the_largest(rgd, V):
             _compare(rgd, z, u, T=T, p=np.full(6, 0.2), m=m)
             _compare(rgd, z, u, T=T, k=[3, V // 5, V // 4, 40, 7, 1], m=m)
             _compare(rgd, z, u, T=T, k=[30, V // 5, V // 4, 40, 70, 10], p=[0.5, 0.6, 0.7, 0.8, 0.9, 0.3], m=m)
+
+
+def _min_p_above_top_p(seed):
+    """Rows of a few logits that many ids share: min_p keeps the highest of them, whose weight is within 1.5 per cent of
+    what top_p keeps, on either side.  (z, u, T, top_p, min_p)"""
+    r = np.random.default_rng(seed)
+    z, T, p, m = np.full((16, 18000), -np.inf, np.float32), np.empty(16), np.empty(16), np.empty(16)
+    for i in range(16):
+        T[i] = r.choice([0.5, 0.8, 1.0, 1.3])
+        values = r.integers(200, 400) / 8 - np.cumsum(np.concatenate([[0], r.integers(1, 5, 4)])) / 8
+        row = np.concatenate([np.full(r.integers(1000, 3000), v) for v in values] + [values[0] - 20 - 20 * r.random(2000)])
+        z[i, r.permutation(z.shape[1])[:len(row)]] = row
+        cut = r.integers(1, 4)  # values that min_p keeps
+        m[i] = np.exp(((values[cut - 1] + values[cut]) / 2 - values[0]) / T[i])
+        w = np.exp((z[i].astype(np.float64) - values[0]) / T[i])
+        p[i] = w[z[i] >= values[cut - 1]].sum() / w.sum() * (1 + r.uniform(-0.015, 0.015))
+    return z, r.choice([0.9999, 0.99999, 0.998, 0.5, 0.3], 16), T, p, m
+
+
+def test_min_p_above_an_estimate_of_top_ps_border(rgd):
+    """6000 ids of 33.125 behind 3000 of 33.375, of which top_p keeps 2988, and min_p all."""
+    r = np.random.default_rng(1)
+    z = r.permutation(np.concatenate([np.full(3000, 33.375), np.full(6000, 33.125), -7 + r.random(4000)]))[None].repeat(3, 0)
+    one = np.ones(3)
+    # u = 0.5 of 2988 equal weights is 1494 of them: on a border
+    out = _compare(rgd, z, [0.9999, 0.5, 0.997], T=0.8 * one, p=0.40427926 * one, m=0.85534531 * one, near=1)
+    assert out[0] == 12943  # u behind the twelve ids that top_p drops
+    for seed in range(6):
+        z, u, T, p, m = _min_p_above_top_p(seed)
+        # where an even number of equal logits is kept, n / 2 weights are u = 0.5 of n: on a border, in up to three of these rows
+        _compare(rgd, z, u, T=T, p=p, m=m, near=3)
+        _compare(rgd, z, u, T=T, k=r.choice([500, 3000, 9000, 13000], 16), p=p, m=m, near=3)
+
