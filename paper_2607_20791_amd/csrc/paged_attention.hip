@@ -92,10 +92,11 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int len, int m, int from) {
   q.tiles = (m * a.G + COLS - 1) / COLS;
   return q;
 }
-// What is left of a sequence of m tokens behind its shared positions; no tiles where that is the other mode's.
+// What is left of a sequence behind its shared positions; no tiles where that is the other mode's.  The plan's tokens and
+// shared positions may be any numbers where it is not this call's (most is 0): then there are no tokens, and no tiles.
 template <int COLS, int MODE>
-RGD_DEV Seq rest_of(const PagedAttnArgs& a, int len, int m, int shared) {
-  Seq q = seq_of<COLS>(a, len, m, min(shared, len / 16 * 16));
+RGD_DEV Seq rest_of(const PagedAttnArgs& a, int len, int tokens, int shared) {
+  Seq q = seq_of<COLS>(a, len, max(min(tokens, a.most), 0), min(max(shared, 0), len / 16 * 16));
   if ((q.steps <= kTailSteps) != (MODE == TAIL)) q.tiles = 0;
   return q;
 }
@@ -107,9 +108,9 @@ RGD_DEV Seq seq_of(const PagedAttnArgs& a, int s) {
     const Plan p(a.plan, a.c.S);
     if constexpr (MODE == SHARED) {
       const PlanGroup g = p.group[s];
-      return seq_of<COLS>(a, g.shared, a.most ? g.tokens : 0, 0);
+      return seq_of<COLS>(a, a.most ? g.shared : 0, a.most ? g.tokens : 0, 0);
     } else {
-      return rest_of<COLS, MODE>(a, paged_len(a.c, s), min(p.tokens[s], a.most), p.shared[s]);
+      return rest_of<COLS, MODE>(a, paged_len(a.c, s), p.tokens[s], p.shared[s]);
     }
   }
 }
@@ -125,10 +126,10 @@ RGD_DEV Seq uniform_seq(const PagedAttnArgs& a, int s) {
     const Plan p(a.plan, a.c.S);
     if constexpr (MODE == SHARED) {
       Scalar g = (Scalar)p.group + 4 * s;
-      return seq_of<COLS>(a, g[0], a.most ? g[1] : 0, 0);
+      return seq_of<COLS>(a, a.most ? g[0] : 0, a.most ? g[1] : 0, 0);
     } else {
       const int len = min(max(((Scalar)a.c.lens)[s], 0), a.c.width * a.c.ps);
-      return rest_of<COLS, MODE>(a, len, min(((Scalar)p.tokens)[s], a.most), ((Scalar)p.shared)[s]);
+      return rest_of<COLS, MODE>(a, len, ((Scalar)p.tokens)[s], ((Scalar)p.shared)[s]);
     }
   }
 }

@@ -418,3 +418,28 @@ def test_two_captured_turns_share_plan_and_workspace(rgd):
         turns[i][0].replay()
         t.cuda.synchronize()
         assert t.equal(turns[i][1], turns[i][2]) and not turns[1 - i][1].any()
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("hk,G", [(2, 3), (2, 4), (1, 8)])
+@pytest.mark.parametrize("width", [0, 400])
+def test_memory_that_is_no_plan_writes_nothing(rgd, bf16, hk, G, width):
+    """A plan of memory as it comes: floats below 0 are counts whose products with G pass 2^31, and random bytes."""
+    t = torch()
+    x, group = _forks(rgd, [100, 64], 4, [5, 20], [2], hk=hk, d=64, bf16=bf16, seed=14, width=width)
+    plan = t.empty(rgd.paged_share_bytes(x.c, 2, hk * G), dtype=t.uint8, device="cuda")
+    words = plan[:plan.numel() // 4 * 4].view(t.int32)
+    q = t.randn(2 * x.S, hk * G, 64, device="cuda").to(_dt(bf16))
+    ws = t.empty(rgd.paged_attention_shared_workspace_bytes(x.c, 2, hk * G), dtype=t.uint8, device="cuda").fill_(255)
+    out, lse = t.full((2 * x.S, hk * G * 64), 7.0, device="cuda").to(_dt(bf16)), t.full((2 * x.S, hk * G), 7.0, device="cuda")
+    pool = (x.c.pool_k.clone(), x.c.pool_v.clone())
+    for fill in (-10.0, -3.0, -2.5, -1.0, 1e30, None):
+        if fill is None:
+            plan.copy_(t.from_numpy(x.r.integers(0, 256, plan.numel()).astype(np.uint8)))
+        else:
+            words.copy_(t.full((words.numel(),), fill, device="cuda").view(t.int32))
+        rgd.paged_attention_shared(x.c, 0, q, 2, plan, ws, out, lse)
+        t.cuda.synchronize()
+        assert (out == 7).all() and (lse == 7).all(), fill
+    same = lambda a, b: bool(((a == b) | (t.isnan(a) & t.isnan(b))).all())  # noqa: E731
+    assert same(x.c.pool_k, pool[0]) and same(x.c.pool_v, pool[1])
