@@ -630,9 +630,9 @@ uint64_t rgd_sample_truncated_workspace_bytes(int32_t R, int32_t V);
  * [0, 1); outside as the nearest inside, NaN as 0) times the kept weight.  T dev fp32 [R] (NULL: 1); where it is 0,
  * negative or NaN the first maximum is drawn.  out dev int32 [R]; logp dev fp32 [R] or NULL: the logarithm of the drawn
  * id's share of the kept weight.  NaN logits count as -inf, which is never kept; a row whose maximum is not finite gives
- * -1 and -inf.  Weights are taken in 64 bits, to 2^-44 of the largest (less weighs nothing), and sums are of whole
- * multiples of 2^-43, so that they do not depend on their order: the draw is the exact one unless u or a limit meets the
- * border of two ids by about 2^-44 for each id.  The same row gives the same id in any batch.  1 <= R <= 65536,
+ * -1 and -inf.  Weights are taken in 64 bits, to 2^-46 of themselves and then to 2^-44 of the largest (less weighs nothing),
+ * and sums are of whole multiples of 2^-43, so that they do not depend on their order: the draw is the exact one unless u or a
+ * limit meets the border of two ids by 2^-43 of the largest weight for each id or less.  The same row gives the same id in any batch.  1 <= R <= 65536,
  * 1 <= V <= 2^20, ldz >= V.  out, logp and the workspace overlap neither each other nor an input.  Asynchronous. */
 int32_t rgd_sample_truncated(const float* z, int64_t ldz, int32_t R, int32_t V, const float* T, const int32_t* top_k,
                              const float* top_p, const float* min_p, const float* u, void* workspace, int32_t* out,

@@ -85,9 +85,10 @@ struct Job {
 };
 
 // ---------------------------------------------------------------- weights --
-// An id's weight 2^y, y = (z - top) log2(e) / T: with n the whole number next to y, 2^(y - n) by a polynomial on
-// [-1/2, 1/2] whose largest error is the least there is (1.1e-12 of the weight), rounded to a whole multiple of 2^-43.  (A table
-// of powers takes four products less, and LDS more time than these.)
+// An id's weight 2^y, y = (z - top) log2(e) / T: with n the whole number next to y, 2^(y - n) by a polynomial of degree 9 on
+// [-1/2, 1/2] whose largest error is the least there is (2^-46 of the weight; of degree 8 2^-40, more than the rounding),
+// rounded to a whole multiple of 2^-43, so that the largest one is 1.  (A table of powers takes four products less, and LDS more
+// time than these.)
 struct Weigher {
   double top, scale;
   float low;  // what is below weighs nothing
@@ -96,15 +97,16 @@ struct Weigher {
     constexpr double kRound = 6755399441055744.0;  // 1.5 * 2^52: a sum's last bit is 1
     constexpr double kUnit = 768.0;                // 1.5 * 2^9: a sum's last bit is 2^-43
     const double d = (double)z - top, t = fma(d, scale, kRound), f = fma(d, scale, -(t - kRound));
-    double s = 1.3344183711502877e-06;
-    s = fma(s, f, 1.5314209233330192e-05);
-    s = fma(s, f, 0.00015403098285418843);
-    s = fma(s, f, 0.0013333434157513703);
-    s = fma(s, f, 0.009618129558840722);
-    s = fma(s, f, 0.055504109592288735);
-    s = fma(s, f, 0.24022650694742584);
-    s = fma(s, f, 0.6931471805412327);
-    s = fma(s, f, 1.0);
+    double s = 1.0150336704816022e-07;
+    s = fma(s, f, 1.325940560926017e-06);
+    s = fma(s, f, 1.5252984838656468e-05);
+    s = fma(s, f, 0.00015403434948072205);
+    s = fma(s, f, 0.0013333557617604436);
+    s = fma(s, f, 0.009618129192067245);
+    s = fma(s, f, 0.05550410866868561);
+    s = fma(s, f, 0.24022650695649653);
+    s = fma(s, f, 0.693147180559871);
+    s = fma(s, f, 1.0000000000000127);
     s = __hiloint2double(__double2hiint(s) + (__double2loint(t) << 20), __double2loint(s));
     return (s + kUnit) - kUnit;
   }

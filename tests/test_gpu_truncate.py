@@ -326,3 +326,24 @@ def test_min_p_above_an_estimate_of_top_ps_border(rgd):
         _compare(rgd, z, u, T=T, p=p, m=m, near=3)
         _compare(rgd, z, u, T=T, k=r.choice([500, 3000, 9000, 13000], 16), p=p, m=m, near=3)
 
+
+
+@pytest.mark.parametrize("T", [1.0, 0.7, 2.5])
+def test_borders_as_near_as_the_weights_are_exact(rgd, T):
+    """Two ids, and every u or top_p among four million rows that lies nearer to their border than 6e-13 of the larger one's weight,
+    but not so near as the weights' rounding to 2^-44 (with their own error of 2^-46) can move it."""
+    T32 = np.float32(T)
+    low = -(np.arange(1 << 22, dtype=np.float32) + 1) * np.float32(2.0**-22) * T32  # weights from 1 down to 1 / e
+    w = np.exp(low.astype(np.float64) / float(T32))
+    for what in ("u", "p"):
+        border = w / (1 + w) if what == "u" else 1 / (1 + w)
+        x = border.astype(np.float32)
+        off = np.abs(border - x.astype(np.float64)) * (1 + w)
+        at = np.flatnonzero((off < 6e-13) & (off > 2.5e-13))
+        assert len(at) >= 20
+        z = np.stack([low[at], np.zeros(len(at), np.float32)], 1)
+        on = np.full(len(at), T)
+        if what == "u":
+            _compare(rgd, z, x[at], T=on)
+        else:
+            _compare(rgd, z, np.zeros(len(at)), T=on, p=x[at])  # the lower id only if top_p keeps it
