@@ -4,7 +4,7 @@
 // A group's query vectors (its sequences' tokens x query heads of a KV head) all see all of its shared positions, so no score is
 // masked but those of pages that are not there.  128 of them are an item; the positions of all items lie one behind the
 // other in steps of 64, and every workgroup takes an equal run of steps.  Where a run enters or leaves an item it leaves
-// a piece: sums weighted against the piece's own maximum, which the second part joins.
+// a piece: sums weighted against a reference of the piece's own, which the second part joins.
 //
 // Many query vectors read the same keys and values, so these come to LDS once for a workgroup, by copies that pass no
 // register, three steps ahead of the products.  Of the eight waves four share out the query vectors, 32 each (two tiles
@@ -321,14 +321,14 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
       for (int t = 0; t < 2; ++t) {
         const float* y = x[t];
         top[t] = scale * fmaxf(fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])), fmaxf(fmaxf(y[4], y[5]), fmaxf(y[6], y[7])));
-        moves = moves || top[t] > m[t] + kLazy;
+        moves = moves || top[t] > m[t];
       }
       if (__any(moves))
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           top[t] = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
           top[t] = fmaxf(top[t], __shfl_xor(top[t], 32, 64));
-          const float nm = fmaxf(m[t], top[t]), down = exp2_raw(m[t] - nm);
+          const float nm = fmaxf(m[t], top[t] + kLazy), down = exp2_raw(m[t] - nm);
           m[t] = nm;
           l[t] *= down;
 #pragma unroll
@@ -340,12 +340,13 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
       scores(buf, s_next);
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float ref = m[t] + kLazy;  // weights are over kLift, 2^kLazy
+        // A weight is 2^(score - m), whose exponent is rounded once, at its own size; no score is above m, which moves to kLazy
+        // above the one that passes it, so no weight is above 1.
         float w[8], sum = 0.f;
         u32x4 hi, lo;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          w[j] = exp2_raw(fmaf(x[t][j], scale, -ref));
+          w[j] = exp2_raw(fmaf(x[t][j], scale, -m[t]));
           sum += w[j];
         }
         l[t] += sum;
@@ -388,7 +389,8 @@ __global__ __launch_bounds__(512, 2) void group_run_kernel(PagedAttnArgs a, int 
       const int col = cg * 32 + t * 16 + row;
       if (pg == t && col < cols) {
         const float2 ml = ml_s[c];
-        const float nm = fmaxf(m[t], ml.x), f0 = exp2_raw(m[t] - nm), f1 = exp2_raw(ml.x - nm);
+        // (over kLift, as all pieces are)
+        const float nm = fmaxf(m[t], ml.x), f0 = exp2_raw(m[t] - nm) * (1.f / kLift), f1 = exp2_raw(ml.x - nm) * (1.f / kLift);
 #pragma unroll
         for (int d = 0; d < VL; ++d) {
           const f32x4 x = *(const f32x4*)(part + c * D + ((d * 4 + grp) ^ (c & (D / 4 - 1) & 15)) * 4);

@@ -443,3 +443,41 @@ def test_memory_that_is_no_plan_writes_nothing(rgd, bf16, hk, G, width):
         assert (out == 7).all() and (lse == 7).all(), fill
     same = lambda a, b: bool(((a == b) | (t.isnan(a) & t.isnan(b))).all())  # noqa: E731
     assert same(x.c.pool_k, pool[0]) and same(x.c.pool_v, pool[1])
+
+
+@pytest.mark.parametrize("bf16", [True, False])
+@pytest.mark.parametrize("power", [0, 10, 16, 17, 20])
+def test_large_scores_of_shared_positions(rgd, bf16, power):
+    """Queries and keys of whole numbers, so that products are exact: scores around 2^power (in units of log 2), whose spacing in fp32 is
+    2^-4 at the last, and whose distances from the maximum, which is all that a weight depends on, are small."""
+    t = torch()
+    d, hk, G = 64, 1, 8
+    x, group = _forks(rgd, [320, 200], 4, [9, 40, 70], [1], hk=hk, d=d, bf16=bf16, seed=power, layers=1)
+    # score = 32768 k0 + 128 k1 + k2 + offset of the head, times log2(e) / 8
+    aim = int(round((2.0**power - 4) / (np.log2(np.e) / 8)))
+    k = np.zeros((x.n_pages, hk, x.ps, d), np.float32)
+    k[..., 0], k[..., 1] = aim // 32768, aim % 32768 // 128
+    k[..., 2] = aim % 128 + x.r.integers(-20, 21, k.shape[:-1])
+    k[..., 3] = 1
+    x.c.pool_k[0] = t.where(t.isnan(x.c.pool_k[0]), x.c.pool_k[0], t.from_numpy(k).cuda().to(_dt(bf16)))
+    q = np.zeros((x.S, hk * G, d), np.float32)
+    q[..., 0], q[..., 1], q[..., 2] = 32768, 128, 1
+    q[..., 3] = np.linspace(-40, 40, hk * G).round()
+    q = t.from_numpy(q).cuda().to(_dt(bf16))
+    plan, shared = _plan(x, 1, None, hk * G, group)
+    assert shared.min() == 192
+    out, lse = t.zeros(x.S, hk * G * d, dtype=_dt(bf16), device="cuda"), t.zeros(x.S, hk * G, device="cuda")
+    ws = t.empty(rgd.paged_attention_shared_workspace_bytes(x.c, 1, hk * G), dtype=t.uint8, device="cuda").fill_(255)
+    rgd.paged_attention_shared(x.c, 0, q, 1, plan, ws, out, lse)
+    pages, pk, pv = x.c.pages.cpu().numpy(), _np(x.c.pool_k)[0], _np(x.c.pool_v)[0]
+    o, l, qn = _np(out).reshape(x.S, 1, hk * G, d), _np(lse).reshape(x.S, 1, hk * G), _np(q).reshape(x.S, 1, hk * G, d)
+    for s in range(x.S):
+        N = int(x.lens[s])
+        kk, v, there = op.gather(pk, pv, pages[s], N, x.ps)
+        ro, rl = op.attention(qn[s], kk, v, there, N - 1)
+        # a distance is at most 40 log2(e) / 8 < 8: rounded once, as its factor is, 2^-24 of it each in log2 units, and the
+        # exponential 2^-22; of a weight that comes twice into the output.  Two bf16 hold it to 2^-16; sums and joins as elsewhere
+        tol = (2.0**-8 if bf16 else 2.0**-24) * np.abs(ro) + (2 * (16 * 2.0**-24 + 2.0**-22) + 2.0**-15 * bf16 + 2 * (N + 64) * 2.0**-24) * np.abs(v).max()
+        assert (np.abs(o[s] - ro) <= tol).all(), (s, np.abs(o[s] - ro).max())
+        # lse: the maximum and the sum's logarithm are added and brought to base e, three roundings of its size, the maximum's own and its factor's
+        assert (np.abs(l[s] - rl) <= 5 * 2.0**-24 * (np.abs(rl) + 16) + (N + 64) * 2.0**-24).all(), (s, np.abs(l[s] - rl).max())
