@@ -572,13 +572,16 @@ def paged_attention(cache, layer, q, n, n_new, workspace, out, lse=None):
 # ------------------------------------------------- rotary positions, head norms --
 class RotaryScaling:
     """How a rotation's frequencies are changed by `factor` for positions beyond the trained `context`: kind "linear",
-    "base", "by_rotations" or "by_index" (the last two between `low` and `high` turns over the context)."""
+    "base", "by_rotations" or "by_index" (the last two between `low` and `high` turns over the context; high None: 4 turns by
+    rotations, 32 by index, as models trained with these have them)."""
 
     KINDS = ("linear", "base", "by_rotations", "by_index")
 
-    def __init__(self, kind, factor, context=0.0, low=1.0, high=4.0):
+    def __init__(self, kind, factor, context=0.0, low=1.0, high=None):
         if kind not in self.KINDS:
             _refuse(f"kind must be one of {', '.join(self.KINDS)}")
+        if high is None:
+            high = 32.0 if kind == "by_index" else 4.0
         self.desc = RotaryScalingDesc(1 + self.KINDS.index(kind), factor, context, low, high)
 
 

@@ -132,3 +132,12 @@ def test_refusals_of_rotations():
             rgd.Rotary(64, **kw)
     with pytest.raises(rgd.RGDError):
         rgd.RotaryScaling("cubic", 2.0)
+
+
+@pytest.mark.parametrize("kind,high", [("by_rotations", 4.0), ("by_index", 32.0)])
+def test_turns_that_are_not_given(kind, high):
+    """Each kind has its own usual number of turns from which on a frequency is kept."""
+    import paper_2607_20791_amd as rgd
+    f, _ = rotary.frequencies(128, 500000.0, kind, 8.0, 8192, 1.0, high)
+    for how in (rgd.RotaryScaling(kind, 8.0, 8192), rgd.RotaryScaling(kind, 8.0, 8192, high=high), rgd.RotaryScaling(kind, 8.0, 8192, 1.0, None)):
+        assert np.allclose(np.array(rgd.Rotary(128, 500000.0, scaling=how).freq[:64]), f, rtol=1e-13, atol=0)
