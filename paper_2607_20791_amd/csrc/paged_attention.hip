@@ -71,8 +71,8 @@ static_assert(2 * kTailSteps + 1 <= 64, "a tail's pages, of 16 positions at leas
 // New tokens of sequence s.
 RGD_DEV int new_tokens(const PagedAttnArgs& a, int s) { return a.n_new ? min(max(a.n_new[s], 0), a.n) : a.n; }
 
-// Floor of col / G for col < 2^20, G <= 1024: the product passes col / G by less than col / 2^31,
-// which is less than 1 / G.
+// Floor of col / G for col * G < 2^31: the product passes col / G by less than col / 2^31, which is less than 1 / G.
+// (A sequence's: below 2^20 * 2^10.  A group's: what the entry point lets through.)
 RGD_DEV int token_of(const PagedAttnArgs& a, int col) { return (int)__umulhi((unsigned)col << 1, a.inv_G); }
 
 struct Seq {
@@ -639,7 +639,8 @@ struct Piece {
         load_q(a, next);
         load_k(a, next.g, first);
       }
-      const int pos = p0 + grp * E;      const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
+      const int pos = p0 + grp * E;
+      const bool there = BF ? (here >> (grp >> 1)) & 1 : here & 1;
       bool odd = false;
       if (here != ALL || p0 + PER > sq.len) {
         const int held = there ? sq.len - pos : 0;

@@ -44,7 +44,7 @@ RGD_DEV Group group_of(const PagedAttnArgs& a, int len, int tokens, int row) {
   return Group{len, tokens, row, (len + kTile - 1) / kTile, (tokens * a.G + kCols - 1) / kCols};
 }
 
-// One item of a run: steps [t0, t1) of query vectors [64 qb, ...) of KV head g of the group of leader s.
+// One item of a run: steps [t0, t1) of query vectors [kCols qb, ...) of KV head g of the group of leader s.
 struct Item {
   Group gr;
   int s, g, qb, t0, t1, number;

@@ -39,6 +39,25 @@ constexpr int kResident = 5120;  // waves of pass 2 at a time: 20 per CU
 
 typedef float f4 __attribute__((ext_vector_type(4), aligned(4)));  // rows need no alignment
 
+// 2^x to 1e-14 for x <= 0: the Taylor series of 2^f, |f| <= 1/2, to f^11.
+RGD_DEV double exp2_f64(double x) {
+  x = fmax(x, -1100.0);  // below: 0 either way (and -inf - rint(-inf) is not a number)
+  const double n = rint(x), g = (x - n) * 0.6931471805599453;
+  double s = 1.0 / 39916800.0;
+  s = fma(s, g, 1.0 / 3628800.0);
+  s = fma(s, g, 1.0 / 362880.0);
+  s = fma(s, g, 1.0 / 40320.0);
+  s = fma(s, g, 1.0 / 5040.0);
+  s = fma(s, g, 1.0 / 720.0);
+  s = fma(s, g, 1.0 / 120.0);
+  s = fma(s, g, 1.0 / 24.0);
+  s = fma(s, g, 1.0 / 6.0);
+  s = fma(s, g, 0.5);
+  s = fma(s, g, 1.0);
+  s = fma(s, g, 1.0);
+  return ldexp(s, (int)n);
+}
+
 RGD_DEV double wave_sum_f64(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
