@@ -575,7 +575,8 @@ typedef struct rgd_rotary {
  * positions[s * n + i] (dev int32 [S * n], any value) where positions is given; the slot in the cache stays
  * the former.  q, k, v dev in the cache's type, row s * n + i at q + (s * n + i) * ldq elements [n_heads][D],
  * k and v [Hkv][D]; q_out alike, with ldo: q itself with its stride, or apart from every input.  Values are rounded
- * once, to the cache's type; norms, angles' remainders (taken in fp64) and rotations are fp32.  Rows at or behind n_new[s]
+ * once, to the cache's type; norms, angles' remainders (taken in fp64) and rotations are fp32, so a head's sum of squares is to lie
+ * within fp32's normal numbers, or below them with an eps that does not.  Rows at or behind n_new[s]
  * are left as they were; a token before position 0 or on a page outside the pool gets its q and no K and V.
  * rotary NULL: no rotation.  ld* at least a row's elements; rows 16-byte aligned; eps >= 0 and finite; 1 <= n,
  * S * n <= 2^24, n_heads a multiple of Hkv, at most 1024.  The inputs are apart from the cache.  Asynchronous. */

@@ -65,7 +65,7 @@ constexpr int kWaves = 4;      // per workgroup
 // tokens of all its members; or what is left of the sequences behind that, whose parts are joined with the shared ones:
 // long ones as WHOLE, the others, of up to kTailSteps, a wave or a workgroup each.
 enum Mode { WHOLE, SHARED, OWN, TAIL };
-constexpr int kTailSteps = 24, kAloneSteps = 2, kManyTails = 768;
+constexpr int kTailSteps = 24, kAloneSteps = 2, kManyTails = 768;  // (one load of page numbers covers a tail)
 static_assert(2 * kTailSteps + 1 <= 64, "a tail's pages, of 16 positions at least, are looked up in one load");
 
 // New tokens of sequence s.
@@ -910,9 +910,11 @@ __host__ __device__ inline int tail_groups(const PagedAttnArgs& a) {
 
 // What is left of a sequence behind its shared positions, where that is short: 16 query vectors of a KV head are a
 // workgroup's, whose waves take rounds and shared parts in turn, or, of up to kAloneSteps steps where there are more than
-// the chip holds workgroups, a wave's.  What bounds it is a chain of loads: lengths and plan, pages, K and V, parts (9 us of
-// the 15 that 64 branches of one prompt take; theirs a wave each, 17).  256 branches, 4 to 300 positions left, 8 KV
+// the chip holds workgroups, a wave's.  What bounds it is a chain of loads: lengths and plan, pages, K and V, parts (64
+// branches of one prompt 12 us).  256 branches, 4 to 300 positions left, 8 KV
 // heads: 30 us, a wave for up to 0, 2, 3 and 6 steps 33, 31, 30 and 31; 64 x 5 tokens, 20 vectors: 16, 16, 19 and 21.
+// Pieces of prompts were no part of that choice: each 16 query vectors read what is left of their sequence again (16 sequences of 64,
+// 256 and 512 new tokens behind 4096 shared positions, 32 heads, 158, 570 and 1246 us with the groups' part).
 // There are four workgroups for each four items, of which the first has work where waves do them; these come
 // before all others, so that they meet all parts of the chip.
 template <typename T, int D>
@@ -1087,7 +1089,8 @@ int runs_for(const PagedView& c, int vectors) {
 
 template <typename T, int D, int NT, int MODE>
 hipError_t launch(const PagedAttnArgs& a, int vectors, hipStream_t s) {
-  // no runs where the table holds no own part that is too long for a tail (2 sequences, 100 shared positions: 22 -> 20 us)
+  // no runs where no own part can be too long for a tail: by the table's width, as lengths are on the device (2 sequences, 100
+  // shared positions, a table of up to 768: 22 -> 20 us; wider tables pay 5 us a layer for a launch that may have nothing to do)
   const int runs = MODE == OWN && a.c.width * a.c.ps <= kTailSteps * kStep ? 0 : runs_for(a.c, vectors);
   // PAST where a round of a wave takes all positions of a page's V row, and so whole cache lines; where waves share
   // lines, the second one is to find them.  64 ragged sequences to 8192, pages of 16: 47 us, 51 without; one of 131072,

@@ -4,7 +4,8 @@
 // y = x / sqrt(mean(x^2) + eps) * gain for each head of q and k; the pair (a, b) of the first `dim` dimensions becomes
 // scale (a cos - b sin, b cos + a sin) of the angle position * freq.  Reading the rows once and writing them once bounds
 // it from below, at 5.35 TB/s; the operations on a row, some 110 a lane, are the greater part of the rest.  8 x 1000 tokens
-// of 32 + 8 + 8 heads of 128 in bf16, 109 MB: 26 us in the trace, 4.1 TB/s (32 a call).  One token: 5.9 us (7.6 a call), of
+// of 32 + 8 + 8 heads of 128 in bf16, 109 MB: 26 us, 4.1 TB/s, where the last-level cache still holds the rows, and 32 to 34, 3.3 TB/s,
+// where it does not.  Pairs of neighbours 26 us, of half a head 28, at odd distances 31; fp32 55 to 62.  One token: 5.9 us (7.6 a call), of
 // which the launch and three loads that need one another's results are most.
 //
 // An angle enters as a part of a turn: position * (freq / 2 pi) and its distance from the nearest whole number in fp64

@@ -10,9 +10,10 @@
 // it has to and sums those that are kept for certain by chunks of 512 ids; the ids in the borders' bins go to a list.  The
 // last, one workgroup a row, finds the borders among the listed ids by exact sums, the chunk that the draw falls in and
 // its id.  The bins only say where to look: a border that is not there, or more listed ids than there is room for, is
-// noticed, and the row is searched as a whole.
+// noticed, and the row is searched as a whole; where min_p's border seems to be above top_p's that is certain by bounds of
+// the bins' weights, or compared at the end by exact ones.
 //
-// Measured, the four in order: 256 rows of 152064 logits (156 MB), all of one limit on the sum, 29 + 7 + 57 + 19 us: the
+// Measured, the four in order: 256 rows of 152064 logits (156 MB), all of one limit on the sum, 29 + 7 + 60 + 20 us: the
 // first is the stream at 5.4 TB/s, the third about 30 instructions an id, the last a chain of
 // reads and sums a row.  One row of 128256 5 + 10 + 4 + 15: launches and chains.  (The whole row ordered by radix passes in
 // place of the bins: 1137 and 481 us.)
